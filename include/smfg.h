@@ -294,6 +294,94 @@ int smfg_sage_layer(const int32_t *d_indptr, const int32_t *d_indices, int64_t m
                     int32_t dim, const void *d_w_packed, const float *d_bias, int32_t out_dim, int32_t relu,
                     void *d_out, int32_t out_elem_bytes, void *hip_stream);
 
+/*
+ * Operators of a training step over the prepared batches, for what the paper's training loop (Listing 1) leaves to its
+ * framework: learned features of nodes that have none and their gradient, layer normalisation and its gradient, and the
+ * clipping of all gradients by their global norm.  All are asynchronous on hip_stream, on the current device, allocate and
+ * synchronise nothing, and can be captured.  As for the other consumers, the number of rows in use is a device int64 (e.g.
+ * &counts[L]), read as at least 0 and at most the max_* that bounds the launch; rows of an output beyond it are not written.
+ * Sums run in float or wider and a result is rounded to its type once.  The same inputs give the same bits.
+ * Element types are SMFG_DTYPE_*; matrices are row-major with their rows `stride` elements apart (>= dim); dim is in
+ * [1, SMFG_MAX_DIM].  Scratch is the caller's device memory of *_scratch_bytes bytes (host only, pure; -1 for sizes that
+ * the call refuses), 256-byte aligned, not shared by calls that overlap in time; a call with less returns SMFG_ERR_CAPACITY.
+ */
+#define SMFG_DTYPE_F32 0  /* float */
+#define SMFG_DTYPE_F16 1  /* IEEE half */
+#define SMFG_DTYPE_BF16 2 /* bfloat16 */
+#define SMFG_MAX_DIM (1 << 23)
+
+/*
+ * Embedding: out[i, :] = scale * table[ids[i], :], i < *d_num_ids; a row of zeros for an id outside [0, num_rows) (a padded
+ * place): no read leaves the table.
+ *   d_table  num_rows x dim, 1 <= num_rows < 2^31;  d_ids  int32 or int64 (id_bytes 4 or 8) [max_ids], max_ids < 2^31
+ *   d_out    max_ids x dim, of the table's type, or of any type where the table is of float
+ */
+int smfg_embedding(const void *d_table, int64_t num_rows, int64_t table_stride, int32_t table_dtype, const void *d_ids,
+                   int32_t id_bytes, const int64_t *d_num_ids, int64_t max_ids, int32_t dim, float scale, void *d_out,
+                   int64_t out_stride, int32_t out_dtype, void *hip_stream);
+
+/*
+ * Its gradient: G[v, :] = scale * sum of dy[i, :] over i < *d_num_ids with ids[i] = v, in the order of i; ids outside
+ * [0, num_rows) have none.  d_dy: max_ids x dim.  The gradient is of float or of dy's type.
+ *   smfg_embedding_grad       the whole table's, num_rows x dim: rows that no id names are zeros; with accumulate != 0 it
+ *                             is added to what d_grad holds, and those rows are not touched
+ *   smfg_embedding_grad_rows  the touched rows alone: their number *d_num_unique, their ids ascending in d_row_ids [max_ids] and
+ *                             their sums in d_grad (max_ids x dim); nothing is written past *d_num_unique
+ * With S = |scale| * sum |dy| over the k summed values (and the value added to) the error of a float result is at most
+ * (k + 2) * 2^-24 * S.
+ */
+int64_t smfg_embedding_grad_scratch_bytes(int64_t max_ids, int64_t num_rows, int32_t dim);
+int smfg_embedding_grad(const void *d_ids, int32_t id_bytes, const int64_t *d_num_ids, int64_t max_ids, const void *d_dy,
+                        int64_t dy_stride, int32_t dy_dtype, int32_t dim, float scale, void *d_grad, int64_t num_rows,
+                        int64_t grad_stride, int32_t grad_dtype, int32_t accumulate, void *d_scratch, int64_t scratch_bytes,
+                        void *hip_stream);
+int smfg_embedding_grad_rows(const void *d_ids, int32_t id_bytes, const int64_t *d_num_ids, int64_t max_ids,
+                             const void *d_dy, int64_t dy_stride, int32_t dy_dtype, int32_t dim, float scale,
+                             int64_t num_rows, int32_t *d_row_ids, int64_t *d_num_unique, void *d_grad,
+                             int64_t grad_stride, int32_t grad_dtype, void *d_scratch, int64_t scratch_bytes,
+                             void *hip_stream);
+
+/*
+ * Layer norm of rows i < *d_num_rows:
+ *   m_i = mean of x[i, :],  r_i = 1 / sqrt(mean of (x[i, :] - m_i)^2 + eps),  y[i, j] = (x[i, j] - m_i) r_i w[j] + b[j]
+ *   d_x, d_y  of dtype; y may be x with the same stride.  d_w, d_b: [dim] of param_dtype, which is float or dtype; either
+ *             may be NULL (ones, zeros).  eps >= 0.
+ *   d_mean, d_rstd  float [max_rows] for the gradient, or NULL
+ */
+int smfg_layer_norm(const void *d_x, int64_t x_stride, int32_t dtype, const int64_t *d_num_rows, int64_t max_rows,
+                    int32_t dim, const void *d_w, const void *d_b, int32_t param_dtype, float eps, void *d_y,
+                    int64_t y_stride, float *d_mean, float *d_rstd, void *hip_stream);
+/*
+ * Its gradient, with h = (x - m) r and g = dy w:
+ *   dx = r (g - mean(g) - h mean(g h)),  dw[j] = sum over rows of dy h,  db[j] = sum over rows of dy
+ *   d_dy, d_x, d_dx  of dtype; dx may be dy or x with the same stride.  d_w as above.  d_dx NULL, or d_dw and d_db NULL (or one
+ *   of them): not wanted.  d_dw, d_db: [dim] of param_dtype.
+ */
+int64_t smfg_layer_norm_grad_scratch_bytes(int64_t max_rows, int32_t dim);
+int smfg_layer_norm_grad(const void *d_dy, int64_t dy_stride, const void *d_x, int64_t x_stride, int32_t dtype,
+                         const int64_t *d_num_rows, int64_t max_rows, int32_t dim, const void *d_w, int32_t param_dtype,
+                         const float *d_mean, const float *d_rstd, void *d_dx, int64_t dx_stride, void *d_dw, void *d_db,
+                         void *d_scratch, int64_t scratch_bytes, void *hip_stream);
+
+/*
+ * Global norm over any number of gradients, and clipping:
+ *   N = sqrt(sum over all elements of (scale g)^2),  out = scale * min(1, max_norm / (N + 1e-6)) * g
+ * scale undoes a loss scale or averages micro-batches; max_norm > 0, infinite: no clipping.  *d_norm = N (device float).  Squares
+ * are added in double.  A NaN among the gradients makes N and all outputs NaN; an infinite one makes N infinite, so finite ones 0.
+ * Gradients that are clipped in place are not written again where scale and factor multiply to one.
+ */
+typedef struct {
+  const void *grad;      /* device, numel contiguous elements of dtype */
+  void *out;             /* device, of out_dtype: dtype, or float; NULL: in place */
+  int64_t numel;         /* >= 0 */
+  int32_t dtype, out_dtype;
+  const int64_t *d_rows; /* device: only the first *d_rows rows of row_elems elements count (the d_num_unique of a */
+  int64_t row_elems;     /* gradient of touched rows); NULL: all do */
+} smfg_grad_t;
+int64_t smfg_clip_grad_norm_scratch_bytes(const smfg_grad_t *grads, int32_t num_grads);
+int smfg_clip_grad_norm(const smfg_grad_t *grads /* host */, int32_t num_grads, float scale, float max_norm, float *d_norm,
+                        void *d_scratch, int64_t scratch_bytes, void *hip_stream);
+
 /* Copies counts[0 .. 2L+2) to the host after synchronising the stream; returns SMFG_OK or, if the
  * status word is non-zero, its (positive) SMFG_ST_* value. */
 int smfg_read_counts(const smfg_output_t *out, int32_t L, int64_t *h_counts, void *hip_stream);

@@ -35,7 +35,9 @@ EXPORTS = [
     "smfg_workspace_destroy", "smfg_workspace_bytes", "smfg_workspace_strategy", "smfg_sample_mfg", "smfg_sample_mfg_many",
     "smfg_sample_mfg_static",
     "smfg_gather_rows", "smfg_gather_many", "smfg_mean_aggregate", "smfg_sage_layer", "smfg_sage_pack_weights",
-    "smfg_sage_packed_bytes", "smfg_read_counts", "smfg_strerror", "smfg_profile_begin", "smfg_profile_end",
+    "smfg_sage_packed_bytes", "smfg_embedding", "smfg_embedding_grad_scratch_bytes", "smfg_embedding_grad", "smfg_embedding_grad_rows",
+    "smfg_layer_norm", "smfg_layer_norm_grad_scratch_bytes", "smfg_layer_norm_grad", "smfg_clip_grad_norm_scratch_bytes",
+    "smfg_clip_grad_norm", "smfg_read_counts", "smfg_strerror", "smfg_profile_begin", "smfg_profile_end",
 ]
 STAGES = ["clear", "seeds", "sample_insert", "flag_rows", "scan_tiles", "assemble", "gather",
           "mean_aggregate", "sage_layer", "partition", "dedup_buckets"]
@@ -60,6 +62,18 @@ class _Output(ctypes.Structure):
     ]
 
 
+class _Grad(ctypes.Structure):
+    _fields_ = [
+        ("grad", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("numel", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32),
+        ("d_rows", ctypes.c_void_p),
+        ("row_elems", ctypes.c_int64),
+    ]
+
+
 _lib = None
 
 
@@ -80,7 +94,6 @@ def lib() -> ctypes.CDLL:
         L.smfg_workspace_create_sized.argtypes = [pp, vp, i32, i32, ctypes.POINTER(i32), i64, i64]
         L.smfg_workspace_destroy.argtypes = [vp]
         L.smfg_workspace_bytes.argtypes = [vp]
-        L.smfg_workspace_bytes.restype = i64
         L.smfg_workspace_strategy.argtypes = [vp]
         L.smfg_sample_mfg.argtypes = [vp, vp, vp, i32, ctypes.POINTER(i32), i32, u64,
                                       ctypes.POINTER(_Output), vp]
@@ -92,16 +105,26 @@ def lib() -> ctypes.CDLL:
         L.smfg_mean_aggregate.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, i32, vp, vp]
         L.smfg_sage_layer.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, vp, vp, i32, i32, vp, i32, vp]
         L.smfg_sage_packed_bytes.argtypes = [i32, i32]
-        L.smfg_sage_packed_bytes.restype = i64
         L.smfg_sage_pack_weights.argtypes = [vp, i32, i32, vp, vp]
+        f32, sizes = ctypes.c_float, ("smfg_workspace_bytes", "smfg_sage_packed_bytes", "smfg_embedding_grad_scratch_bytes",
+                                      "smfg_layer_norm_grad_scratch_bytes", "smfg_clip_grad_norm_scratch_bytes")
+        L.smfg_embedding.argtypes = [vp, i64, i64, i32, vp, i32, vp, i64, i32, f32, vp, i64, i32, vp]
+        L.smfg_embedding_grad_scratch_bytes.argtypes = [i64, i64, i32]
+        L.smfg_embedding_grad.argtypes = [vp, i32, vp, i64, vp, i64, i32, i32, f32, vp, i64, i64, i32, i32, vp, i64, vp]
+        L.smfg_embedding_grad_rows.argtypes = [vp, i32, vp, i64, vp, i64, i32, i32, f32, i64, vp, vp, vp, i64, i32, vp, i64, vp]
+        L.smfg_layer_norm.argtypes = [vp, i64, i32, vp, i64, i32, vp, vp, i32, f32, vp, i64, vp, vp, vp]
+        L.smfg_layer_norm_grad_scratch_bytes.argtypes = [i64, i32]
+        L.smfg_layer_norm_grad.argtypes = [vp, i64, vp, i64, i32, vp, i64, i32, vp, i32, vp, vp, vp, i64, vp, vp, vp, i64, vp]
+        L.smfg_clip_grad_norm_scratch_bytes.argtypes = [ctypes.POINTER(_Grad), i32]
+        L.smfg_clip_grad_norm.argtypes = [ctypes.POINTER(_Grad), i32, f32, f32, vp, vp, i64, vp]
         L.smfg_read_counts.argtypes = [ctypes.POINTER(_Output), i32, ctypes.POINTER(i64), vp]
         L.smfg_profile_begin.argtypes = [i32, i32]
         L.smfg_profile_end.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i64)]
         L.smfg_strerror.argtypes = [ctypes.c_int]
         L.smfg_strerror.restype = ctypes.c_char_p
         for name in EXPORTS:
-            if name not in ("smfg_workspace_bytes", "smfg_strerror", "smfg_sage_packed_bytes"):
-                getattr(L, name).restype = ctypes.c_int
+            if name != "smfg_strerror":
+                getattr(L, name).restype = i64 if name in sizes else ctypes.c_int
         _lib = L
     return _lib
 
@@ -396,6 +419,168 @@ def sage_layer(indptr: torch.Tensor, indices: torch.Tensor, num_dst: torch.Tenso
                                int(bool(relu)), ctypes.c_void_p(out.data_ptr()), out.element_size(),
                                _stream_ptr(stream))
     _check(rc, "smfg_sage_layer")
+
+
+# ---- operators of a training step ---------------------------------------------------------------
+
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+class Scratch:
+    """Device memory that a call works in; keep it from call to call, one per call that may be in flight."""
+
+    def __init__(self, nbytes: int, where: str, device=None):
+        if nbytes < 0:
+            raise SmfgError(ERR_INVALID_ARG, where)
+        self.nbytes = nbytes
+        self.data = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device if device is not None else "cuda")
+
+
+def _matrix(t: torch.Tensor, rows: int, name: str):
+    """(address, row stride in elements, type) of a matrix with at least `rows` rows."""
+    assert t.dim() == 2 and t.dtype in DTYPES and t.is_cuda, name
+    assert t.shape[1] == 1 or t.stride(1) == 1, name
+    assert t.shape[0] >= rows, name
+    # the stride of a single row means nothing, and torch may report any
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]), DTYPES[t.dtype]
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype, name: str):
+    if t is None:
+        return None
+    assert t.is_contiguous() and t.numel() >= n and t.dtype == dtype and t.is_cuda, name
+    return t.data_ptr()
+
+
+def embedding(table: torch.Tensor, ids: torch.Tensor, num_ids: torch.Tensor, max_ids: int, out: torch.Tensor, scale: float = 1.0,
+              stream: Optional[torch.cuda.Stream] = None) -> None:
+    """out[i] = scale * table[ids[i]] for i < num_ids (device int64); zeros for an id outside the table.  ids int32 or int64; out of
+    the table's type, or of any where the table is float32."""
+    assert ids.dtype in (torch.int32, torch.int64)
+    assert out.dim() == 2 and table.dim() == 2 and out.shape[1] == table.shape[1]
+    t, ts, tt = _matrix(table, 1, "table")
+    o, os_, ot = _matrix(out, max_ids, "out")
+    rc = lib().smfg_embedding(t, table.shape[0], ts, tt, _vector(ids, max_ids, ids.dtype, "ids"), ids.element_size(),
+                              _vector(num_ids, 1, torch.int64, "num_ids"), max_ids, table.shape[1], scale, o, os_, ot, _stream_ptr(stream))
+    _check(rc, "smfg_embedding")
+
+
+def embedding_grad_workspace(max_ids: int, num_rows: int, dim: int, device=None) -> Scratch:
+    """Scratch of embedding_grad and embedding_grad_rows for up to max_ids ids."""
+    return Scratch(int(lib().smfg_embedding_grad_scratch_bytes(max_ids, num_rows, dim)), "smfg_embedding_grad_scratch_bytes", device)
+
+
+def embedding_grad(ids: torch.Tensor, num_ids: torch.Tensor, max_ids: int, grad_out: torch.Tensor, grad_table: torch.Tensor, ws: Scratch,
+                   scale: float = 1.0, accumulate: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """grad_table[v] = scale * sum of grad_out[i] over ids[i] == v, all other rows zero; with accumulate it is added to grad_table.
+    grad_table float32 or of grad_out's type."""
+    assert ids.dtype in (torch.int32, torch.int64)
+    assert grad_out.dim() == 2 and grad_table.dim() == 2 and grad_out.shape[1] == grad_table.shape[1]
+    d, ds, dt = _matrix(grad_out, max_ids, "grad_out")
+    g, gs, gt = _matrix(grad_table, 1, "grad_table")
+    rc = lib().smfg_embedding_grad(_vector(ids, max_ids, ids.dtype, "ids"), ids.element_size(), _vector(num_ids, 1, torch.int64, "num_ids"),
+                                   max_ids, d, ds, dt, grad_out.shape[1], scale, g, grad_table.shape[0], gs, gt, int(bool(accumulate)),
+                                   ws.data.data_ptr(), ws.nbytes, _stream_ptr(stream))
+    _check(rc, "smfg_embedding_grad")
+
+
+def embedding_grad_rows(ids: torch.Tensor, num_ids: torch.Tensor, max_ids: int, grad_out: torch.Tensor, num_rows: int, row_ids: torch.Tensor,
+                        num_unique: torch.Tensor, grad_rows: torch.Tensor, ws: Scratch, scale: float = 1.0,
+                        stream: Optional[torch.cuda.Stream] = None) -> None:
+    """The touched rows of a table of num_rows rows alone: their number (num_unique, device int64), their ids ascending (row_ids,
+    int32 [max_ids]) and their gradients (grad_rows [max_ids x dim], float32 or of grad_out's type)."""
+    assert ids.dtype in (torch.int32, torch.int64)
+    assert grad_out.dim() == 2 and grad_rows.dim() == 2 and grad_out.shape[1] == grad_rows.shape[1]
+    d, ds, dt = _matrix(grad_out, max_ids, "grad_out")
+    g, gs, gt = _matrix(grad_rows, max_ids, "grad_rows")
+    rc = lib().smfg_embedding_grad_rows(_vector(ids, max_ids, ids.dtype, "ids"), ids.element_size(), _vector(num_ids, 1, torch.int64, "num_ids"),
+                                        max_ids, d, ds, dt, grad_out.shape[1], scale, num_rows, _vector(row_ids, max_ids, torch.int32, "row_ids"),
+                                        _vector(num_unique, 1, torch.int64, "num_unique"), g, gs, gt, ws.data.data_ptr(), ws.nbytes,
+                                        _stream_ptr(stream))
+    _check(rc, "smfg_embedding_grad_rows")
+
+
+def layer_norm(x: torch.Tensor, num_rows: torch.Tensor, max_rows: int, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], eps: float,
+               y: torch.Tensor, mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> None:
+    """y[i] = (x[i] - mean) * rstd * weight + bias for i < num_rows (device int64); mean and rstd (float32 [max_rows]) are what
+    layer_norm_grad needs.  weight and bias float32 or of x's type, or None; y of x's type, and may be x."""
+    assert x.dim() == 2 and y.dim() == 2 and x.shape[1] == y.shape[1] and x.dtype == y.dtype
+    a, as_, at = _matrix(x, max_rows, "x")
+    o, os_, _ = _matrix(y, max_rows, "y")
+    pd = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
+    assert pd in DTYPES
+    rc = lib().smfg_layer_norm(a, as_, at, _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, x.shape[1], _vector(weight, x.shape[1], pd, "weight"),
+                               _vector(bias, x.shape[1], pd, "bias"), DTYPES[pd], eps, o, os_, _vector(mean, max_rows, torch.float32, "mean"),
+                               _vector(rstd, max_rows, torch.float32, "rstd"), _stream_ptr(stream))
+    _check(rc, "smfg_layer_norm")
+
+
+def layer_norm_grad_workspace(max_rows: int, dim: int, device=None) -> Scratch:
+    """Scratch of layer_norm_grad for up to max_rows rows."""
+    return Scratch(int(lib().smfg_layer_norm_grad_scratch_bytes(max_rows, dim)), "smfg_layer_norm_grad_scratch_bytes", device)
+
+
+def layer_norm_grad(grad_y: torch.Tensor, x: torch.Tensor, num_rows: torch.Tensor, max_rows: int, weight: Optional[torch.Tensor],
+                    mean: torch.Tensor, rstd: torch.Tensor, grad_x: Optional[torch.Tensor], grad_weight: Optional[torch.Tensor],
+                    grad_bias: Optional[torch.Tensor], ws: Optional[Scratch], stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Gradients of layer_norm's input, weight and bias; None where one is not wanted (without the last two, ws may be None).
+    grad_x is of x's type and may be grad_y; grad_weight and grad_bias are of weight's type."""
+    assert x.dim() == 2 and grad_y.shape[1] == x.shape[1] and grad_y.dtype == x.dtype
+    dim = int(x.shape[1])
+    d, ds, _ = _matrix(grad_y, max_rows, "grad_y")
+    a, as_, at = _matrix(x, max_rows, "x")
+    gx, gs = None, 0
+    if grad_x is not None:
+        assert grad_x.shape[1] == dim and grad_x.dtype == x.dtype
+        gx, gs, _ = _matrix(grad_x, max_rows, "grad_x")
+    pd = next((t.dtype for t in (weight, grad_weight, grad_bias) if t is not None), torch.float32)
+    assert pd in DTYPES
+    rc = lib().smfg_layer_norm_grad(d, ds, a, as_, at, _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, dim, _vector(weight, dim, pd, "weight"),
+                                    DTYPES[pd], _vector(mean, max_rows, torch.float32, "mean"), _vector(rstd, max_rows, torch.float32, "rstd"), gx, gs,
+                                    _vector(grad_weight, dim, pd, "grad_weight"), _vector(grad_bias, dim, pd, "grad_bias"),
+                                    ws.data.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0, _stream_ptr(stream))
+    _check(rc, "smfg_layer_norm_grad")
+
+
+class GradList:
+    """Gradients to be clipped together, their outputs and scratch; keeps the tensors alive."""
+
+    def __init__(self, c, n: int, scratch: Scratch, tensors):
+        self.c, self.n, self.scratch, self.tensors = c, n, scratch, tensors
+
+
+def grad_list(grads: Sequence[torch.Tensor], outs: Optional[Sequence[Optional[torch.Tensor]]] = None,
+              rows: Optional[Sequence[Optional[torch.Tensor]]] = None, device=None) -> GradList:
+    """The buffers that clip_grad_norm reads and writes: contiguous gradients; outs[i] the buffer of a clipped one, of its type or
+    float32 (None: in place); rows[i] (device int64) how many of its rows count (None: all), as embedding_grad_rows tells it.
+    What the buffers hold is read by each call anew."""
+    n = len(grads)
+    assert (outs is None or len(outs) == n) and (rows is None or len(rows) == n)
+    c = (_Grad * max(1, n))()
+    for i, g in enumerate(grads):
+        assert g.dtype in DTYPES and g.is_contiguous() and g.is_cuda
+        e = c[i]
+        e.grad, e.numel, e.dtype = g.data_ptr(), g.numel(), DTYPES[g.dtype]
+        o = outs[i] if outs is not None else None
+        if o is not None:
+            assert o.dtype in DTYPES and o.is_contiguous() and o.is_cuda and o.numel() == g.numel()
+            e.out, e.out_dtype = o.data_ptr(), DTYPES[o.dtype]
+        r = rows[i] if rows is not None else None
+        if r is not None:
+            e.d_rows, e.row_elems = _vector(r, 1, torch.int64, "rows"), max(1, g.numel() // max(1, g.shape[0]))
+    nbytes = int(lib().smfg_clip_grad_norm_scratch_bytes(c, n))
+    if device is None and n > 0:
+        device = grads[0].device
+    return GradList(c, n, Scratch(nbytes, "smfg_clip_grad_norm_scratch_bytes", device), (list(grads), outs, rows))
+
+
+def clip_grad_norm(grads: GradList, max_norm: float, norm: torch.Tensor, scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """norm (float32, one element) = the 2-norm of all gradients times scale; every gradient is multiplied by
+    scale * min(1, max_norm / (norm + 1e-6)).  max_norm may be infinite."""
+    rc = lib().smfg_clip_grad_norm(grads.c, grads.n, scale, max_norm, _vector(norm, 1, torch.float32, "norm"), grads.scratch.data.data_ptr(),
+                                   grads.scratch.nbytes, _stream_ptr(stream))
+    _check(rc, "smfg_clip_grad_norm")
 
 
 def read_counts(out: Output, stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> List[int]:

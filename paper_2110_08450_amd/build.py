@@ -7,6 +7,7 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SRC = os.path.join(_HERE, "csrc", "smfg.hip")
+SOURCES = [SRC, os.path.join(_HERE, "csrc", "train.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(_HERE, "libsmfg.so")
 
@@ -22,7 +23,7 @@ def build_lib(verbose: bool = False) -> str:
     cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            "-Wall", "-Wno-unused-command-line-argument",
-           "-I", INCLUDE, SRC, "-o", LIB]
+           "-I", INCLUDE, *SOURCES, "-o", LIB]
     if verbose:
         print(" ".join(cmd))
     subprocess.check_call(cmd)

@@ -1,0 +1,333 @@
+// libsmfg layer norm over rows, and its gradient.
+//
+//   m = mean(x_i), r = 1 / sqrt(mean((x_i - m)^2) + eps), y_ij = (x_ij - m) r w_j + b_j
+//   h = (x - m) r, g = dy w:  dx = r (g - mean(g) - h mean(g h)),  dw_j = sum_i dy_ij h_ij,  db_j = sum_i dy_ij
+#ifndef SMFG_KERNELS_NORM_H_
+#define SMFG_KERNELS_NORM_H_
+
+#include "elements.h"
+
+namespace smfg_dev {
+
+struct NormArgs {
+  const void* x;
+  int64_t x_stride;
+  const int64_t* num;
+  int64_t max_rows;
+  int32_t dim;
+  int32_t float_params;
+  const void* w;
+  const void* b;
+  float eps;
+  void* y;
+  int64_t y_stride;
+  float* mean;
+  float* rstd;
+};
+
+// A group of LANES lanes has a row in its registers, NV vectors of V columns a lane: read once, centred before it is squared.
+template <typename T, int V, int NV, int LANES>
+__global__ void __launch_bounds__(kThreads) k_layer_norm(NormArgs A) {
+  __shared__ float lds[kThreads / 64];
+  constexpr int kGroups = kThreads / LANES;
+  const int lane = threadIdx.x % LANES;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES;
+  if (row >= count_of(A.num, A.max_rows)) return;
+  const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
+  float v[NV][V];
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const Columns<V> c(k * LANES + lane, A.dim);
+    Elems<T, V> e = {};
+    if (c.dup < V) e = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      v[k][j] = as_float(e.v[j]);
+      s += j >= c.dup ? v[k][j] : 0.f;
+    }
+  }
+  const float m = group_sum<LANES>(s, lds) / static_cast<float>(A.dim);
+  s = 0.f;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const Columns<V> c(k * LANES + lane, A.dim);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      v[k][j] -= m;
+      s += j >= c.dup ? v[k][j] * v[k][j] : 0.f;
+    }
+  }
+  const float r = 1.f / sqrtf(group_sum<LANES>(s, lds) / static_cast<float>(A.dim) + A.eps);
+  if (lane == 0) {
+    if (A.mean) A.mean[row] = m;
+    if (A.rstd) A.rstd[row] = r;
+  }
+  T* y = static_cast<T*>(A.y) + row * A.y_stride;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const Columns<V> c(k * LANES + lane, A.dim);
+    if (c.dup == V) continue;
+    float w[V], b[V];
+    load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w);
+    load_params<T, V>(A.b, A.float_params != 0, c.start, 0.f, b);
+    Elems<T, V> e;
+#pragma unroll
+    for (int j = 0; j < V; ++j) e.v[j] = from_float<T>(v[k][j] * r * w[j] + b[j]);
+    *reinterpret_cast<Elems<T, V>*>(y + c.start) = e;
+  }
+}
+
+// Rows that outgrow the registers of a block: one to a block, read three times.  The columns that the last vector shares with the
+// one before are written once, as y may be x.
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads) k_layer_norm_long(NormArgs A) {
+  __shared__ float lds[kThreads / 64];
+  const int64_t row = blockIdx.x;
+  if (row >= count_of(A.num, A.max_rows)) return;
+  const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
+  const int vectors = (A.dim + V - 1) / V;
+  float s = 0.f;
+  for (int i = threadIdx.x; i < vectors; i += kThreads) {
+    const Columns<V> c(i, A.dim);
+    const Elems<T, V> e = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
+#pragma unroll
+    for (int j = 0; j < V; ++j) s += j >= c.dup ? as_float(e.v[j]) : 0.f;
+  }
+  const float m = group_sum<kThreads>(s, lds) / static_cast<float>(A.dim);
+  s = 0.f;
+  for (int i = threadIdx.x; i < vectors; i += kThreads) {
+    const Columns<V> c(i, A.dim);
+    const Elems<T, V> e = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float d = as_float(e.v[j]) - m;
+      s += j >= c.dup ? d * d : 0.f;
+    }
+  }
+  const float r = 1.f / sqrtf(group_sum<kThreads>(s, lds) / static_cast<float>(A.dim) + A.eps);
+  if (threadIdx.x == 0) {
+    if (A.mean) A.mean[row] = m;
+    if (A.rstd) A.rstd[row] = r;
+  }
+  T* y = static_cast<T*>(A.y) + row * A.y_stride;
+  for (int i = threadIdx.x; i < vectors; i += kThreads) {
+    const Columns<V> c(i, A.dim);
+    const Elems<T, V> e = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
+    float w[V], b[V];
+    load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w);
+    load_params<T, V>(A.b, A.float_params != 0, c.start, 0.f, b);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (j >= c.dup) y[c.start + j] = from_float<T>((as_float(e.v[j]) - m) * r * w[j] + b[j]);
+  }
+}
+
+struct NormGradArgs {
+  const void* dy;
+  int64_t dy_stride;
+  const void* x;
+  int64_t x_stride;
+  const int64_t* num;
+  int64_t max_rows;
+  int32_t dim;
+  int32_t float_params;
+  const void* w;
+  const float* mean;
+  const float* rstd;
+  void* dx;  // or null
+  int64_t dx_stride;
+  float* part;  // [slices][2][dim]: sums of dy h and of dy over the rows of a slice, or null
+};
+
+// As k_layer_norm, a block striding over rows: a lane's columns are the same in each of them, so the sums for dw and db stay in
+// its registers until the block is done, and leave it once, as a slice of `part`.
+template <typename T, int V, int NV, int LANES>
+__global__ void __launch_bounds__(kThreads) k_layer_norm_grad(NormGradArgs A) {
+  __shared__ float lds[kThreads / 64];
+  constexpr int kGroups = kThreads / LANES;
+  const int lane = threadIdx.x % LANES;
+  const int64_t n = count_of(A.num, A.max_rows);
+  const float inv = 1.f / static_cast<float>(A.dim);
+  float w[NV][V], dw[NV][V], db[NV][V];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const Columns<V> c(k * LANES + lane, A.dim);
+#pragma unroll
+    for (int j = 0; j < V; ++j) w[k][j] = dw[k][j] = db[k][j] = 0.f;
+    if (c.dup < V) load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w[k]);
+  }
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES; row < n;
+       row += static_cast<int64_t>(gridDim.x) * kGroups) {
+    const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
+    const T* dy = static_cast<const T*>(A.dy) + row * A.dy_stride;
+    const float m = A.mean[row], r = A.rstd[row];
+    float h[NV][V], g[NV][V];
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const Columns<V> c(k * LANES + lane, A.dim);
+      Elems<T, V> ex = {}, ey = {};
+      if (c.dup < V) {
+        ex = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
+        ey = *reinterpret_cast<const Elems<T, V>*>(dy + c.start);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        h[k][j] = (as_float(ex.v[j]) - m) * r;
+        const float d = as_float(ey.v[j]);
+        dw[k][j] += d * h[k][j];
+        db[k][j] += d;
+        g[k][j] = d * w[k][j];
+        s1 += j >= c.dup ? g[k][j] : 0.f;
+        s2 += j >= c.dup ? g[k][j] * h[k][j] : 0.f;
+      }
+    }
+    if (!A.dx) continue;
+    const float c1 = group_sum<LANES>(s1, lds) * inv, c2 = group_sum<LANES>(s2, lds) * inv;
+    T* dx = static_cast<T*>(A.dx) + row * A.dx_stride;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const Columns<V> c(k * LANES + lane, A.dim);
+      if (c.dup == V) continue;
+      Elems<T, V> e;
+#pragma unroll
+      for (int j = 0; j < V; ++j) e.v[j] = from_float<T>(r * (g[k][j] - c1 - h[k][j] * c2));
+      *reinterpret_cast<Elems<T, V>*>(dx + c.start) = e;
+    }
+  }
+  if (!A.part) return;
+  // groups of a wave, then waves, always in the same order
+  constexpr int kWidth = LANES * NV * V;
+  __shared__ float sums[LANES <= 64 ? kThreads / 64 * kWidth : 1];
+  float* out = A.part + static_cast<int64_t>(blockIdx.x) * 2 * A.dim;
+#pragma unroll
+  for (int what = 0; what < 2; ++what) {
+    float(&acc)[NV][V] = what == 0 ? dw : db;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int o = LANES; o < 64; o <<= 1) acc[k][j] += __shfl_xor(acc[k][j], o, 64);
+    }
+    if constexpr (LANES > 64) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const Columns<V> c(k * LANES + lane, A.dim);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (j >= c.dup) out[what * static_cast<int64_t>(A.dim) + c.start + j] = acc[k][j];
+      }
+    } else {
+      __syncthreads();
+      if ((threadIdx.x & 63) < LANES) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int j = 0; j < V; ++j) sums[(threadIdx.x >> 6) * kWidth + (k * V + j) * LANES + lane] = acc[k][j];
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < kWidth; i += kThreads) {
+        const int kj = i / LANES;
+        const Columns<V> c(kj / V * LANES + i % LANES, A.dim);
+        const int j = kj % V;
+        if (j < c.dup) continue;
+        float s = 0.f;
+#pragma unroll
+        for (int q = 0; q < kThreads / 64; ++q) s += sums[q * kWidth + i];
+        out[what * static_cast<int64_t>(A.dim) + c.start + j] = s;
+      }
+    }
+  }
+}
+
+// Rows that outgrow the registers of a block: dx by a block per row, which reads it twice; the sums by k_norm_grad_columns.
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads) k_layer_norm_grad_long(NormGradArgs A) {
+  __shared__ float lds[kThreads / 64];
+  const int64_t row = blockIdx.x;
+  if (row >= count_of(A.num, A.max_rows)) return;
+  const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
+  const T* dy = static_cast<const T*>(A.dy) + row * A.dy_stride;
+  T* dx = static_cast<T*>(A.dx) + row * A.dx_stride;
+  const float m = A.mean[row], r = A.rstd[row], inv = 1.f / static_cast<float>(A.dim);
+  const int vectors = (A.dim + V - 1) / V;
+  float s1 = 0.f, s2 = 0.f;
+  for (int i = threadIdx.x; i < vectors; i += kThreads) {
+    const Columns<V> c(i, A.dim);
+    const Elems<T, V> ex = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
+    const Elems<T, V> ey = *reinterpret_cast<const Elems<T, V>*>(dy + c.start);
+    float w[V];
+    load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float g = as_float(ey.v[j]) * w[j], h = (as_float(ex.v[j]) - m) * r;
+      s1 += j >= c.dup ? g : 0.f;
+      s2 += j >= c.dup ? g * h : 0.f;
+    }
+  }
+  const float c1 = group_sum<kThreads>(s1, lds) * inv, c2 = group_sum<kThreads>(s2, lds) * inv;
+  for (int i = threadIdx.x; i < vectors; i += kThreads) {
+    const Columns<V> c(i, A.dim);
+    const Elems<T, V> ex = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
+    const Elems<T, V> ey = *reinterpret_cast<const Elems<T, V>*>(dy + c.start);
+    float w[V];
+    load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float g = as_float(ey.v[j]) * w[j], h = (as_float(ex.v[j]) - m) * r;
+      if (j >= c.dup) dx[c.start + j] = from_float<T>(r * (g - c1 - h * c2));
+    }
+  }
+}
+
+// Slice blockIdx.y of the rows, V columns a thread.  Where dx takes the place of dy or x it has to run before it.
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads) k_norm_grad_columns(NormGradArgs A) {
+  const int64_t n = count_of(A.num, A.max_rows);
+  const Columns<V> c(static_cast<int>(blockIdx.x * kThreads + threadIdx.x), A.dim);
+  if (c.dup == V) return;
+  float dw[V] = {}, db[V] = {};
+  for (int64_t row = blockIdx.y; row < n; row += gridDim.y) {
+    const Elems<T, V> ex = *reinterpret_cast<const Elems<T, V>*>(static_cast<const T*>(A.x) + row * A.x_stride + c.start);
+    const Elems<T, V> ey = *reinterpret_cast<const Elems<T, V>*>(static_cast<const T*>(A.dy) + row * A.dy_stride + c.start);
+    const float m = A.mean[row], r = A.rstd[row];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float d = as_float(ey.v[j]);
+      dw[j] += d * ((as_float(ex.v[j]) - m) * r);
+      db[j] += d;
+    }
+  }
+  float* out = A.part + static_cast<int64_t>(blockIdx.y) * 2 * A.dim;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    if (j >= c.dup) {
+      out[c.start + j] = dw[j];
+      out[static_cast<int64_t>(A.dim) + c.start + j] = db[j];
+    }
+}
+
+// dw and db (either may be null) from the slices' sums: 32 columns to a block, their slices dealt to its 8 rows of threads.
+constexpr int kJoinCols = 32;
+constexpr int kJoinRows = kThreads / kJoinCols;
+template <typename P>
+__global__ void __launch_bounds__(kThreads) k_norm_grad_join(const float* __restrict__ part, int32_t slices, int32_t dim, P* dw, P* db) {
+  __shared__ float lds[kThreads];
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kJoinCols + threadIdx.x % kJoinCols, width = 2 * static_cast<int64_t>(dim);
+  float s = 0.f;
+  if (i < width)
+    for (int q = threadIdx.x / kJoinCols; q < slices; q += kJoinRows) s += part[q * width + i];
+  lds[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x >= kJoinCols || i >= width) return;
+#pragma unroll
+  for (int q = 1; q < kJoinRows; ++q) s += lds[q * kJoinCols + threadIdx.x];
+  P* out = i < dim ? dw : db;
+  if (out) out[i < dim ? i : i - dim] = from_float<P>(s);
+}
+
+}  // namespace smfg_dev
+
+#endif  // SMFG_KERNELS_NORM_H_

@@ -46,6 +46,7 @@
 #include "smfg.h"
 
 #include "device_common.h"
+#include "host_common.h"
 #include "kernels_aggregate.h"
 #include "kernels_fast.h"
 #include "kernels_gather.h"
@@ -64,8 +65,6 @@ namespace {
 using namespace smfg_dev;
 
 // ---- host side --------------------------------------------------------------------------------
-
-inline int hip_err(hipError_t e) { return e == hipSuccess ? SMFG_OK : SMFG_ERR_HIP_BASE - static_cast<int>(e); }
 
 
 constexpr int kAnyRow = 7;  // between the vectors of 8 and of 4 bytes: see AnyRow
@@ -121,17 +120,6 @@ void profiler_free() {
   for (auto& n : g_prof.also) n.store(0);
   g_prof.ev = nullptr;
   g_prof.stage = nullptr;
-}
-
-// Typed device pointers must be multiples of their element size (atomics and vector accesses on a
-// misaligned address are undefined).
-inline bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
-
-inline unsigned blocks_for(int64_t work_items, int64_t per_block, unsigned cap) {
-  int64_t b = (work_items + per_block - 1) / per_block;
-  if (b < 1) b = 1;
-  if (b > cap) b = cap;
-  return static_cast<unsigned>(b);
 }
 
 }  // namespace

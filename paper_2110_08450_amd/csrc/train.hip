@@ -1,0 +1,396 @@
+// libsmfg: operators of a training step (include/smfg.h), host side.  Kernels: kernels_embed.h, kernels_norm.h,
+// kernels_clip.h.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "smfg.h"
+
+#include "elements.h"
+#include "host_common.h"
+#include "kernels_clip.h"
+#include "kernels_embed.h"
+#include "kernels_norm.h"
+
+namespace {
+
+using namespace smfg_dev;
+
+constexpr int64_t kMaxRows = int64_t(1) << 31;
+
+inline int64_t type_bytes(int32_t t) { return t == SMFG_DTYPE_F32 ? 4 : t == SMFG_DTYPE_F16 || t == SMFG_DTYPE_BF16 ? 2 : 0; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t up256(int64_t a) { return (a + 255) & ~int64_t(255); }
+
+// A matrix argument: type, stride, alignment.
+inline bool bad_matrix(const void* p, int32_t type, int64_t stride, int64_t dim) {
+  return type_bytes(type) == 0 || stride < dim || stride >= (int64_t(1) << 40) || misaligned(p, static_cast<uintptr_t>(type_bytes(type)));
+}
+inline bool bad_dim(int32_t dim) { return dim < 1 || dim > SMFG_MAX_DIM; }
+
+// Calls f(T{}) with the element type.
+template <typename F>
+void with_type(int32_t type, F f) {
+  if (type == SMFG_DTYPE_F32) f(float{});
+  else if (type == SMFG_DTYPE_F16) f(_Float16{});
+  else f(__bf16{});
+}
+template <typename T>
+constexpr int kVec = 16 / static_cast<int>(sizeof(T));  // columns of a 16-byte vector
+
+// ---- embedding ----------------------------------------------------------------------------------
+
+template <typename TI, typename TO>
+void launch_embedding(const EmbedArgs& A, unsigned blocks, bool vectors, hipStream_t st) {
+  if (vectors) k_embedding<TI, TO, kVec<TO>><<<blocks, kThreads, 0, st>>>(A);
+  else k_embedding<TI, TO, 1><<<blocks, kThreads, 0, st>>>(A);
+}
+
+// Sorted tokens of a chunk: as many as leave about 3000 waves of 64 lanes, but 16 to kMaxChunk.
+int chunk_of(int64_t max_ids, int32_t dim) {
+  const int64_t lanes = ceil_div(dim, 8);
+  int c = 16;
+  while (c < kMaxChunk && max_ids * lanes / (2 * c) >= 3000 * 64) c *= 2;
+  return c;
+}
+
+struct EmbedScratch {
+  int64_t rec[2], hist, total, part, tile_runs, chunk_runs, bytes;
+  int64_t tiles, chunks, run_tiles, part_width;
+  int chunk;
+};
+EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
+  EmbedScratch S;
+  S.chunk = chunk_of(max_ids, dim);
+  S.tiles = ceil_div(max_ids, kSortTile);
+  S.chunks = ceil_div(max_ids, S.chunk);
+  S.run_tiles = ceil_div(max_ids, kRunTile);
+  S.part_width = ceil_div(dim, 8) * 8;
+  int64_t at = 0;
+  const auto take = [&at](int64_t bytes) {
+    const int64_t here = at;
+    at += up256(bytes);
+    return here;
+  };
+  S.rec[0] = take(8 * max_ids);
+  S.rec[1] = take(8 * max_ids);
+  S.hist = take(4 * kSortBins * S.tiles);
+  S.total = take(4 * kSortBins);
+  S.part = take(4 * 2 * S.part_width * S.chunks);
+  S.tile_runs = take(4 * S.run_tiles);
+  S.chunk_runs = take(4 * S.chunks);
+  S.bytes = at;
+  return S;
+}
+
+// (row, token) of the call's ids, sorted by row.
+const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* ids, int32_t id_bytes, const int64_t* num, int64_t max_ids,
+                         int64_t num_rows, hipStream_t st) {
+  SortArgs A = {ids, id_bytes, 0, num_rows, num, max_ids, nullptr, nullptr, reinterpret_cast<uint32_t*>(scratch + S.hist),
+                reinterpret_cast<uint32_t*>(scratch + S.total), static_cast<int32_t>(S.tiles)};
+  int b = 0;
+  for (; A.shift == 0 || num_rows >> A.shift != 0; A.shift += kSortBits, b ^= 1) {
+    A.out = reinterpret_cast<uint2*>(scratch + S.rec[b]);
+    k_sort_count<<<static_cast<unsigned>(S.tiles), kThreads, 0, st>>>(A);
+    k_sort_scan<<<kSortBins, kThreads, 0, st>>>(A);
+    k_sort_scatter<<<static_cast<unsigned>(S.tiles), kThreads, 0, st>>>(A);
+    A.in = A.out;
+  }
+  return A.in;
+}
+
+template <typename TD, typename TG, int V>
+void launch_embed_sums(const EmbedGradArgs& A, int64_t chunks, hipStream_t st) {
+  const int64_t vectors = ceil_div(A.dim, V);
+  const auto blocks = [&](int lanes) {
+    return dim3(static_cast<unsigned>(ceil_div(chunks, kThreads / lanes)), static_cast<unsigned>(ceil_div(vectors, lanes)));
+  };
+  if (vectors <= 16) k_embed_grad<TD, TG, V, 16><<<blocks(16), kThreads, 0, st>>>(A);
+  else if (vectors <= 32) k_embed_grad<TD, TG, V, 32><<<blocks(32), kThreads, 0, st>>>(A);
+  else k_embed_grad<TD, TG, V, 64><<<blocks(64), kThreads, 0, st>>>(A);
+  if (chunks > 1) k_embed_join<TG, V><<<static_cast<unsigned>(chunks), kThreads, 0, st>>>(A);
+}
+
+template <typename TD, typename TG>
+void launch_embed_grad(const EmbedGradArgs& A, int64_t chunks, bool clear, hipStream_t st) {
+  constexpr int kG = kVec<TG>;
+  if (clear) {
+    const int64_t rows = A.num_rows;
+    if (A.dim >= kG) k_embed_clear<TG, kG><<<blocks_for(rows * ceil_div(A.dim, kG), 4 * kThreads, 65536), kThreads, 0, st>>>(A.grad, A.grad_stride, rows, A.dim);
+    else k_embed_clear<TG, 1><<<blocks_for(rows * A.dim, 4 * kThreads, 65536), kThreads, 0, st>>>(A.grad, A.grad_stride, rows, A.dim);
+  }
+  if (chunks == 0) return;
+  if (A.dim >= kVec<TD>) launch_embed_sums<TD, TG, kVec<TD>>(A, chunks, st);
+  else launch_embed_sums<TD, TG, 1>(A, chunks, st);
+}
+
+int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids, int64_t max_ids, const void* d_dy, int64_t dy_stride,
+                   int32_t dy_dtype, int32_t dim, float scale, void* d_grad, int64_t num_rows, int64_t grad_stride, int32_t grad_dtype,
+                   int32_t accumulate, bool rows_only, int32_t* d_row_ids, int64_t* d_num_unique, void* d_scratch, int64_t scratch_bytes,
+                   hipStream_t st) {
+  if (!d_num_ids || !d_grad || (max_ids > 0 && (!d_ids || !d_dy || !d_scratch))) return SMFG_ERR_NULL_PTR;
+  if (rows_only && (!d_num_unique || (max_ids > 0 && !d_row_ids))) return SMFG_ERR_NULL_PTR;
+  if (bad_dim(dim) || (id_bytes != 4 && id_bytes != 8) || max_ids < 0 || max_ids >= kMaxRows || num_rows < 1 || num_rows >= kMaxRows ||
+      bad_matrix(d_dy, dy_dtype, dy_stride, dim) || bad_matrix(d_grad, grad_dtype, grad_stride, dim) ||
+      (grad_dtype != SMFG_DTYPE_F32 && grad_dtype != dy_dtype) || misaligned(d_ids, static_cast<uintptr_t>(id_bytes)) ||
+      misaligned(d_num_ids, 8) || misaligned(d_row_ids, 4) || misaligned(d_num_unique, 8) || misaligned(d_scratch, 256))
+    return SMFG_ERR_INVALID_ARG;
+  if (max_ids == 0 && !rows_only && accumulate) return SMFG_OK;
+  const EmbedScratch S = embed_scratch(max_ids, dim);
+  if (max_ids > 0 && scratch_bytes < S.bytes) return SMFG_ERR_CAPACITY;
+  uint8_t* scratch = static_cast<uint8_t*>(d_scratch);
+  EmbedGradArgs A = {nullptr, d_num_ids, max_ids, num_rows, S.chunk, dim, d_dy, dy_stride, scale, accumulate, d_grad, grad_stride,
+                     reinterpret_cast<float*>(scratch + S.part), S.part_width, d_row_ids, d_num_unique,
+                     reinterpret_cast<uint32_t*>(scratch + S.tile_runs), reinterpret_cast<uint32_t*>(scratch + S.chunk_runs)};
+  if (max_ids > 0) A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, st);
+  if (rows_only) {
+    if (max_ids > 0) k_embed_runs<<<static_cast<unsigned>(S.run_tiles), kThreads, 0, st>>>(A);
+    k_embed_scan<<<1, kThreads, 0, st>>>(A, S.run_tiles);
+  }
+  with_type(dy_dtype, [&](auto t) {
+    using T = decltype(t);
+    if (grad_dtype == SMFG_DTYPE_F32) launch_embed_grad<T, float>(A, S.chunks, !rows_only && !accumulate, st);
+    else launch_embed_grad<T, T>(A, S.chunks, !rows_only && !accumulate, st);
+  });
+  return hip_err(hipGetLastError());
+}
+
+// ---- layer norm ---------------------------------------------------------------------------------
+
+// How rows of `vectors` vectors are dealt: LANES lanes and NV vectors a lane; f.template operator()<V, NV, LANES>.
+template <typename T, typename F>
+bool with_row_shape(int32_t dim, F f) {
+  constexpr int V = kVec<T>;
+  if (dim < V) return f.template operator()<1, 1, 16>(), true;
+  const int64_t vectors = ceil_div(dim, V);
+  if (vectors <= 16) f.template operator()<V, 1, 16>();
+  else if (vectors <= 32) f.template operator()<V, 1, 32>();
+  else if (vectors <= 64) f.template operator()<V, 1, 64>();
+  else if (vectors <= 128) f.template operator()<V, 2, 64>();
+  else if (vectors <= 256) f.template operator()<V, 1, 256>();
+  else if (vectors <= 512) f.template operator()<V, 2, 256>();
+  else if (vectors <= 1024) f.template operator()<V, 4, 256>();
+  else if (V == 4 && vectors <= 2048) f.template operator()<V, V == 4 ? 8 : 4, 256>();
+  else return false;
+  return true;
+}
+
+template <typename T>
+struct LaunchNorm {
+  const NormArgs& A;
+  hipStream_t st;
+  template <int V, int NV, int LANES>
+  void operator()() const {
+    k_layer_norm<T, V, NV, LANES><<<static_cast<unsigned>(ceil_div(A.max_rows, kThreads / LANES)), kThreads, 0, st>>>(A);
+  }
+};
+
+// Blocks, and slices of the weight's gradient, of the launch over max_rows rows of dim columns: the most that 4 MiB of sums hold.
+constexpr int kNormSlices = 1024;
+int64_t norm_slices(int64_t max_rows, int32_t dim) {
+  int64_t s = (int64_t(4) << 20) / (8 * static_cast<int64_t>(dim));
+  if (s < 256) s = 256;
+  if (s > kNormSlices) s = kNormSlices;
+  return s < max_rows ? s : max_rows;
+}
+
+template <typename T>
+struct LaunchNormGrad {
+  const NormGradArgs& A;
+  int64_t& slices;
+  hipStream_t st;
+  template <int V, int NV, int LANES>
+  void operator()() const {
+    const int64_t blocks = ceil_div(A.max_rows, kThreads / LANES);
+    if (blocks < slices) slices = blocks;
+    k_layer_norm_grad<T, V, NV, LANES><<<static_cast<unsigned>(slices), kThreads, 0, st>>>(A);
+  }
+};
+
+// ---- clipping -----------------------------------------------------------------------------------
+
+bool bad_grads(const smfg_grad_t* g, int32_t n) {
+  for (int i = 0; i < n; ++i) {
+    if (g[i].numel < 0 || g[i].numel >= (int64_t(1) << 48) || type_bytes(g[i].dtype) == 0) return true;
+    if (g[i].d_rows && (g[i].row_elems < 1 || misaligned(g[i].d_rows, 8))) return true;
+    if (misaligned(g[i].grad, static_cast<uintptr_t>(type_bytes(g[i].dtype)))) return true;
+    if (!g[i].out) continue;
+    if ((g[i].out_dtype != g[i].dtype && g[i].out_dtype != SMFG_DTYPE_F32) || misaligned(g[i].out, static_cast<uintptr_t>(type_bytes(g[i].out_dtype)))) return true;
+    if (g[i].out == g[i].grad && g[i].out_dtype != g[i].dtype) return true;
+  }
+  return false;
+}
+
+// Elements of a block: about 4096 blocks, of 1 to 16 turns.
+int64_t clip_chunk(const smfg_grad_t* g, int32_t n) {
+  double all = 0;
+  for (int i = 0; i < n; ++i) all += static_cast<double>(g[i].numel);
+  const int64_t turns = static_cast<int64_t>(all / 4096 / kClipStep);
+  return (turns < 1 ? 1 : turns > 16 ? 16 : turns) * kClipStep;
+}
+int64_t clip_blocks(const smfg_grad_t* g, int32_t n, int64_t chunk) {
+  int64_t b = 0;
+  for (int i = 0; i < n; ++i) b += ceil_div(g[i].numel, chunk);
+  return b;
+}
+
+// Calls f with the tensors that fit a launch, until there are no more.
+template <typename F>
+void for_clip_launches(const smfg_grad_t* g, int32_t n, int64_t chunk, double* part, const float* factor, F f) {
+  ClipArgs A;
+  A.chunk = chunk;
+  A.factor = factor;
+  for (int i = 0; i < n;) {
+    A.tensors = 0;
+    A.blocks = 0;
+    A.part = part;
+    for (; i < n && A.tensors < kClipTensors; ++i) {
+      if (g[i].numel == 0) continue;
+      const int64_t blocks = ceil_div(g[i].numel, chunk);
+      if (A.blocks + blocks > 0x7FFFFFFF) break;
+      void* const out = g[i].out ? g[i].out : const_cast<void*>(g[i].grad);
+      A.t[A.tensors++] = {g[i].grad, out, g[i].numel, g[i].d_rows, g[i].d_rows ? g[i].row_elems : 1, A.blocks,
+                          g[i].dtype | (g[i].out ? g[i].out_dtype : g[i].dtype) << 4};
+      A.blocks += static_cast<uint32_t>(blocks);
+    }
+    if (A.tensors == 0) break;
+    f(A);
+    part += A.blocks;
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int smfg_embedding(const void* d_table, int64_t num_rows, int64_t table_stride, int32_t table_dtype, const void* d_ids, int32_t id_bytes,
+                   const int64_t* d_num_ids, int64_t max_ids, int32_t dim, float scale, void* d_out, int64_t out_stride, int32_t out_dtype,
+                   void* hip_stream) {
+  if (!d_table || !d_num_ids || (max_ids > 0 && (!d_ids || !d_out))) return SMFG_ERR_NULL_PTR;
+  if (bad_dim(dim) || (id_bytes != 4 && id_bytes != 8) || max_ids < 0 || max_ids >= kMaxRows || num_rows < 1 || num_rows >= kMaxRows ||
+      bad_matrix(d_table, table_dtype, table_stride, dim) || bad_matrix(d_out, out_dtype, out_stride, dim) ||
+      (table_dtype != SMFG_DTYPE_F32 && table_dtype != out_dtype) || misaligned(d_ids, static_cast<uintptr_t>(id_bytes)) || misaligned(d_num_ids, 8))
+    return SMFG_ERR_INVALID_ARG;
+  if (max_ids == 0) return SMFG_OK;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const EmbedArgs A = {d_table, num_rows, table_stride, dim, id_bytes, d_ids, d_num_ids, max_ids, scale, d_out, out_stride};
+  const int vector = static_cast<int>(16 / type_bytes(out_dtype));
+  const bool vectors = dim >= vector;
+  const int64_t blocks = ceil_div(max_ids * ceil_div(dim, vectors ? vector : 1), kEmbedTurns * kThreads);
+  if (blocks > 0x7FFFFFFF) return SMFG_ERR_INVALID_ARG;
+  const unsigned b = static_cast<unsigned>(blocks);
+  with_type(out_dtype, [&](auto o) {
+    using O = decltype(o);
+    if (table_dtype == SMFG_DTYPE_F32) launch_embedding<float, O>(A, b, vectors, st);
+    else launch_embedding<O, O>(A, b, vectors, st);
+  });
+  return hip_err(hipGetLastError());
+}
+
+int64_t smfg_embedding_grad_scratch_bytes(int64_t max_ids, int64_t num_rows, int32_t dim) {
+  if (bad_dim(dim) || max_ids < 0 || max_ids >= kMaxRows || num_rows < 1 || num_rows >= kMaxRows) return -1;
+  return embed_scratch(max_ids, dim).bytes;
+}
+
+int smfg_embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids, int64_t max_ids, const void* d_dy, int64_t dy_stride,
+                        int32_t dy_dtype, int32_t dim, float scale, void* d_grad, int64_t num_rows, int64_t grad_stride, int32_t grad_dtype,
+                        int32_t accumulate, void* d_scratch, int64_t scratch_bytes, void* hip_stream) {
+  return embedding_grad(d_ids, id_bytes, d_num_ids, max_ids, d_dy, dy_stride, dy_dtype, dim, scale, d_grad, num_rows, grad_stride, grad_dtype,
+                        accumulate, false, nullptr, nullptr, d_scratch, scratch_bytes, static_cast<hipStream_t>(hip_stream));
+}
+
+int smfg_embedding_grad_rows(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids, int64_t max_ids, const void* d_dy, int64_t dy_stride,
+                             int32_t dy_dtype, int32_t dim, float scale, int64_t num_rows, int32_t* d_row_ids, int64_t* d_num_unique, void* d_grad,
+                             int64_t grad_stride, int32_t grad_dtype, void* d_scratch, int64_t scratch_bytes, void* hip_stream) {
+  return embedding_grad(d_ids, id_bytes, d_num_ids, max_ids, d_dy, dy_stride, dy_dtype, dim, scale, d_grad, num_rows, grad_stride, grad_dtype, 0,
+                        true, d_row_ids, d_num_unique, d_scratch, scratch_bytes, static_cast<hipStream_t>(hip_stream));
+}
+
+int smfg_layer_norm(const void* d_x, int64_t x_stride, int32_t dtype, const int64_t* d_num_rows, int64_t max_rows, int32_t dim, const void* d_w,
+                    const void* d_b, int32_t param_dtype, float eps, void* d_y, int64_t y_stride, float* d_mean, float* d_rstd, void* hip_stream) {
+  if (!d_num_rows || (max_rows > 0 && (!d_x || !d_y))) return SMFG_ERR_NULL_PTR;
+  if (bad_dim(dim) || max_rows < 0 || max_rows >= kMaxRows || bad_matrix(d_x, dtype, x_stride, dim) || bad_matrix(d_y, dtype, y_stride, dim) ||
+      (param_dtype != SMFG_DTYPE_F32 && param_dtype != dtype) || misaligned(d_w, static_cast<uintptr_t>(type_bytes(param_dtype))) ||
+      misaligned(d_b, static_cast<uintptr_t>(type_bytes(param_dtype))) || !(eps >= 0.f) || misaligned(d_num_rows, 8) || misaligned(d_mean, 4) ||
+      misaligned(d_rstd, 4) || (d_x == d_y && x_stride != y_stride))
+    return SMFG_ERR_INVALID_ARG;
+  if (max_rows == 0) return SMFG_OK;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const NormArgs A = {d_x, x_stride, d_num_rows, max_rows, dim, param_dtype == SMFG_DTYPE_F32, d_w, d_b, eps, d_y, y_stride, d_mean, d_rstd};
+  with_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    if (!with_row_shape<T>(dim, LaunchNorm<T>{A, st})) k_layer_norm_long<T, kVec<T>><<<static_cast<unsigned>(max_rows), kThreads, 0, st>>>(A);
+  });
+  return hip_err(hipGetLastError());
+}
+
+int64_t smfg_layer_norm_grad_scratch_bytes(int64_t max_rows, int32_t dim) {
+  if (bad_dim(dim) || max_rows < 0 || max_rows >= kMaxRows) return -1;
+  return up256(norm_slices(max_rows, dim) * 8 * dim);
+}
+
+int smfg_layer_norm_grad(const void* d_dy, int64_t dy_stride, const void* d_x, int64_t x_stride, int32_t dtype, const int64_t* d_num_rows,
+                         int64_t max_rows, int32_t dim, const void* d_w, int32_t param_dtype, const float* d_mean, const float* d_rstd, void* d_dx,
+                         int64_t dx_stride, void* d_dw, void* d_db, void* d_scratch, int64_t scratch_bytes, void* hip_stream) {
+  const bool sums = d_dw || d_db;
+  if (!d_num_rows || (max_rows > 0 && (!d_x || !d_dy || !d_mean || !d_rstd || (sums && !d_scratch)))) return SMFG_ERR_NULL_PTR;
+  if (bad_dim(dim) || max_rows < 0 || max_rows >= kMaxRows || bad_matrix(d_x, dtype, x_stride, dim) || bad_matrix(d_dy, dtype, dy_stride, dim) ||
+      (d_dx && bad_matrix(d_dx, dtype, dx_stride, dim)) || (param_dtype != SMFG_DTYPE_F32 && param_dtype != dtype))
+    return SMFG_ERR_INVALID_ARG;
+  const uintptr_t pa = static_cast<uintptr_t>(type_bytes(param_dtype));
+  if (misaligned(d_w, pa) || misaligned(d_dw, pa) || misaligned(d_db, pa) || misaligned(d_num_rows, 8) || misaligned(d_mean, 4) ||
+      misaligned(d_rstd, 4) || misaligned(d_scratch, 256) || (d_dx && ((d_dx == d_dy && dx_stride != dy_stride) || (d_dx == d_x && dx_stride != x_stride))))
+    return SMFG_ERR_INVALID_ARG;
+  int64_t slices = norm_slices(max_rows, dim);
+  if (sums && scratch_bytes < up256(slices * 8 * dim)) return SMFG_ERR_CAPACITY;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  float* part = sums ? static_cast<float*>(d_scratch) : nullptr;
+  const NormGradArgs A = {d_dy, dy_stride, d_x, x_stride, d_num_rows, max_rows, dim, param_dtype == SMFG_DTYPE_F32, d_w, d_mean, d_rstd, d_dx, dx_stride, part};
+  if (!sums && (max_rows == 0 || !d_dx)) return SMFG_OK;
+  if (max_rows > 0) {
+    with_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      constexpr int V = kVec<T>;
+      if (with_row_shape<T>(dim, LaunchNormGrad<T>{A, slices, st})) return;
+      if (sums) {
+        if (slices > 64) slices = 64;
+        k_norm_grad_columns<T, V><<<dim3(static_cast<unsigned>(ceil_div(ceil_div(dim, V), kThreads)), static_cast<unsigned>(slices)), kThreads, 0, st>>>(A);
+      }
+      if (d_dx) k_layer_norm_grad_long<T, V><<<static_cast<unsigned>(max_rows), kThreads, 0, st>>>(A);
+    });
+  }
+  if (sums) {
+    const unsigned blocks = static_cast<unsigned>(ceil_div(2 * static_cast<int64_t>(dim), kJoinCols));
+    with_type(param_dtype, [&](auto p) {
+      using P = decltype(p);
+      k_norm_grad_join<P><<<blocks, kThreads, 0, st>>>(part, static_cast<int32_t>(slices), dim, static_cast<P*>(d_dw), static_cast<P*>(d_db));
+    });
+  }
+  return hip_err(hipGetLastError());
+}
+
+int64_t smfg_clip_grad_norm_scratch_bytes(const smfg_grad_t* grads, int32_t num_grads) {
+  if (num_grads < 0 || (num_grads > 0 && !grads) || bad_grads(grads, num_grads)) return -1;
+  return 256 + up256(8 * clip_blocks(grads, num_grads, clip_chunk(grads, num_grads)));
+}
+
+int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale, float max_norm, float* d_norm, void* d_scratch,
+                        int64_t scratch_bytes, void* hip_stream) {
+  if ((num_grads > 0 && !grads) || !d_norm || !d_scratch) return SMFG_ERR_NULL_PTR;
+  if (num_grads < 0 || bad_grads(grads, num_grads) || !std::isfinite(scale) || !(max_norm > 0.f) || misaligned(d_norm, 4) || misaligned(d_scratch, 256))
+    return SMFG_ERR_INVALID_ARG;
+  for (int i = 0; i < num_grads; ++i)
+    if (grads[i].numel > 0 && !grads[i].grad) return SMFG_ERR_NULL_PTR;
+  const int64_t chunk = clip_chunk(grads, num_grads), parts = clip_blocks(grads, num_grads, chunk);
+  if (scratch_bytes < 256 + up256(8 * parts)) return SMFG_ERR_CAPACITY;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  float* factor = static_cast<float*>(d_scratch);
+  double* part = reinterpret_cast<double*>(static_cast<uint8_t*>(d_scratch) + 256);
+  for_clip_launches(grads, num_grads, chunk, part, factor, [&](const ClipArgs& A) { k_clip_squares<<<A.blocks, kThreads, 0, st>>>(A); });
+  k_clip_norm<<<1, kClipNormThreads, 0, st>>>(part, parts, scale, max_norm, d_norm, factor);
+  for_clip_launches(grads, num_grads, chunk, part, factor, [&](const ClipArgs& A) { k_clip_scale<<<A.blocks, kThreads, 0, st>>>(A); });
+  return hip_err(hipGetLastError());
+}
+
+}  // extern "C"

@@ -1,0 +1,500 @@
+"""Embedding, layer norm, their gradients and gradient clipping against their definitions in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2110_08450_amd import binding as smfg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+UNIT = {torch.float32: U, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+LEAST = {torch.float32: 2.0 ** -149, torch.float16: 2.0 ** -24, torch.bfloat16: 2.0 ** -133}
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+def count(n):
+    return torch.tensor([n], dtype=torch.int64, device=DEV)
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def rounded(tol, want, dtype):
+    """Room for the one rounding to dtype, of a value that is itself off by tol."""
+    return tol + UNIT[dtype] * (want.abs() + tol) + LEAST[dtype]
+
+
+def check(got, want, tol):
+    bad = ~((got.double() - want).abs() <= tol)
+    assert not bad.any(), (int(bad.sum()), got.double()[bad][:4], want[bad][:4])
+
+
+def strided(shape, dtype, pad, seed, spread=1.0):
+    """Rows in a wider buffer, the rest of which is NaN."""
+    wide = torch.full((max(1, shape[0]), shape[1] + pad), float("nan"), dtype=dtype, device=DEV)
+    wide[:, :shape[1]] = (torch.randn((max(1, shape[0]), shape[1]), device=DEV, generator=gen(seed)) * spread).to(dtype)
+    return wide[:shape[0], :shape[1]], wide
+
+
+# ---- embedding ----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n,spare,rows,dim,table,out,ids,pad", [
+    (1, 0, 1, 1, F32, F32, torch.int32, 0), (3, 2, 5, 3, F16, F16, torch.int64, 1), (16, 0, 1000, 100, F16, F16, torch.int32, 0),
+    (257, 40, 77, 7, BF16, BF16, torch.int32, 5), (1000, 24, 300, 128, F32, F16, torch.int64, 0), (513, 0, 40, 301, F32, BF16, torch.int32, 3),
+    (700, 1, 9, 9, BF16, BF16, torch.int64, 0), (60, 4, 31, 4096, BF16, BF16, torch.int32, 8), (33, 0, 50, 8195, F32, F32, torch.int32, 1),
+    (5, 5, 7, 70_001, F16, F16, torch.int64, 0), (0, 9, 4, 16, F16, F16, torch.int32, 0), (3001, 0, 2, 4, F32, F32, torch.int32, 0)])
+def test_embedding(n, spare, rows, dim, table, out, ids, pad):
+    """One product and its rounding: exact where nothing is scaled; an id outside the table gives zeros, whatever the table holds."""
+    w, _ = strided((rows, dim), table, pad, 1)
+    w[rows - 1, 0] = float("inf")
+    i = torch.randint(-2, rows + 2, (n + spare,), device=DEV, generator=gen(2)).to(ids)
+    for scale in (1.0, math.sqrt(dim)):
+        y, wide = strided((n + spare, dim), out, pad, 3)
+        before = wide.clone()
+        smfg.embedding(w, i, count(n), n + spare, y, scale=scale)
+        ok = (i[:n] >= 0) & (i[:n] < rows)
+        want = torch.where(ok[:, None], (w.float() * scale)[i[:n].long().clamp(0, rows - 1)], 0.0).to(out)
+        assert torch.equal(y[:n], want)
+        before[:n, :dim] = want
+        assert torch.equal(wide.view(torch.int16), before.view(torch.int16))  # nothing else is written
+
+
+def test_embedding_of_a_table_beyond_32_bits():
+    """Row offsets pass 2^32 elements, and 2^31 rows less one are the most."""
+    rows, dim = 2 ** 31 - 1, 3
+    w = torch.empty((rows, dim), dtype=F16, device=DEV)
+    at = torch.tensor([0, 2 ** 30, 1_431_655_766, rows - 1], device=DEV)
+    w[at] = torch.arange(12, device=DEV).reshape(4, 3).to(F16)
+    ids = torch.cat([at, torch.tensor([rows, 2 ** 33, -1, 2 ** 32 + 5], device=DEV), at])
+    out = torch.empty((12, dim), dtype=F16, device=DEV)
+    smfg.embedding(w, ids, count(12), 12, out)
+    assert torch.equal(out[:4], w[at]) and not out[4:8].any() and torch.equal(out[8:], w[at])
+    # its gradient, added in place: the sums of two tokens each
+    ws = smfg.embedding_grad_workspace(12, rows, dim)
+    smfg.embedding_grad(ids, count(12), 12, out, w, ws, accumulate=True)
+    assert torch.equal(w[at], 3 * out[:4])
+
+
+# ---- its gradient -------------------------------------------------------------------------------
+
+def ids_of(kind, n, rows, seed):
+    g = gen(seed)
+    if kind == "uniform":
+        return torch.randint(0, rows, (n,), device=DEV, generator=g)
+    if kind == "outside":
+        return torch.where(torch.rand(n, device=DEV, generator=g) < 0.5, -1, rows + 3)
+    if kind == "same":
+        return torch.full((n,), rows - 1, device=DEV)
+    if kind == "mixed":  # long runs, single ones, padded places
+        u = torch.rand(n, device=DEV, generator=g)
+        r = torch.randint(-1, rows + 1, (n,), device=DEV, generator=g)
+        r[u < 0.6] = rows // 2
+        r[u < 0.3] = 0
+        r[u < 0.1] = rows - 1
+        return r
+    return torch.arange(n, device=DEV).flip(0) % rows
+
+
+def sums_of(ids, dy, rows, scale):
+    """Per row of the table: sums, sums of magnitudes and numbers of its tokens, in 64 bits."""
+    ok = (ids >= 0) & (ids < rows)
+    i, d = ids[ok].long(), dy[ok].double()
+    out = torch.zeros((rows, dy.shape[1]), dtype=torch.float64, device=DEV)
+    mag = torch.zeros_like(out)
+    return (out.index_add_(0, i, d) * scale, mag.index_add_(0, i, d.abs()) * abs(scale), torch.bincount(i, minlength=rows))
+
+
+GRADS = [(1, 0, 1, 1, F32, F32, "uniform", 0), (5, 3, 9, 3, F16, F32, "uniform", 1), (64, 0, 300, 7, BF16, BF16, "mixed", 0),
+         (1000, 10, 10_000, 32, F32, F32, "uniform", 0), (4097, 0, 256, 100, F16, F16, "mixed", 3), (4096, 5, 255, 9, BF16, F32, "same", 0),
+         (30_000, 2000, 65_536, 128, F16, F32, "mixed", 0), (9000, 0, 70_000, 301, F32, F32, "backwards", 2),
+         (20_000, 1, 3, 256, F16, F32, "uniform", 0), (3000, 0, 50, 1025, BF16, F32, "mixed", 1), (2500, 100, 2_000_000, 64, F16, F16, "uniform", 0),
+         (700, 4, 17, 4096, F32, F32, "mixed", 0), (300, 0, 5, 8199, F16, F32, "same", 0), (5000, 0, 999, 128, BF16, BF16, "outside", 0),
+         (0, 700, 40, 16, F32, F32, "uniform", 0), (150_000, 0, 4096, 16, F32, F32, "mixed", 0), (260_000, 1, 100, 33, F16, F32, "same", 0),
+         (8192, 0, 16_777_217, 8, F32, F32, "uniform", 0)]
+
+
+@pytest.mark.parametrize("n,spare,rows,dim,dtype,gtype,kind,pad", GRADS)
+@pytest.mark.parametrize("idtype", [torch.int32, torch.int64])
+def test_embedding_grad(n, spare, rows, dim, dtype, gtype, kind, pad, idtype):
+    """(k + 2) 2^-24 of the sum of magnitudes, k summed values; then the gradient's rounding.  Whole, added, and touched rows."""
+    cap = n + spare
+    ids = ids_of(kind, cap, rows, 5).to(idtype)
+    dy, _ = strided((cap, dim), dtype, pad, 6)
+    scale = 1.0 if n % 2 else 0.75 * math.sqrt(dim)
+    want, mag, k = sums_of(ids[:n], dy[:n], rows, scale)
+    ws = smfg.embedding_grad_workspace(cap, rows, dim)
+    ws.data.fill_(0xA5)
+    g, wide = strided((rows, dim), gtype, pad, 7)
+    before = wide.clone()
+    smfg.embedding_grad(ids, count(n), cap, dy, g, ws, scale=scale)
+    check(g, want, rounded((k[:, None] + 2) * U * mag, want, gtype))
+    assert not g[k == 0].any() and torch.equal(wide[:, dim:].isnan(), before[:, dim:].isnan())
+    # added to what is there: rows without a token keep their bits
+    h = before.clone()[:, :dim]
+    base = h.clone()
+    smfg.embedding_grad(ids, count(n), cap, dy, h, ws, scale=scale, accumulate=True)
+    both = want + base.double()
+    check(h, both, rounded((k[:, None] + 2) * U * (mag + base.double().abs()), both, gtype))
+    assert torch.equal(h[k == 0], base[k == 0])
+    # the touched rows alone: the same bits, ids ascending, nothing behind them
+    rid = torch.full((cap,), -7, dtype=torch.int32, device=DEV)
+    num = count(-1)
+    c, cwide = strided((cap, dim), gtype, pad, 8)
+    cbefore = cwide.clone()
+    smfg.embedding_grad_rows(ids, count(n), cap, dy, rows, rid, num, c, ws, scale=scale)
+    u = int(num)
+    touched = torch.nonzero(k)[:, 0]
+    assert u == touched.numel() and torch.equal(rid[:u].long(), touched) and bool((rid[u:] == -7).all())
+    assert torch.equal(c[:u], g[touched])
+    cbefore[:u, :dim] = c[:u]
+    assert torch.equal(cwide.view(torch.int16), cbefore.view(torch.int16))
+
+
+@pytest.mark.parametrize("n,max_ids", [(-5, 100), (100, 50), (2 ** 40, 3000)])
+def test_counts_are_held_to_the_launch(n, max_ids):
+    """A count on the device that is negative or too large is read as 0 or as max_ids."""
+    m = min(max(n, 0), max_ids)
+    ids = torch.randint(0, 20, (max_ids,), device=DEV, generator=gen(1))
+    dy = torch.randn((max_ids, 24), device=DEV, generator=gen(2))
+    out = torch.full((max_ids, 24), 9.0, device=DEV)
+    smfg.embedding(dy, ids, count(n), max_ids, out)
+    assert torch.equal(out[:m], dy[ids[:m]]) and bool((out[m:] == 9).all())
+    ws = smfg.embedding_grad_workspace(max_ids, 20, 24)
+    g = torch.empty((20, 24), device=DEV)
+    smfg.embedding_grad(ids, count(n), max_ids, dy, g, ws)
+    want, mag, k = sums_of(ids[:m], dy[:m], 20, 1.0)
+    check(g, want, (k[:, None] + 2) * U * mag)
+    y = torch.full((max_ids, 24), 9.0, device=DEV)
+    smfg.layer_norm(dy, count(n), max_ids, None, None, 1e-5, y)
+    assert bool((y[m:] == 9).all()) and not (y[:m] == 9).any()
+
+
+def test_embedding_grad_of_infinities():
+    """An infinite or NaN gradient reaches its own row alone; a padded place's reaches none."""
+    ids = torch.tensor([0, 1, 2, -1, 1, 3, 99], device=DEV)
+    dy = torch.ones((7, 40), device=DEV)
+    dy[1, 3], dy[3], dy[6], dy[5, 0] = float("inf"), float("nan"), float("nan"), float("nan")
+    g = torch.empty((4, 40), device=DEV)
+    smfg.embedding_grad(ids, count(7), 7, dy, g, smfg.embedding_grad_workspace(7, 4, 40))
+    assert torch.equal(g[0], torch.ones(40, device=DEV)) and torch.equal(g[2], torch.ones(40, device=DEV))
+    assert g[1, 3].item() == float("inf") and torch.isfinite(g[1, 4:]).all() and g[3, 0].isnan() and torch.isfinite(g[3, 1:]).all()
+
+
+def test_embedding_grad_against_differences():
+    """The lookup is linear: its difference along any direction is the gradient's product with it, but for roundings."""
+    n, rows, dim, scale = 3000, 200, 48, 1.7
+    ids = ids_of("mixed", n, rows, 3)
+    dy = torch.randn((n, dim), device=DEV, generator=gen(4))
+    v = torch.randn((rows, dim), device=DEV, generator=gen(5))
+    g = torch.empty((rows, dim), device=DEV)
+    smfg.embedding_grad(ids, count(n), n, dy, g, smfg.embedding_grad_workspace(n, rows, dim), scale=scale)
+    outs = []
+    for s in (1, -1):
+        o = torch.empty((n, dim), device=DEV)
+        smfg.embedding(s * v, ids, count(n), n, o, scale=scale)
+        outs.append((o.double() * dy.double()).sum())
+    slope = (outs[0] - outs[1]) / 2
+    tol = (n + 4) * U * (sums_of(ids, dy, rows, scale)[1] * v.double().abs()).sum()
+    assert abs(slope - (g.double() * v.double()).sum()) <= tol
+
+
+# ---- layer norm ---------------------------------------------------------------------------------
+
+def depth(dim):
+    """Additions that a value goes through in a sum over a row: at most a lane's columns, then the lanes."""
+    return 64 + dim // 256
+
+
+def norm_of(x, w, b, eps):
+    """(y, mean, rstd, tolerances of them before a rounding) in 64 bits.  The mean is off by dm; the variance by a share: its sum's
+    roundings and dm^2 / variance; a centred value by dm and its rounding."""
+    dim = x.shape[1]
+    x, w, b = x.double(), w.double(), b.double()
+    m = x.mean(1, keepdim=True)
+    d = x - m
+    var = (d * d).mean(1, keepdim=True)
+    r = 1 / torch.sqrt(var + eps)
+    dm = (depth(dim) + 2) * U * x.abs().mean(1, keepdim=True)
+    share = (depth(dim) + 8) * U / 2 + dm * dm / (2 * (var + eps)) + 4 * U
+    y = d * r * w + b
+    tol = w.abs() * r * (dm + d.abs() * U) * (1 + share) + (d * r * w).abs() * (share + 4 * U) + U * (y.abs() + b.abs())
+    return y, m[:, 0], r[:, 0], tol, dm[:, 0], (r * share)[:, 0]
+
+
+NORMS = [(1, 0, 1, F32, F32, 0), (3, 1, 3, F16, F16, 2), (17, 0, 7, BF16, F32, 0), (100, 20, 8, F16, F32, 0), (33, 0, 31, F32, F32, 1),
+         (65, 3, 64, F32, F32, 0), (1000, 24, 100, F16, F16, 0), (257, 0, 128, F32, F32, 4), (130, 0, 129, BF16, BF16, 0), (700, 9, 256, F16, F32, 0),
+         (90, 0, 257, F32, F32, 3), (64, 1, 301, F16, F16, 19), (50, 0, 512, BF16, F32, 0), (41, 0, 513, F32, F32, 0), (30, 2, 1000, F16, F16, 0),
+         (29, 0, 1025, F32, F32, 0), (28, 0, 2048, BF16, BF16, 0), (27, 1, 2049, F16, F32, 5), (26, 0, 4096, BF16, BF16, 0), (25, 0, 4099, F32, F32, 0),
+         (12, 0, 8192, F16, F32, 0), (11, 1, 8192, F32, F32, 0), (9, 0, 8193, BF16, BF16, 1), (5, 0, 20_001, F32, F32, 0), (1, 4, 5120, BF16, F32, 0),
+         (20_000, 0, 100, F32, F32, 0), (0, 5, 64, F32, F32, 0)]
+
+
+def norm_inputs(n, cap, dim, dtype, ptype, pad, offset=1.0):
+    x, _ = strided((cap, dim), dtype, pad, 1, 2.0)
+    x += torch.randn((cap, 1), device=DEV, generator=gen(2)).to(dtype) * offset
+    w = (1 + 0.2 * torch.randn(dim, device=DEV, generator=gen(3))).to(ptype)
+    b = (0.3 * torch.randn(dim, device=DEV, generator=gen(4))).to(ptype)
+    return x, w, b
+
+
+@pytest.mark.parametrize("n,spare,dim,dtype,ptype,pad", NORMS)
+def test_layer_norm(n, spare, dim, dtype, ptype, pad):
+    cap, eps = n + spare, 1e-5
+    x, w, b = norm_inputs(n, cap, dim, dtype, ptype, pad)
+    y, wide = strided((cap, dim), dtype, pad + 1, 5)
+    before = wide.clone()
+    mean, rstd = torch.full((cap,), 7.0, device=DEV), torch.full((cap,), 7.0, device=DEV)
+    smfg.layer_norm(x, count(n), cap, w, b, eps, y, mean, rstd)
+    want, m, r, tol, tm, tr = norm_of(x[:n], w, b, eps)
+    check(y[:n], want, rounded(tol, want, dtype))
+    check(mean[:n], m, rounded(tm, m, F32))
+    check(rstd[:n], r, rounded(tr, r, F32))
+    assert bool((mean[n:] == 7).all()) and bool((rstd[n:] == 7).all())
+    before[:n, :dim] = y[:n]
+    assert torch.equal(wide.view(torch.int16), before.view(torch.int16))
+    # in place, without statistics; without parameters
+    z = x.clone()
+    smfg.layer_norm(z, count(n), cap, w, b, eps, z)
+    assert torch.equal(z[:n], y[:n]) and torch.equal(z[n:], x[n:])
+    smfg.layer_norm(x, count(n), cap, None, None, eps, z)
+    want, _, _, tol, _, _ = norm_of(x[:n], torch.ones_like(w), torch.zeros_like(b), eps)
+    check(z[:n], want, rounded(tol, want, dtype))
+
+
+def test_layer_norm_of_rows_off_centre():
+    """Means a thousand times the spread: squares of centred values keep their digits (a difference of means of squares would not)."""
+    x = 1000 + torch.randn((64, 4096), device=DEV, generator=gen(1))
+    one, zero = torch.ones(4096, device=DEV), torch.zeros(4096, device=DEV)
+    y = torch.empty_like(x)
+    smfg.layer_norm(x, count(64), 64, one, zero, 1e-5, y)
+    want, _, _, tol, _, _ = norm_of(x, one, zero, 1e-5)
+    check(y, want, rounded(tol, want, F32))
+    assert float(tol.max()) < 0.05
+
+
+def test_layer_norm_of_constant_rows_and_infinities():
+    """A constant row is its bias; an infinite or NaN row harms no other."""
+    for dim in (5, 100, 1000, 9000):
+        x = torch.full((6, dim), 3.0, device=DEV)
+        x[1], x[2, 0], x[4, dim - 1] = torch.randn(dim, device=DEV, generator=gen(1)), float("inf"), float("nan")
+        w, b = torch.full((dim,), 2.0, device=DEV), torch.arange(dim, device=DEV).float()
+        y = torch.empty_like(x)
+        smfg.layer_norm(x, count(6), 6, w, b, 1e-5, y)
+        want, _, _, tol, _, _ = norm_of(x[:2], w, b, 1e-5)
+        check(y[:2], want, rounded(tol, want, F32))
+        assert torch.equal(y[3], y[0]) and torch.equal(y[5], y[0])
+        assert y[2].isnan().all() and y[4].isnan().all()
+
+
+def norm_grad_of(dy, x, w, mean, rstd):
+    """(dx, dw, db, their tolerances before a rounding) in 64 bits, for the given statistics."""
+    n, dim = x.shape
+    dy, x, w, m, r = dy.double(), x.double(), w.double(), mean.double()[:, None], rstd.double()[:, None]
+    h, g = (x - m) * r, dy * w
+    c1, c2 = g.mean(1, keepdim=True), (g * h).mean(1, keepdim=True)
+    dx = r * (g - c1 - h * c2)
+    e = depth(dim) + 8
+    tol = r * (3 * U * g.abs() + e * U * g.abs().mean(1, keepdim=True) + h.abs() * (e * U * (g * h).abs().mean(1, keepdim=True) + 6 * U * c2.abs()) + 3 * U * c1.abs())
+    return dx, (dy * h).sum(0), dy.sum(0), 1.01 * tol, (n + 8) * U * (dy * h).abs().sum(0), (n + 8) * U * dy.abs().sum(0)
+
+
+@pytest.mark.parametrize("n,spare,dim,dtype,ptype,pad", NORMS)
+def test_layer_norm_grad(n, spare, dim, dtype, ptype, pad):
+    cap = n + spare
+    x, w, _ = norm_inputs(n, cap, dim, dtype, ptype, pad)
+    dy, _ = strided((cap, dim), dtype, pad + 2, 6)
+    v, m = torch.var_mean(x.float(), 1, correction=0)
+    r = (v + 1e-5).rsqrt()
+    ws = smfg.layer_norm_grad_workspace(cap, dim)
+    ws.data.fill_(0xA5)
+    dx, wide = strided((cap, dim), dtype, pad + 1, 7)
+    before = wide.clone()
+    dw, db = torch.full_like(w, 9), torch.full_like(w, 9)
+    smfg.layer_norm_grad(dy, x, count(n), cap, w, m, r, dx, dw, db, ws)
+    wx, ww, wb, tx, tw, tb = norm_grad_of(dy[:n], x[:n], w, m[:n], r[:n])
+    check(dx[:n], wx, rounded(tx, wx, dtype))
+    check(dw, ww, rounded(tw, ww, ptype))
+    check(db, wb, rounded(tb, wb, ptype))
+    before[:n, :dim] = dx[:n]
+    assert torch.equal(wide.view(torch.int16), before.view(torch.int16))
+    # one at a time, the same bits; dx in place of dy
+    a, b = torch.full_like(w, 9), torch.full_like(w, 9)
+    smfg.layer_norm_grad(dy, x, count(n), cap, w, m, r, None, a, None, ws)
+    smfg.layer_norm_grad(dy, x, count(n), cap, w, m, r, None, None, b, ws)
+    assert torch.equal(a, dw) and torch.equal(b, db)
+    z = dy.clone()
+    smfg.layer_norm_grad(z, x, count(n), cap, w, m, r, z, None, None, None)
+    assert torch.equal(z[:n], dx[:n]) and torch.equal(z[n:], dy[n:])
+    z = dy.clone()
+    smfg.layer_norm_grad(z, x, count(n), cap, w, m, r, z, a, b, ws)
+    assert torch.equal(z[:n], dx[:n]) and torch.equal(a, dw) and torch.equal(b, db)
+
+
+@pytest.mark.parametrize("dim", [24, 300])
+def test_layer_norm_grad_against_differences(dim):
+    """Central differences of the definition in 64 bits, at the kernel's own statistics: their error is of third order in the step."""
+    n, eps = 12, 1e-3
+    x, w, b = norm_inputs(n, n, dim, F32, F32, 0)
+    dy = torch.randn((n, dim), device=DEV, generator=gen(9))
+    y, m, r = torch.empty_like(x), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    smfg.layer_norm(x, count(n), n, w, b, eps, y, m, r)
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+    smfg.layer_norm_grad(dy, x, count(n), n, w, m, r, dx, dw, db, smfg.layer_norm_grad_workspace(n, dim))
+
+    def loss(x, w, b):
+        d = x - x.mean(1, keepdim=True)
+        return (dy.double() * (d / torch.sqrt((d * d).mean(1, keepdim=True) + eps) * w + b)).sum()
+
+    for seed in range(3):
+        vx, vw, vb = [torch.randn(t.shape, device=DEV, dtype=torch.float64, generator=gen(20 + seed)) for t in (x, w, b)]
+        s = 1e-4
+        at = [loss(x.double() + q * vx, w.double() + q * vw, b.double() + q * vb) for q in (s, -s)]
+        slope = float((at[0] - at[1]) / (2 * s))
+        got = float((dx.double() * vx).sum() + (dw.double() * vw).sum() + (db.double() * vb).sum())
+        # third derivatives of y are of the order r^3 for unit steps; the gradient's own roundings of 2^-24 per value
+        size = float((dx.double() * vx).abs().sum() + (dw.double() * vw).abs().sum() + (db.double() * vb).abs().sum())
+        cube = float((dy.abs().double().sum(1) * (r.double() * (1 + vx.abs().amax(1))) ** 3).sum()) * (1 + float(w.abs().max()))
+        assert abs(slope - got) <= 10 * s * s * cube + 200 * U * size
+
+
+# ---- clipping -----------------------------------------------------------------------------------
+
+def buffers(sizes, dtypes, seed, spread=1.0):
+    """Contiguous gradients that begin at any element of a larger buffer."""
+    out = []
+    for i, (n, t) in enumerate(zip(sizes, dtypes)):
+        wide = torch.full((n + 5,), float("nan"), dtype=t, device=DEV)
+        at = i % 4
+        wide[at:at + n] = (torch.randn(n, device=DEV, generator=gen(seed + i)) * spread).to(t)
+        out.append((wide[at:at + n], wide, at))
+    return out
+
+
+@pytest.mark.parametrize("sizes,max_norm,scale", [([1], 0.5, 1.0), ([0, 7, 0], 1.0, 1.0), ([], 1.0, 1.0), ([2048, 2049, 5, 2047], 1e6, 1.0),
+                                                  ([100_003, 33, 250_000], 1.0, 0.125), (list(range(1, 400)), 3.0, -2.0),
+                                                  ([9_000_000, 17], 0.1, 1.0 / 1024), ([64] * 85 + [5_000_000] + [0, 1], float("inf"), 3.0),
+                                                  ([256] * 84, float("inf"), 1.0)])
+def test_clip_grad_norm(sizes, max_norm, scale):
+    """The norm is added in double: one rounding.  A clipped value: the factor's rounding, the product's and the output's."""
+    types = [(F32, F16, BF16)[i % 3] for i in range(len(sizes))]
+    grads = buffers(sizes, types, 1)
+    outs = [torch.full((n,), 5.0, dtype=(F32 if i % 2 else t), device=DEV) for i, (n, t) in enumerate(zip(sizes, types))]
+    norm = torch.zeros(1, device=DEV)
+    n64 = math.sqrt(sum(float((g.double() * scale).square().sum()) for g, _, _ in grads))
+    f = scale * min(1.0, max_norm / (n64 + 1e-6)) if not math.isinf(max_norm) else scale
+    before = [w.clone() for _, w, _ in grads]
+    smfg.clip_grad_norm(smfg.grad_list([g for g, _, _ in grads], outs), max_norm, norm, scale=scale)
+    assert abs(float(norm) - n64) <= 2 * U * n64
+    for (g, w, _), o, b in zip(grads, outs, before):
+        want = g.double() * f
+        check(o, want, rounded(4 * U * want.abs(), want, o.dtype))
+        assert torch.equal(w.view(torch.int16), b.view(torch.int16))
+    # in place, half of them: the same bits, and nothing beside them
+    where = [o if i % 2 else None for i, o in enumerate(outs)]
+    smfg.clip_grad_norm(smfg.grad_list([g for g, _, _ in grads], where), max_norm, norm, scale=scale)
+    for i, ((g, w, at), o, b) in enumerate(zip(grads, outs, before)):
+        if i % 2 == 0:
+            assert torch.equal(g, o)
+            b[at:at + g.numel()] = o
+        assert torch.equal(w.view(torch.int16), b.view(torch.int16))
+
+
+def test_clip_grad_norm_of_counted_rows():
+    """Of a gradient of touched rows only those in use count and are written, however many the device says."""
+    rows, dim = 300, 37
+    for used in (0, 1, 299, 300, 999, -4):
+        g = torch.randn((rows, dim), device=DEV, generator=gen(1))
+        g[max(0, min(used, rows)):] = float("nan")
+        other = torch.randn(1000, device=DEV, generator=gen(2)).half()
+        was = g.clone()
+        m = max(0, min(used, rows))
+        n64 = math.sqrt(float(g[:m].double().square().sum() + other.double().square().sum()))
+        norm = torch.zeros(1, device=DEV)
+        smfg.clip_grad_norm(smfg.grad_list([g, other], rows=[count(used), None]), 2.0, norm)
+        assert abs(float(norm) - n64) <= 2 * U * n64
+        want = was[:m].double() * (2.0 / (n64 + 1e-6))
+        check(g[:m], want, rounded(4 * U * want.abs(), want, F32))
+        assert g[m:].isnan().all()
+
+
+def test_clip_grad_norm_of_large_infinite_and_nan_gradients():
+    norm = torch.zeros(1, device=DEV)
+    g = torch.full((5000,), 1e30, device=DEV)  # squares beyond a float's range
+    smfg.clip_grad_norm(smfg.grad_list([g]), 1.0, norm)
+    assert abs(float(norm) / (1e30 * math.sqrt(5000)) - 1) <= 4 * U
+    check(g, torch.full_like(g, 1 / math.sqrt(5000)).double(), 4 * U)
+    a, b = torch.ones(10, device=DEV), torch.full((3,), float("inf"), device=DEV)
+    smfg.clip_grad_norm(smfg.grad_list([a, b]), 1.0, norm)
+    assert float(norm) == float("inf") and not a.any() and b.isnan().all()
+    a, b = torch.ones(10, device=DEV), torch.full((3,), float("nan"), dtype=F16, device=DEV)
+    for limit in (1.0, 1e30):
+        smfg.clip_grad_norm(smfg.grad_list([a, b]), limit, norm)
+        assert float(norm) != float(norm) and a.isnan().all() and b.isnan().all()
+    z = torch.zeros(70, device=DEV)
+    smfg.clip_grad_norm(smfg.grad_list([z]), 1.0, norm)
+    assert float(norm) == 0 and not z.any()
+
+
+# ---- streams, graphs, order ---------------------------------------------------------------------
+
+def step_state(n=20_000, rows=5000, dim=96):
+    s = dict(n=n, rows=rows, dim=dim, ids=ids_of("mixed", n, rows, 1), table=torch.randn((rows, dim), device=DEV, generator=gen(2)), num=count(n),
+             h=torch.empty((n, dim), dtype=F16, device=DEV), y=torch.empty((n, dim), dtype=F16, device=DEV), m=torch.empty(n, device=DEV),
+             r=torch.empty(n, device=DEV), dy=torch.randn((n, dim), device=DEV, generator=gen(3)).half(), dh=torch.empty((n, dim), dtype=F16, device=DEV),
+             w=torch.ones(dim, device=DEV), b=torch.zeros(dim, device=DEV), dw=torch.empty(dim, device=DEV), db=torch.empty(dim, device=DEV),
+             rid=torch.zeros(n, dtype=torch.int32, device=DEV), nu=count(0), g=torch.zeros((n, dim), device=DEV), norm=torch.zeros(1, device=DEV),
+             ws=smfg.embedding_grad_workspace(n, rows, dim), wn=smfg.layer_norm_grad_workspace(n, dim))
+    s["list"] = smfg.grad_list([s["g"], s["dw"], s["db"]], rows=[s["nu"], None, None])
+    return s
+
+
+def step(s, stream=None):
+    """Lookup, norm and back, touched rows, clipping: all of them in one step."""
+    smfg.embedding(s["table"], s["ids"], s["num"], s["n"], s["h"], scale=2.0, stream=stream)
+    smfg.layer_norm(s["h"], s["num"], s["n"], s["w"], s["b"], 1e-5, s["y"], s["m"], s["r"], stream=stream)
+    smfg.layer_norm_grad(s["dy"], s["h"], s["num"], s["n"], s["w"], s["m"], s["r"], s["dh"], s["dw"], s["db"], s["wn"], stream=stream)
+    smfg.embedding_grad_rows(s["ids"], s["num"], s["n"], s["dh"], s["rows"], s["rid"], s["nu"], s["g"], s["ws"], scale=2.0, stream=stream)
+    smfg.clip_grad_norm(s["list"], 1.0, s["norm"], stream=stream)
+
+
+OUTS = ("y", "m", "r", "dh", "dw", "db", "rid", "nu", "g", "norm")
+
+
+def test_a_step_on_another_stream_and_again():
+    a, b = step_state(), step_state()
+    step(a)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    step(b, stream=side)
+    side.synchronize()
+    for k in OUTS:
+        assert torch.equal(a[k], b[k]), k
+    assert float(a["norm"]) > 1
+
+
+def test_a_step_in_a_graph():
+    """Replays over new inputs, with eager work between them, give the eager step's bits."""
+    a, b = step_state(), step_state()
+    step(a)  # nothing is set up by a first call
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a)
+    for k in range(4):
+        ids = ids_of(("mixed", "uniform", "outside", "same")[k], a["n"], a["rows"], 30 + k)
+        dy = torch.randn((a["n"], a["dim"]), device=DEV, generator=gen(40 + k)).half()
+        for s in (a, b):
+            s["ids"].copy_(ids)
+            s["dy"].copy_(dy)
+            s["num"].fill_(a["n"] - 3000 * k)
+            for o in ("g", "rid", "y", "dh", "m", "r"):
+                s[o].zero_()
+        graph.replay()
+        step(b)
+        torch.cuda.synchronize()
+        for o in OUTS:
+            assert torch.equal(a[o], b[o]), (k, o)
