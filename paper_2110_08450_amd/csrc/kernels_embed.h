@@ -172,33 +172,37 @@ static __global__ void __launch_bounds__(kThreads) k_sort_scatter(SortArgs A) {
 
 // ---- sums over runs of equal rows --------------------------------------------------------------
 //
-// The sorted tokens are cut into chunks of equal length, each the work of one group of lanes, whatever the ids are.  A run that
-// begins and ends in a chunk is a row of the gradient; what a chunk has of a run that began before it (its head) and of one that
-// goes on behind it (its tail) goes to `part`, from where k_embed_join adds it up, tail first, then the heads in their order.
+// The sorted tokens are cut into pieces of kGradTokens, each the work of one group of lanes, whatever the ids are, so that a
+// frequent id is no one's burden.  A run that begins and ends in a piece is a row of the gradient.  Of one that crosses pieces, what a
+// piece has of a run that began before it (its head) and of one that goes on behind it (its tail) is joined in the block, in the
+// order of the tokens; what crosses blocks goes to `part`, from where k_embed_join adds it up.
+constexpr int kGradTokens = 16;
+constexpr int kRunTile = 1024;     // a multiple of every block's tokens
+constexpr int kScanTiles = 1024;   // more run tiles than that are scanned by a launch of their own
+
 struct EmbedGradArgs {
-  const uint2* sorted;   // (row, token)
+  const uint2* sorted;     // (row, token)
   const int64_t* num;
   int64_t max_ids;
   int64_t num_rows;
-  int32_t chunk;         // tokens of a chunk
   int32_t dim;
+  int32_t accumulate;
   const void* dy;
   int64_t dy_stride;
   float scale;
-  int32_t accumulate;
+  uint32_t sum_blocks, tiles;  // blocks of k_embed_sums that add up, and tiles of columns; the blocks behind all of them clear
   void* grad;
   int64_t grad_stride;
-  float* part;           // [chunks][2][part_width]: head and tail
+  float* part;             // [blocks][2][part_width]: head and tail
   int64_t part_width;
+  int32_t clear_rows;      // rows of a block that clears
   // touched rows alone (row_ids != null): a run's row of `grad` is its rank
+  int32_t scanned;         // tile_runs holds its exclusive scan
   int32_t* row_ids;
   int64_t* num_unique;
-  uint32_t* tile_runs;   // runs that begin in a tile of kRunTile sorted tokens
-  uint32_t* chunk_runs;  // runs that begin in the tile of a chunk before it
+  uint32_t* tile_runs;     // runs that begin in a tile of kRunTile sorted tokens
+  int64_t run_tiles;
 };
-
-constexpr int kRunTile = 1024;  // a multiple of every chunk
-constexpr int kMaxChunk = 256;
 
 // Run begins at sorted place p?
 __device__ __forceinline__ bool run_begins(const EmbedGradArgs& A, int64_t p, int64_t n) {
@@ -209,41 +213,59 @@ __device__ __forceinline__ bool run_begins(const EmbedGradArgs& A, int64_t p, in
 
 static __global__ void __launch_bounds__(kThreads) k_embed_runs(EmbedGradArgs A) {
   __shared__ uint32_t lds[kThreads / 64];
-  constexpr int kPer = kRunTile / kThreads;
   const int64_t n = count_of(A.num, A.max_ids);
-  const int64_t p0 = static_cast<int64_t>(blockIdx.x) * kRunTile + threadIdx.x * kPer;
-  uint32_t c[kPer], sum = 0;
+  const int64_t p0 = static_cast<int64_t>(blockIdx.x) * kRunTile + threadIdx.x;
+  uint32_t sum = 0;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    c[k] = sum;
-    sum += run_begins(A, p0 + k, n) ? 1u : 0u;
-  }
+  for (int k = 0; k < kRunTile / kThreads; ++k) sum += run_begins(A, p0 + k * kThreads, n) ? 1u : 0u;
   uint32_t total;
-  const uint32_t before = block_exscan(sum, lds, total);
-#pragma unroll
-  for (int k = 0; k < kPer; ++k)
-    if (p0 + k < n && (p0 + k) % A.chunk == 0) A.chunk_runs[(p0 + k) / A.chunk] = before + c[k];
+  (void)block_exscan(sum, lds, total);
   if (threadIdx.x == 0) A.tile_runs[blockIdx.x] = total;
 }
 
 // Exclusive scan of the tiles' runs, by one block; their number.
-static __global__ void __launch_bounds__(kThreads) k_embed_scan(EmbedGradArgs A, int64_t tiles) {
+static __global__ void __launch_bounds__(kThreads) k_embed_scan(EmbedGradArgs A) {
   __shared__ uint32_t lds[kThreads / 64];
   uint32_t before = 0;
-  for (int64_t t0 = 0; t0 < tiles; t0 += kThreads) {
+  for (int64_t t0 = 0; t0 < A.run_tiles; t0 += kThreads) {
     const int64_t t = t0 + threadIdx.x;
-    const uint32_t c = t < tiles ? A.tile_runs[t] : 0u;
+    const uint32_t c = t < A.run_tiles ? A.tile_runs[t] : 0u;
     uint32_t sum;
     const uint32_t ex = block_exscan(c, lds, sum);
-    if (t < tiles) A.tile_runs[t] = before + ex;
+    if (t < A.run_tiles) A.tile_runs[t] = before + ex;
     before += sum;
   }
   if (threadIdx.x == 0) *A.num_unique = before;
 }
 
-// Rank among all runs of the first that begins in chunk c.
-__device__ __forceinline__ uint32_t runs_before_chunk(const EmbedGradArgs& A, int64_t c) {
-  return A.tile_runs[c * A.chunk / kRunTile] + A.chunk_runs[c];
+// Runs that begin before sorted place p, the first of a block's tokens; by the whole block.  *all: number of runs, for
+// p == 0 where the tiles are not scanned.
+__device__ __forceinline__ uint32_t runs_before(const EmbedGradArgs& A, int64_t p, int64_t n, uint32_t* lds, uint32_t& all) {
+  const int64_t tile = p / kRunTile;
+  uint32_t x = 0, y = 0;
+  if (A.scanned) {
+    if (threadIdx.x == 0) x = A.tile_runs[tile];
+  } else {
+    for (int64_t t = threadIdx.x; t < (p == 0 ? A.run_tiles : tile); t += blockDim.x) (p == 0 ? y : x) += A.tile_runs[t];
+  }
+  for (int64_t q = tile * kRunTile + threadIdx.x; q < p; q += blockDim.x) x += run_begins(A, q, n) ? 1u : 0u;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    x += __shfl_xor(x, o, 64);
+    y += __shfl_xor(y, o, 64);
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) {
+    lds[2 * (threadIdx.x >> 6)] = x;
+    lds[2 * (threadIdx.x >> 6) + 1] = y;
+  }
+  __syncthreads();
+  x = all = 0;
+  for (int w = 0; w < static_cast<int>(blockDim.x) / 64; ++w) {
+    x += lds[2 * w];
+    all += lds[2 * w + 1];
+  }
+  return x;
 }
 
 // V columns of a row of the gradient from their sum; those that the vector before has as well are left to it.
@@ -256,151 +278,248 @@ __device__ __forceinline__ void write_grad(const EmbedGradArgs& A, int64_t row, 
 #pragma unroll
     for (int j = 0; j < V; ++j) e.v[j] = from_float<TG>(as_float(e.v[j]) + A.scale * sum[j]);
     *reinterpret_cast<Elems<TG, V>*>(g) = e;
-  } else {
+  } else if (c.dup < V) {
 #pragma unroll
     for (int j = 0; j < V; ++j)
       if (j >= c.dup) g[j] = from_float<TG>((A.accumulate ? as_float(g[j]) : 0.f) + A.scale * sum[j]);
   }
 }
 
-constexpr int kGradDepth = 8;  // rows of dy on their way
-
-// A group of LANES lanes has a chunk and LANES * V columns of it (column tile blockIdx.y).
-template <typename TD, typename TG, int V, int LANES>
-__global__ void __launch_bounds__(kThreads) k_embed_grad(EmbedGradArgs A) {
-  constexpr int kGroups = kThreads / LANES;
-  const int lane = threadIdx.x % LANES;
-  const int64_t n = count_of(A.num, A.max_ids);
-  const int64_t chunk = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES;
-  const int64_t p0 = chunk * A.chunk;
-  if (p0 >= n) return;
-  const int len = static_cast<int>(n - p0 < A.chunk ? n - p0 : A.chunk);
-  const int index = static_cast<int>(blockIdx.y) * LANES + lane;
-  const Columns<V> c(index, A.dim);
-  const bool live = c.dup < V;
-  const uint2* rec = A.sorted + p0;
-  const uint32_t none = static_cast<uint32_t>(A.num_rows);
-  bool head = p0 > 0 && A.sorted[p0 - 1].x == rec[0].x;
-  const uint32_t behind = p0 + len < n ? A.sorted[p0 + len].x : none;
-  int64_t rank = A.row_ids ? static_cast<int64_t>(runs_before_chunk(A, chunk)) : 0;
-  const TD* dy = static_cast<const TD*>(A.dy) + c.start;
-  float* part = A.part + chunk * 2 * A.part_width + static_cast<int64_t>(index) * V;
-  float sum[V] = {};
-  uint32_t key = rec[0].x;
-  for (int t0 = 0; t0 < len; t0 += kGradDepth) {
-    uint32_t keys[kGradDepth];
-    Elems<TD, V> e[kGradDepth];
-#pragma unroll
-    for (int u = 0; u < kGradDepth; ++u) {
-      const uint2 r = rec[t0 + u < len ? t0 + u : len - 1];
-      keys[u] = r.x;
-      e[u] = {};
-      if (live && t0 + u < len && r.x < none) e[u] = *reinterpret_cast<const Elems<TD, V>*>(dy + r.y * A.dy_stride);
-    }
-#pragma unroll
-    for (int u = 0; u < kGradDepth; ++u) {
-      if (t0 + u >= len) break;
-      if (keys[u] != key) {  // the run of `key` ends here
-        if (key < none && live) {
-          if (head) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) part[j] = sum[j];
-          } else {
-            write_grad<TG, V>(A, A.row_ids ? rank : static_cast<int64_t>(key), c, sum);
-          }
-        }
-        if (!head && key < none) {
-          if (A.row_ids && index == 0) A.row_ids[rank] = static_cast<int32_t>(key);
-          ++rank;
-        }
-        head = false;
-        key = keys[u];
-#pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] = 0.f;
-      }
-#pragma unroll
-      for (int j = 0; j < V; ++j) sum[j] += as_float(e[u].v[j]);
-    }
+// First sorted place whose row is at least `key`, in [lo, hi].
+__device__ __forceinline__ int64_t sorted_bound(const uint2* sorted, int64_t lo, int64_t hi, uint32_t key) {
+  while (lo < hi) {
+    const int64_t mid = lo + (hi - lo) / 2;
+    if (sorted[mid].x < key) lo = mid + 1;
+    else hi = mid;
   }
-  if (key >= none) return;
-  if (!head && A.row_ids && index == 0) A.row_ids[rank] = static_cast<int32_t>(key);
-  if (!live) return;
-  if (head || key == behind) {
-    if (!head) part += A.part_width;
-#pragma unroll
-    for (int j = 0; j < V; ++j) part[j] = sum[j];
-  } else {
-    write_grad<TG, V>(A, A.row_ids ? rank : static_cast<int64_t>(key), c, sum);
+  return lo;
+}
+// The same by a wave, 64 places at a time.
+__device__ __forceinline__ int64_t wave_sorted_bound(const uint2* sorted, int64_t lo, int64_t hi, uint32_t key) {
+  const int lane = threadIdx.x & 63;
+  while (lo < hi) {  // the bound is in [lo, hi]
+    const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+    const int below = __popcll(__ballot(at < hi && sorted[at < hi ? at : lo].x < key));
+    if (below == 0) return lo;
+    const int64_t last = lo + (below - 1) * step;  // below the bound
+    hi = last + step < hi ? last + step : hi;
+    lo = last + 1;
+  }
+  return lo;
+}
+
+// Rows of the whole table's gradient that no token names: zeros.
+template <typename TG, int V>
+__device__ __forceinline__ void clear_rows(const EmbedGradArgs& A, int64_t n, uint32_t block, uint32_t* lds) {
+  const int64_t r0 = static_cast<int64_t>(block) * A.clear_rows;
+  const int rows = static_cast<int>(A.num_rows - r0 < A.clear_rows ? A.num_rows - r0 : A.clear_rows);
+  const int64_t lo = wave_sorted_bound(A.sorted, 0, n, static_cast<uint32_t>(r0));
+  const int64_t hi = wave_sorted_bound(A.sorted, lo, n, static_cast<uint32_t>(r0 + rows));
+  if (static_cast<int>(threadIdx.x) < rows) {
+    const uint32_t key = static_cast<uint32_t>(r0) + threadIdx.x;
+    const int64_t p = sorted_bound(A.sorted, lo, hi, key);
+    lds[threadIdx.x] = p < hi && A.sorted[p].x == key;
+  }
+  __syncthreads();
+  const uint32_t per_row = static_cast<uint32_t>((A.dim + V - 1) / V);
+  TG* g = static_cast<TG*>(A.grad) + r0 * A.grad_stride;
+  for (uint32_t i = threadIdx.x; i < rows * per_row; i += kThreads) {
+    const uint32_t r = i / per_row;
+    if (!lds[r]) *reinterpret_cast<Elems<TG, V>*>(g + r * A.grad_stride + Columns<V>(static_cast<int>(i - r * per_row), A.dim).start) = {};
   }
 }
 
-// First sorted place whose row is at least `key` (beyond: whose row is larger), from `from` on.
-__device__ __forceinline__ int64_t sorted_bound(const uint2* sorted, int64_t from, int64_t n, uint32_t key, bool beyond) {
-  int64_t lo = from, hi = n;
+template <typename TD, typename TG, int V, int LANES>
+__global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedGradArgs A) {
+  constexpr int kGroups = kThreads / LANES, kBlockTokens = kGroups * kGradTokens;
+  __shared__ float heads[kGroups][LANES * V];
+  __shared__ uint32_t goes_on[kGroups];  // bit 0: the group's last run goes on behind it; bit 1: it is its first and began before
+  __shared__ uint32_t lds[kThreads];
+  const int64_t n = count_of(A.num, A.max_ids);
+  const uint32_t tile = blockIdx.x / A.sum_blocks, block = blockIdx.x - tile * A.sum_blocks;
+  if (tile >= A.tiles) {
+    clear_rows<TG, V>(A, n, blockIdx.x - A.sum_blocks * A.tiles, lds);
+    return;
+  }
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  const int64_t b0 = static_cast<int64_t>(block) * kBlockTokens, p0 = b0 + group * kGradTokens;
+  uint32_t rank = 0;
+  if (A.row_ids) {
+    uint32_t all;
+    rank = runs_before(A, b0, n, lds, all);
+    if (blockIdx.x == 0 && threadIdx.x == 0 && !A.scanned) *A.num_unique = all;
+  }
+  if (b0 >= n) return;
+  const uint32_t none = static_cast<uint32_t>(A.num_rows);
+  const int index = static_cast<int>(tile) * LANES + lane;
+  const Columns<V> c(index, A.dim);
+  // the group's tokens, one to a lane
+  const int at = lane & (kGradTokens - 1);
+  const uint2 mine = p0 + at < n ? A.sorted[p0 + at] : make_uint2(none, 0);
+  const uint32_t before = p0 > 0 && p0 < n ? A.sorted[p0 - 1].x : none;
+  const uint32_t behind = p0 + kGradTokens < n ? A.sorted[p0 + kGradTokens].x : none;
+  const TD* dy = static_cast<const TD*>(A.dy) + c.start;
+  Elems<TD, V> e[kGradTokens];
+  uint32_t keys[kGradTokens];
+#pragma unroll
+  for (int u = 0; u < kGradTokens; ++u) {
+    keys[u] = __shfl(mine.x, u, LANES);
+    const uint32_t token = __shfl(mine.y, u, LANES);
+    e[u] = {};
+    if (c.dup < V && keys[u] < none) e[u] = *reinterpret_cast<const Elems<TD, V>*>(dy + token * A.dy_stride);
+  }
+  if (A.row_ids) {  // runs that begin in the groups before
+    const uint32_t left = __shfl_up(mine.x, 1, LANES);
+    const bool begins = lane < kGradTokens && mine.x < none && mine.x != (lane == 0 ? before : left);
+    const uint64_t set = __ballot(begins) >> (threadIdx.x & 63 & ~(LANES - 1));
+    const uint32_t begun = __popcll(LANES < 64 ? set & ((1ull << LANES % 64) - 1) : set);
+    __syncthreads();
+    if (lane == 0) lds[group] = begun;
+    __syncthreads();
+    for (int g = 0; g < group; ++g) rank += lds[g];
+    if (begins && tile == 0) A.row_ids[rank + __popcll(set & ((1ull << lane) - 1))] = static_cast<int32_t>(mine.x);
+  }
+  bool head = keys[0] < none && keys[0] == before;
+  float sum[V] = {};
+#pragma unroll
+  for (int u = 0; u < kGradTokens; ++u) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] += as_float(e[u].v[j]);
+    const bool last = u == kGradTokens - 1;
+    if (keys[u] == (last ? behind : keys[last ? 0 : u + 1])) continue;  // the run goes on
+    if (keys[u] < none) {
+      if (head) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) heads[group][j * LANES + lane] = sum[j];
+      } else {
+        write_grad<TG, V>(A, A.row_ids ? static_cast<int64_t>(rank++) : static_cast<int64_t>(keys[u]), c, sum);
+      }
+    }
+    head = false;
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = 0.f;
+  }
+  const uint32_t key = keys[kGradTokens - 1];
+  const bool open = key < none && key == behind;
+  if (open && head) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) heads[group][j * LANES + lane] = sum[j];
+  }
+  if (lane == 0) goes_on[group] = (open ? 1u : 0u) | (open && head ? 2u : 0u);
+  __syncthreads();
+  float* part = A.part + static_cast<int64_t>(block) * 2 * A.part_width + static_cast<int64_t>(index) * V;
+  if (c.dup == V) return;
+  // the run that goes on behind the group, unless it began before it
+  if (open && !head) {
+    int g = group + 1;
+    for (; g < kGroups; ++g) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[j] += heads[g][j * LANES + lane];
+      if (!(goes_on[g] & 2u)) break;
+    }
+    if (g < kGroups) {
+      write_grad<TG, V>(A, A.row_ids ? static_cast<int64_t>(rank) : static_cast<int64_t>(key), c, sum);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) part[A.part_width + j] = sum[j];
+    }
+  }
+  // the run that began before the block
+  if (group == 0 && keys[0] < none && keys[0] == before) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = heads[0][j * LANES + lane];
+    for (int g = 0; g + 1 < kGroups && (goes_on[g] & 2u); ++g) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[j] += heads[g + 1][j * LANES + lane];
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) part[j] = sum[j];
+  }
+}
+
+// Place of a touched row among their ascending ids.
+__device__ __forceinline__ int64_t rank_of_row(const EmbedGradArgs& A, uint32_t row) {
+  int64_t lo = 0, hi = *A.num_unique;
   while (lo < hi) {
     const int64_t mid = lo + (hi - lo) / 2;
-    const uint32_t k = sorted[mid].x;
-    if (k < key || (beyond && k == key)) lo = mid + 1;
+    if (static_cast<uint32_t>(A.row_ids[mid]) < row) lo = mid + 1;
     else hi = mid;
   }
   return lo;
 }
 
-// Runs that cross chunks: a block per chunk, which looks whether one begins in it and goes on.
-template <typename TG, int V>
-__global__ void __launch_bounds__(kThreads) k_embed_join(EmbedGradArgs A) {
-  constexpr int kLanes = 16, kGroups = kThreads / kLanes;
-  __shared__ float lds[kThreads * V];
+// Runs that cross blocks of k_embed_sums (of kGroups * kGradTokens tokens): one that ends within kJoinShort blocks behind the one it begins in by a
+// group of lanes, a longer one by a block of its own, which is the one of the first multiple of kJoinShort behind it.
+constexpr int kJoinThreads = 1024;
+constexpr int kJoinShort = 16;
+template <typename TG, int V, int LANES>
+__global__ void __launch_bounds__(kJoinThreads) k_embed_join(EmbedGradArgs A, uint32_t short_blocks) {
+  constexpr int kGroups = kJoinThreads / LANES;
+  constexpr int64_t kTokens = kThreads / LANES * kGradTokens;
+  __shared__ float lds[kGroups][LANES * V];
   const int64_t n = count_of(A.num, A.max_ids);
-  const int64_t chunk = blockIdx.x, p1 = (chunk + 1) * A.chunk;
-  if (p1 >= n) return;
-  const uint32_t key = A.sorted[p1 - 1].x;
-  if (key >= A.num_rows || A.sorted[p1].x != key) return;
-  const int64_t p0 = chunk * A.chunk;
-  if (A.sorted[p0].x == key && p0 > 0 && A.sorted[p0 - 1].x == key) return;  // it began before
-  const int64_t last = (sorted_bound(A.sorted, p1, n, key, true) - 1) / A.chunk;
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  const int index = static_cast<int>(blockIdx.y) * LANES + lane;
+  const Columns<V> c(index, A.dim);
+  const int64_t width = A.part_width;
+  const float* part = A.part + static_cast<int64_t>(index) * V;
+  float sum[V] = {};
+  if (blockIdx.x < short_blocks) {
+    const int64_t b = static_cast<int64_t>(blockIdx.x) * kGroups + group, p1 = (b + 1) * kTokens;
+    uint32_t key = static_cast<uint32_t>(A.num_rows);
+    bool begins = false;
+    int blocks = 0;  // behind b that have some of the run
+    if (p1 < n) {
+      key = A.sorted[p1 - 1].x;
+      begins = key < A.num_rows && (b == 0 || A.sorted[b * kTokens - 1].x != key);
+      const int64_t p = p1 + (lane % kJoinShort) * kTokens;
+      const bool goes_on = lane < kJoinShort && p < n && A.sorted[p < n ? p : p1].x == key;
+      const uint64_t set = __ballot(goes_on) >> (threadIdx.x & 63 & ~(LANES - 1));
+      blocks = __popcll(set & ((1ull << kJoinShort) - 1));
+    }
+    const bool joins = begins && blocks > 0 && blocks < kJoinShort;
+    if (!joins) return;
+    int64_t row = key;
+    if (A.row_ids) row = rank_of_row(A, key);
+    if (c.dup == V) return;
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = part[(2 * b + 1) * width + j];
+    for (int q = 1; q <= blocks; ++q) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[j] += part[2 * (b + q) * width + j];
+    }
+    write_grad<TG, V>(A, row, c, sum);
+    return;
+  }
+  const int64_t m = (static_cast<int64_t>(blockIdx.x - short_blocks) + 1) * kJoinShort;
+  if (m * kTokens >= n) return;
+  const uint32_t key = A.sorted[m * kTokens].x;
+  if (key >= A.num_rows || A.sorted[m * kTokens - 1].x != key) return;
+  const int64_t first = wave_sorted_bound(A.sorted, 0, m * kTokens, key), b = first / kTokens;
+  const int64_t last = (wave_sorted_bound(A.sorted, m * kTokens, n, key + 1) - 1) / kTokens;
+  if (m - b > kJoinShort || last - b < kJoinShort) return;
   int64_t row = key;
-  if (A.row_ids) {  // the last run that begins in the chunk
-    row = static_cast<int64_t>(runs_before_chunk(A, chunk + 1)) - 1;
-  }
-  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
-  const int vectors = (A.dim + V - 1) / V;
-  for (int i0 = 0; i0 < vectors; i0 += kLanes) {
-    const int index = i0 + lane;
-    float sum[V] = {};
-    if (index < vectors) {
-      const float* part = A.part + static_cast<int64_t>(index) * V;
-      if (group == 0) {
+  if (A.row_ids) row = rank_of_row(A, key);
+  if (c.dup < V) {
+    if (group == 0) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] = part[(2 * chunk + 1) * A.part_width + j];
-      }
-      for (int64_t q = chunk + 1 + group; q <= last; q += kGroups) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] += part[2 * q * A.part_width + j];
-      }
+      for (int j = 0; j < V; ++j) sum[j] = part[(2 * b + 1) * width + j];
     }
-    __syncthreads();
+#pragma unroll 4
+    for (int64_t q = b + 1 + group; q <= last; q += kGroups) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) lds[j * kThreads + threadIdx.x] = sum[j];
-    __syncthreads();
-    if (group == 0 && index < vectors) {
-      for (int g = 1; g < kGroups; ++g) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] += lds[j * kThreads + g * kLanes + lane];
-      }
-      write_grad<TG, V>(A, row, Columns<V>(index, A.dim), sum);
+      for (int j = 0; j < V; ++j) sum[j] += part[2 * q * width + j];
     }
   }
-}
-
-// Rows of the whole table's gradient before the touched ones are written.
-template <typename TG, int V>
-__global__ void __launch_bounds__(kThreads) k_embed_clear(void* grad, int64_t grad_stride, int64_t num_rows, int32_t dim) {
-  const int64_t per_row = (dim + V - 1) / V, all = num_rows * per_row;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
-    const int64_t row = i / per_row;
-    *reinterpret_cast<Elems<TG, V>*>(static_cast<TG*>(grad) + row * grad_stride + Columns<V>(static_cast<int>(i - row * per_row), dim).start) = {};
+#pragma unroll
+  for (int j = 0; j < V; ++j) lds[group][j * LANES + lane] = sum[j];
+  __syncthreads();
+  if (group != 0 || c.dup == V) return;
+  for (int g = 1; g < kGroups; ++g) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] += lds[g][j * LANES + lane];
   }
+  write_grad<TG, V>(A, row, c, sum);
 }
 
 }  // namespace smfg_dev

@@ -47,26 +47,38 @@ void launch_embedding(const EmbedArgs& A, unsigned blocks, bool vectors, hipStre
   else k_embedding<TI, TO, 1><<<blocks, kThreads, 0, st>>>(A);
 }
 
-// Sorted tokens of a chunk: as many as leave about 3000 waves of 64 lanes, but 16 to kMaxChunk.
-int chunk_of(int64_t max_ids, int32_t dim) {
-  const int64_t lanes = ceil_div(dim, 8);
-  int c = 16;
-  while (c < kMaxChunk && max_ids * lanes / (2 * c) >= 3000 * 64) c *= 2;
-  return c;
+// How the sums of a gradient are dealt: V columns a lane, LANES lanes a group, kThreads / LANES groups a block.
+struct GradShape {
+  int vector, lanes;
+  int64_t tokens, blocks, tiles, width;  // tokens of a block, blocks, tiles of columns, floats of a row of partial sums
+};
+GradShape grad_shape(int64_t max_ids, int32_t dim, int vector) {
+  GradShape S;
+  S.vector = dim < vector ? 1 : vector;
+  const int64_t vectors = ceil_div(dim, S.vector);
+  S.lanes = vectors <= 16 ? 16 : vectors <= 32 ? 32 : 64;
+  S.tokens = kThreads / S.lanes * kGradTokens;
+  S.blocks = ceil_div(max_ids, S.tokens);
+  S.tiles = ceil_div(vectors, S.lanes);
+  S.width = vectors * S.vector;
+  return S;
 }
+// 16 bytes of the wider of the two types: whole vectors are read and written, neither wider than an instruction.
+inline int grad_vector(int32_t dy_dtype, int32_t grad_dtype) { return type_bytes(dy_dtype) == 2 && type_bytes(grad_dtype) == 2 ? 8 : 4; }
 
 struct EmbedScratch {
-  int64_t rec[2], hist, total, part, tile_runs, chunk_runs, bytes;
-  int64_t tiles, chunks, run_tiles, part_width;
-  int chunk;
+  int64_t rec[2], hist, total, part, tile_runs, bytes;
+  int64_t tiles, run_tiles;
 };
 EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
   EmbedScratch S;
-  S.chunk = chunk_of(max_ids, dim);
   S.tiles = ceil_div(max_ids, kSortTile);
-  S.chunks = ceil_div(max_ids, S.chunk);
   S.run_tiles = ceil_div(max_ids, kRunTile);
-  S.part_width = ceil_div(dim, 8) * 8;
+  int64_t part = 0;
+  for (const int v : {4, 8}) {
+    const GradShape G = grad_shape(max_ids, dim, v);
+    if (G.blocks * G.width > part) part = G.blocks * G.width;
+  }
   int64_t at = 0;
   const auto take = [&at](int64_t bytes) {
     const int64_t here = at;
@@ -77,9 +89,8 @@ EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
   S.rec[1] = take(8 * max_ids);
   S.hist = take(4 * kSortBins * S.tiles);
   S.total = take(4 * kSortBins);
-  S.part = take(4 * 2 * S.part_width * S.chunks);
+  S.part = take(4 * 2 * part);
   S.tile_runs = take(4 * S.run_tiles);
-  S.chunk_runs = take(4 * S.chunks);
   S.bytes = at;
   return S;
 }
@@ -100,29 +111,30 @@ const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* id
   return A.in;
 }
 
-template <typename TD, typename TG, int V>
-void launch_embed_sums(const EmbedGradArgs& A, int64_t chunks, hipStream_t st) {
-  const int64_t vectors = ceil_div(A.dim, V);
-  const auto blocks = [&](int lanes) {
-    return dim3(static_cast<unsigned>(ceil_div(chunks, kThreads / lanes)), static_cast<unsigned>(ceil_div(vectors, lanes)));
-  };
-  if (vectors <= 16) k_embed_grad<TD, TG, V, 16><<<blocks(16), kThreads, 0, st>>>(A);
-  else if (vectors <= 32) k_embed_grad<TD, TG, V, 32><<<blocks(32), kThreads, 0, st>>>(A);
-  else k_embed_grad<TD, TG, V, 64><<<blocks(64), kThreads, 0, st>>>(A);
-  if (chunks > 1) k_embed_join<TG, V><<<static_cast<unsigned>(chunks), kThreads, 0, st>>>(A);
+template <typename TD, typename TG, int V, int LANES>
+void launch_embed_sums(EmbedGradArgs A, const GradShape& G, bool clear, hipStream_t st) {
+  A.sum_blocks = static_cast<uint32_t>(G.blocks);
+  // a block clears about 32 KiB, of at most a row a thread
+  const int64_t rows = (32 << 10) / (A.dim * static_cast<int64_t>(sizeof(TG)));
+  A.clear_rows = static_cast<int32_t>(rows < 1 ? 1 : rows > kThreads ? kThreads : rows);
+  A.tiles = G.blocks > 0 ? static_cast<uint32_t>(G.tiles) : 0u;
+  if (G.blocks == 0) A.sum_blocks = 1;  // none of whose tiles there is
+  const int64_t blocks = G.blocks * G.tiles + (clear ? ceil_div(A.num_rows, A.clear_rows) : 0);
+  if (blocks == 0) return;
+  k_embed_sums<TD, TG, V, LANES><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(A);
+  if (G.blocks < 2) return;
+  const uint32_t joins = static_cast<uint32_t>(ceil_div(G.blocks, kJoinThreads / LANES));
+  const unsigned longs = static_cast<unsigned>((G.blocks - 1) / kJoinShort);
+  k_embed_join<TG, V, LANES><<<dim3(joins + longs, static_cast<unsigned>(G.tiles)), kJoinThreads, 0, st>>>(A, joins);
 }
 
 template <typename TD, typename TG>
-void launch_embed_grad(const EmbedGradArgs& A, int64_t chunks, bool clear, hipStream_t st) {
-  constexpr int kG = kVec<TG>;
-  if (clear) {
-    const int64_t rows = A.num_rows;
-    if (A.dim >= kG) k_embed_clear<TG, kG><<<blocks_for(rows * ceil_div(A.dim, kG), 4 * kThreads, 65536), kThreads, 0, st>>>(A.grad, A.grad_stride, rows, A.dim);
-    else k_embed_clear<TG, 1><<<blocks_for(rows * A.dim, 4 * kThreads, 65536), kThreads, 0, st>>>(A.grad, A.grad_stride, rows, A.dim);
-  }
-  if (chunks == 0) return;
-  if (A.dim >= kVec<TD>) launch_embed_sums<TD, TG, kVec<TD>>(A, chunks, st);
-  else launch_embed_sums<TD, TG, 1>(A, chunks, st);
+void launch_embed_grad(const EmbedGradArgs& A, const GradShape& G, bool clear, hipStream_t st) {
+  constexpr int V = sizeof(TD) == 2 && sizeof(TG) == 2 ? 8 : 4;
+  if (G.vector == 1) launch_embed_sums<TD, TG, 1, 16>(A, G, clear, st);
+  else if (G.lanes == 16) launch_embed_sums<TD, TG, V, 16>(A, G, clear, st);
+  else if (G.lanes == 32) launch_embed_sums<TD, TG, V, 32>(A, G, clear, st);
+  else launch_embed_sums<TD, TG, V, 64>(A, G, clear, st);
 }
 
 int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids, int64_t max_ids, const void* d_dy, int64_t dy_stride,
@@ -139,19 +151,35 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
   if (max_ids == 0 && !rows_only && accumulate) return SMFG_OK;
   const EmbedScratch S = embed_scratch(max_ids, dim);
   if (max_ids > 0 && scratch_bytes < S.bytes) return SMFG_ERR_CAPACITY;
+  const GradShape G = grad_shape(max_ids, dim, grad_vector(dy_dtype, grad_dtype));
   uint8_t* scratch = static_cast<uint8_t*>(d_scratch);
-  EmbedGradArgs A = {nullptr, d_num_ids, max_ids, num_rows, S.chunk, dim, d_dy, dy_stride, scale, accumulate, d_grad, grad_stride,
-                     reinterpret_cast<float*>(scratch + S.part), S.part_width, d_row_ids, d_num_unique,
-                     reinterpret_cast<uint32_t*>(scratch + S.tile_runs), reinterpret_cast<uint32_t*>(scratch + S.chunk_runs)};
+  EmbedGradArgs A = {};
+  A.num = d_num_ids;
+  A.max_ids = max_ids;
+  A.num_rows = num_rows;
+  A.dim = dim;
+  A.accumulate = accumulate;
+  A.dy = d_dy;
+  A.dy_stride = dy_stride;
+  A.scale = scale;
+  A.grad = d_grad;
+  A.grad_stride = grad_stride;
+  A.part = reinterpret_cast<float*>(scratch + S.part);
+  A.part_width = G.width;
+  A.row_ids = d_row_ids;
+  A.num_unique = d_num_unique;
+  A.tile_runs = reinterpret_cast<uint32_t*>(scratch + S.tile_runs);
+  A.run_tiles = S.run_tiles;
   if (max_ids > 0) A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, st);
   if (rows_only) {
     if (max_ids > 0) k_embed_runs<<<static_cast<unsigned>(S.run_tiles), kThreads, 0, st>>>(A);
-    k_embed_scan<<<1, kThreads, 0, st>>>(A, S.run_tiles);
+    A.scanned = S.run_tiles == 0 || S.run_tiles > kScanTiles;
+    if (A.scanned) k_embed_scan<<<1, kThreads, 0, st>>>(A);
   }
   with_type(dy_dtype, [&](auto t) {
     using T = decltype(t);
-    if (grad_dtype == SMFG_DTYPE_F32) launch_embed_grad<T, float>(A, S.chunks, !rows_only && !accumulate, st);
-    else launch_embed_grad<T, T>(A, S.chunks, !rows_only && !accumulate, st);
+    if (grad_dtype == SMFG_DTYPE_F32) launch_embed_grad<T, float>(A, G, !rows_only && !accumulate, st);
+    else launch_embed_grad<T, T>(A, G, !rows_only && !accumulate, st);
   });
   return hip_err(hipGetLastError());
 }
