@@ -32,7 +32,8 @@ __device__ __forceinline__ int64_t count_of(const int64_t* num, int64_t max) {
 }
 
 // The vector of V columns that a lane has of a row of dim (>= V) columns, by the vector's index: it begins at column
-// index * V, or ends with the row, its first `dup` columns those of the vector before.  dup == V: there is none.
+// index * V, or ends with the row, its first `dup` columns those of the vector before.  dup == V: there is none, and `start` is the
+// last vector's, so that a load needs no condition.
 template <int V>
 struct Columns {
   int start, dup;

@@ -6,10 +6,13 @@
 
 namespace smfg_dev {
 
-// Ids of 4 or 8 bytes; one outside [0, num_rows) stands for no row and is read as num_rows.
+// Ids of 4 or 8 bytes; one outside [0, num_rows) stands for no row and is read as num_rows.  An id's words are read without a
+// condition, as a load under one is waited for before the next: an id of 4 bytes as its own upper word, which is not looked at.
 __device__ __forceinline__ uint32_t row_of_id(const void* ids, int32_t id_bytes, int64_t i, int64_t num_rows) {
-  const int64_t v = id_bytes == 8 ? static_cast<const int64_t*>(ids)[i] : static_cast<const int32_t*>(ids)[i];
-  return static_cast<uint32_t>(v < 0 || v >= num_rows ? num_rows : v);
+  const int words = id_bytes >> 2;
+  const uint32_t* p = static_cast<const uint32_t*>(ids) + i * words;
+  const uint32_t lower = p[0], upper = p[words - 1];
+  return (lower < num_rows) & ((words == 1) | (upper == 0)) ? lower : static_cast<uint32_t>(num_rows);
 }
 
 struct EmbedArgs {
@@ -43,14 +46,15 @@ __global__ void __launch_bounds__(kThreads) k_embedding(EmbedArgs A) {
     const uint32_t i = off + k * kThreads + threadIdx.x;
     row[k] = i / per_row;
     at[k] = i - row[k] * per_row;
-    id[k] = row0 + row[k] < n ? row_of_id(A.ids, A.id_bytes, row0 + row[k], A.num_rows) : static_cast<uint32_t>(A.num_rows);
+    const int64_t r = row0 + row[k];
+    id[k] = row_of_id(A.ids, A.id_bytes, r < A.max_ids ? r : A.max_ids - 1, A.num_rows);
   }
   Elems<TI, V> e[kEmbedTurns];
 #pragma unroll
   for (int k = 0; k < kEmbedTurns; ++k) {
-    e[k] = {};
-    if (id[k] < A.num_rows)
-      e[k] = *reinterpret_cast<const Elems<TI, V>*>(static_cast<const TI*>(A.table) + id[k] * A.table_stride + Columns<V>(at[k], A.dim).start);
+    // row 0 stands for one that there is not: a load under a condition is waited for before the next
+    e[k] = *reinterpret_cast<const Elems<TI, V>*>(static_cast<const TI*>(A.table) + (id[k] < A.num_rows ? id[k] : 0u) * A.table_stride +
+                                                  Columns<V>(at[k], A.dim).start);
   }
 #pragma unroll
   for (int k = 0; k < kEmbedTurns; ++k) {
@@ -172,13 +176,20 @@ static __global__ void __launch_bounds__(kThreads) k_sort_scatter(SortArgs A) {
 
 // ---- sums over runs of equal rows --------------------------------------------------------------
 //
-// The sorted tokens are cut into pieces of kGradTokens, each the work of one group of lanes, whatever the ids are, so that a
-// frequent id is no one's burden.  A run that begins and ends in a piece is a row of the gradient.  Of one that crosses pieces, what a
-// piece has of a run that began before it (its head) and of one that goes on behind it (its tail) is joined in the block, in the
-// order of the tokens; what crosses blocks goes to `part`, from where k_embed_join adds it up.
+// The sorted tokens are cut into pieces of kGradTokens, each the work of one wave, whatever the ids are, so that a frequent id is no
+// one's burden.  A run that begins and ends in a piece is a row of the gradient.  Of one that crosses pieces, what a piece has of a
+// run that began before it (its head) and of one that goes on behind it (its tail) is joined in the block, in the order of the
+// tokens; what crosses blocks goes to `part`, from where k_embed_join adds it up.
+//
+// A wave has one row at a time, so that rows, their ends and the addresses are scalar: with groups of 32 lanes, two rows to a wave, ends that
+// differ made both halves wait and every lane work out addresses.  A lane has V columns, as few as let 64 lanes have the whole row.
 constexpr int kGradTokens = 16;
+constexpr int kGradWaves = 8;
+constexpr int kGradThreads = 64 * kGradWaves;
+constexpr int kBlockTokens = kGradWaves * kGradTokens;
 constexpr int kRunTile = 1024;     // a multiple of every block's tokens
 constexpr int kScanTiles = 1024;   // more run tiles than that are scanned by a launch of their own
+constexpr int grad_columns(int dim) { return dim <= 64 ? 1 : dim <= 128 ? 2 : 4; }
 
 struct EmbedGradArgs {
   const uint2* sorted;     // (row, token)
@@ -201,25 +212,24 @@ struct EmbedGradArgs {
   int32_t* row_ids;
   int64_t* num_unique;
   uint32_t* tile_runs;     // runs that begin in a tile of kRunTile sorted tokens
+  uint32_t* block_runs;    // runs that begin in a block's tile before it
   int64_t run_tiles;
 };
 
-// Run begins at sorted place p?
-__device__ __forceinline__ bool run_begins(const EmbedGradArgs& A, int64_t p, int64_t n) {
-  if (p >= n) return false;
-  const uint32_t key = A.sorted[p].x;
-  return key < A.num_rows && (p == 0 || A.sorted[p - 1].x != key);
-}
-
 static __global__ void __launch_bounds__(kThreads) k_embed_runs(EmbedGradArgs A) {
   __shared__ uint32_t lds[kThreads / 64];
+  constexpr int kPer = kRunTile / kThreads;
   const int64_t n = count_of(A.num, A.max_ids);
-  const int64_t p0 = static_cast<int64_t>(blockIdx.x) * kRunTile + threadIdx.x;
-  uint32_t sum = 0;
+  const int64_t p0 = static_cast<int64_t>(blockIdx.x) * kRunTile + threadIdx.x * kPer;
+  const uint32_t none = static_cast<uint32_t>(A.num_rows);
+  uint32_t keys[kPer + 1], sum = 0;
 #pragma unroll
-  for (int k = 0; k < kRunTile / kThreads; ++k) sum += run_begins(A, p0 + k * kThreads, n) ? 1u : 0u;
+  for (int k = 0; k <= kPer; ++k) keys[k] = A.sorted[p0 + k > 0 && p0 + k <= A.max_ids ? p0 + k - 1 : 0].x;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) sum += p0 + k < n && keys[k + 1] < none && (p0 + k == 0 || keys[k] != keys[k + 1]) ? 1u : 0u;
   uint32_t total;
-  (void)block_exscan(sum, lds, total);
+  const uint32_t before = block_exscan(sum, lds, total);
+  if (p0 % kBlockTokens == 0 && p0 < A.max_ids) A.block_runs[p0 / kBlockTokens] = before;
   if (threadIdx.x == 0) A.tile_runs[blockIdx.x] = total;
 }
 
@@ -238,33 +248,15 @@ static __global__ void __launch_bounds__(kThreads) k_embed_scan(EmbedGradArgs A)
   if (threadIdx.x == 0) *A.num_unique = before;
 }
 
-// Runs that begin before sorted place p, the first of a block's tokens; by the whole block.  *all: number of runs, for
-// p == 0 where the tiles are not scanned.
-__device__ __forceinline__ uint32_t runs_before(const EmbedGradArgs& A, int64_t p, int64_t n, uint32_t* lds, uint32_t& all) {
-  const int64_t tile = p / kRunTile;
-  uint32_t x = 0, y = 0;
-  if (A.scanned) {
-    if (threadIdx.x == 0) x = A.tile_runs[tile];
-  } else {
-    for (int64_t t = threadIdx.x; t < (p == 0 ? A.run_tiles : tile); t += blockDim.x) (p == 0 ? y : x) += A.tile_runs[t];
-  }
-  for (int64_t q = tile * kRunTile + threadIdx.x; q < p; q += blockDim.x) x += run_begins(A, q, n) ? 1u : 0u;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    x += __shfl_xor(x, o, 64);
-    y += __shfl_xor(y, o, 64);
-  }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) {
-    lds[2 * (threadIdx.x >> 6)] = x;
-    lds[2 * (threadIdx.x >> 6) + 1] = y;
-  }
-  __syncthreads();
-  x = all = 0;
-  for (int w = 0; w < static_cast<int>(blockDim.x) / 64; ++w) {
-    x += lds[2 * w];
-    all += lds[2 * w + 1];
-  }
+// A thread's share of the runs that begin before a block's tokens; all: of all runs, where the tiles are not scanned, for block 0.
+__device__ __forceinline__ uint32_t share_of_runs(const EmbedGradArgs& A, uint32_t block, uint32_t& all) {
+  const int64_t tile = static_cast<int64_t>(block) * kBlockTokens / kRunTile;
+  uint32_t x = threadIdx.x == 0 ? A.block_runs[block] : 0u;
+  all = 0;
+  if (A.scanned) return threadIdx.x == 0 ? x + A.tile_runs[tile] : 0u;
+  if (block == 0)
+    for (int64_t t = threadIdx.x; t < A.run_tiles; t += blockDim.x) all += A.tile_runs[t];
+  for (int64_t t = threadIdx.x; t < tile; t += blockDim.x) x += A.tile_runs[t];
   return x;
 }
 
@@ -323,101 +315,108 @@ __device__ __forceinline__ void clear_rows(const EmbedGradArgs& A, int64_t n, ui
   __syncthreads();
   const uint32_t per_row = static_cast<uint32_t>((A.dim + V - 1) / V);
   TG* g = static_cast<TG*>(A.grad) + r0 * A.grad_stride;
-  for (uint32_t i = threadIdx.x; i < rows * per_row; i += kThreads) {
+  for (uint32_t i = threadIdx.x; i < rows * per_row; i += blockDim.x) {
     const uint32_t r = i / per_row;
     if (!lds[r]) *reinterpret_cast<Elems<TG, V>*>(g + r * A.grad_stride + Columns<V>(static_cast<int>(i - r * per_row), A.dim).start) = {};
   }
 }
 
-template <typename TD, typename TG, int V, int LANES>
-__global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedGradArgs A) {
-  constexpr int kGroups = kThreads / LANES, kBlockTokens = kGroups * kGradTokens;
-  __shared__ float heads[kGroups][LANES * V];
-  __shared__ uint32_t goes_on[kGroups];  // bit 0: the group's last run goes on behind it; bit 1: it is its first and began before
-  __shared__ uint32_t lds[kThreads];
-  const int64_t n = count_of(A.num, A.max_ids);
+template <typename TD, typename TG, int V>
+__global__ void __launch_bounds__(kGradThreads) k_embed_sums(EmbedGradArgs A) {
+  __shared__ float heads[kGradWaves][64 * V];
+  __shared__ uint32_t goes_on[kGradWaves];  // the wave's tokens are all of one run, that began before them and goes on behind them
+  __shared__ uint32_t lds[kGradThreads];
   const uint32_t tile = blockIdx.x / A.sum_blocks, block = blockIdx.x - tile * A.sum_blocks;
+  const int64_t n = count_of(A.num, A.max_ids);
   if (tile >= A.tiles) {
     clear_rows<TG, V>(A, n, blockIdx.x - A.sum_blocks * A.tiles, lds);
     return;
   }
-  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
-  const int64_t b0 = static_cast<int64_t>(block) * kBlockTokens, p0 = b0 + group * kGradTokens;
-  uint32_t rank = 0;
-  if (A.row_ids) {
-    uint32_t all;
-    rank = runs_before(A, b0, n, lds, all);
-    if (blockIdx.x == 0 && threadIdx.x == 0 && !A.scanned) *A.num_unique = all;
-  }
-  if (b0 >= n) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t b0 = static_cast<int64_t>(block) * kBlockTokens, p0 = b0 + wave * kGradTokens;
   const uint32_t none = static_cast<uint32_t>(A.num_rows);
-  const int index = static_cast<int>(tile) * LANES + lane;
+  const int index = static_cast<int>(tile) * 64 + lane;
   const Columns<V> c(index, A.dim);
-  // the group's tokens, one to a lane
-  const int at = lane & (kGradTokens - 1);
-  const uint2 mine = p0 + at < n ? A.sorted[p0 + at] : make_uint2(none, 0);
-  const uint32_t before = p0 > 0 && p0 < n ? A.sorted[p0 - 1].x : none;
-  const uint32_t behind = p0 + kGradTokens < n ? A.sorted[p0 + kGradTokens].x : none;
-  const TD* dy = static_cast<const TD*>(A.dy) + c.start;
+  // the wave's tokens, one to a lane, from lane 1 on; lane 0 has the one before, lane kGradTokens + 1 the one behind
+  const int64_t at = p0 - 1 + lane;
+  uint2 mine = A.sorted[at < 0 ? 0 : at < A.max_ids ? at : A.max_ids - 1];
+  if (lane > kGradTokens + 1 || at < 0 || at >= n) mine = make_uint2(none, 0);
+  uint32_t rank = 0, all = 0;
+  if (A.row_ids) rank = share_of_runs(A, block, all);
+  // Every row is read, also a padded place's and for columns that there are not (the last ones again), and dropped later: loads under a
+  // condition are waited for one by one.  Token 0 stands for those behind the last.
+  const TD* dy = static_cast<const TD*>(A.dy);
   Elems<TD, V> e[kGradTokens];
-  uint32_t keys[kGradTokens];
 #pragma unroll
   for (int u = 0; u < kGradTokens; ++u) {
-    keys[u] = __shfl(mine.x, u, LANES);
-    const uint32_t token = __shfl(mine.y, u, LANES);
-    e[u] = {};
-    if (c.dup < V && keys[u] < none) e[u] = *reinterpret_cast<const Elems<TD, V>*>(dy + token * A.dy_stride);
+    const uint32_t token = __builtin_amdgcn_readlane(mine.y, u + 1);
+    e[u] = *reinterpret_cast<const Elems<TD, V>*>(dy + token * A.dy_stride + c.start);
   }
-  if (A.row_ids) {  // runs that begin in the groups before
-    const uint32_t left = __shfl_up(mine.x, 1, LANES);
-    const bool begins = lane < kGradTokens && mine.x < none && mine.x != (lane == 0 ? before : left);
-    const uint64_t set = __ballot(begins) >> (threadIdx.x & 63 & ~(LANES - 1));
-    const uint32_t begun = __popcll(LANES < 64 ? set & ((1ull << LANES % 64) - 1) : set);
+  if (A.row_ids) {
+    const uint32_t left = __shfl_up(mine.x, 1, 64);  // by all lanes: not in the condition
+    const bool begins = lane >= 1 && lane <= kGradTokens && mine.x < none && mine.x != left;
+    const uint64_t set = __ballot(begins);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      rank += __shfl_xor(rank, o, 64);
+      if (block == 0) all += __shfl_xor(all, o, 64);
+    }
+    if (lane == 0) {
+      lds[wave] = rank;
+      lds[kGradWaves + wave] = all;
+      lds[2 * kGradWaves + wave] = __popcll(set);
+    }
     __syncthreads();
-    if (lane == 0) lds[group] = begun;
-    __syncthreads();
-    for (int g = 0; g < group; ++g) rank += lds[g];
+    rank = all = 0;
+    for (int w = 0; w < kGradWaves; ++w) {
+      rank += lds[w] + (w < wave ? lds[2 * kGradWaves + w] : 0u);
+      all += lds[kGradWaves + w];
+    }
+    rank = __builtin_amdgcn_readfirstlane(rank);
+    if (blockIdx.x == 0 && threadIdx.x == 0 && !A.scanned) *A.num_unique = all;
     if (begins && tile == 0) A.row_ids[rank + __popcll(set & ((1ull << lane) - 1))] = static_cast<int32_t>(mine.x);
   }
-  bool head = keys[0] < none && keys[0] == before;
+  if (b0 >= n) return;
+  const uint32_t before = __builtin_amdgcn_readlane(mine.x, 0), first = __builtin_amdgcn_readlane(mine.x, 1);
+  const uint32_t key = __builtin_amdgcn_readlane(mine.x, kGradTokens), behind = __builtin_amdgcn_readlane(mine.x, kGradTokens + 1);
+  const bool began_before = first < none && first == before, open = key < none && key == behind;
+  bool head = began_before;
   float sum[V] = {};
 #pragma unroll
   for (int u = 0; u < kGradTokens; ++u) {
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] += as_float(e[u].v[j]);
-    const bool last = u == kGradTokens - 1;
-    if (keys[u] == (last ? behind : keys[last ? 0 : u + 1])) continue;  // the run goes on
-    if (keys[u] < none) {
+    const uint32_t here = __builtin_amdgcn_readlane(mine.x, u + 1), next = __builtin_amdgcn_readlane(mine.x, u + 2);
+    if (here == next) continue;  // the run goes on
+    if (here < none) {
       if (head) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) heads[group][j * LANES + lane] = sum[j];
+        for (int j = 0; j < V; ++j) heads[wave][j * 64 + lane] = sum[j];
       } else {
-        write_grad<TG, V>(A, A.row_ids ? static_cast<int64_t>(rank++) : static_cast<int64_t>(keys[u]), c, sum);
+        write_grad<TG, V>(A, A.row_ids ? static_cast<int64_t>(rank++) : static_cast<int64_t>(here), c, sum);
       }
     }
     head = false;
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = 0.f;
   }
-  const uint32_t key = keys[kGradTokens - 1];
-  const bool open = key < none && key == behind;
   if (open && head) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) heads[group][j * LANES + lane] = sum[j];
+    for (int j = 0; j < V; ++j) heads[wave][j * 64 + lane] = sum[j];
   }
-  if (lane == 0) goes_on[group] = (open ? 1u : 0u) | (open && head ? 2u : 0u);
+  if (lane == 0) goes_on[wave] = open && head ? 1u : 0u;
   __syncthreads();
   float* part = A.part + static_cast<int64_t>(block) * 2 * A.part_width + static_cast<int64_t>(index) * V;
   if (c.dup == V) return;
-  // the run that goes on behind the group, unless it began before it
+  // the run that goes on behind the wave's tokens, unless it began before them
   if (open && !head) {
-    int g = group + 1;
-    for (; g < kGroups; ++g) {
+    int w = wave + 1;
+    for (; w < kGradWaves; ++w) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) sum[j] += heads[g][j * LANES + lane];
-      if (!(goes_on[g] & 2u)) break;
+      for (int j = 0; j < V; ++j) sum[j] += heads[w][j * 64 + lane];
+      if (!goes_on[w]) break;
     }
-    if (g < kGroups) {
+    if (w < kGradWaves) {
       write_grad<TG, V>(A, A.row_ids ? static_cast<int64_t>(rank) : static_cast<int64_t>(key), c, sum);
     } else {
 #pragma unroll
@@ -425,12 +424,12 @@ __global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedGradArgs A) {
     }
   }
   // the run that began before the block
-  if (group == 0 && keys[0] < none && keys[0] == before) {
+  if (wave == 0 && began_before) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) sum[j] = heads[0][j * LANES + lane];
-    for (int g = 0; g + 1 < kGroups && (goes_on[g] & 2u); ++g) {
+    for (int j = 0; j < V; ++j) sum[j] = heads[0][j * 64 + lane];
+    for (int w = 0; w + 1 < kGradWaves && goes_on[w]; ++w) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) sum[j] += heads[g + 1][j * LANES + lane];
+      for (int j = 0; j < V; ++j) sum[j] += heads[w + 1][j * 64 + lane];
     }
 #pragma unroll
     for (int j = 0; j < V; ++j) part[j] = sum[j];
@@ -448,39 +447,30 @@ __device__ __forceinline__ int64_t rank_of_row(const EmbedGradArgs& A, uint32_t 
   return lo;
 }
 
-// Runs that cross blocks of k_embed_sums (of kGroups * kGradTokens tokens): one that ends within kJoinShort blocks behind the one it begins in by a
-// group of lanes, a longer one by a block of its own, which is the one of the first multiple of kJoinShort behind it.
+// Runs that cross blocks of k_embed_sums: one that ends within kJoinShort blocks behind the one it begins in by a wave, a
+// longer one by a block of its own, which is the one of the first multiple of kJoinShort behind it.
 constexpr int kJoinThreads = 1024;
+constexpr int kJoinWaves = kJoinThreads / 64;
 constexpr int kJoinShort = 16;
-template <typename TG, int V, int LANES>
+template <typename TG, int V>
 __global__ void __launch_bounds__(kJoinThreads) k_embed_join(EmbedGradArgs A, uint32_t short_blocks) {
-  constexpr int kGroups = kJoinThreads / LANES;
-  constexpr int64_t kTokens = kThreads / LANES * kGradTokens;
-  __shared__ float lds[kGroups][LANES * V];
+  __shared__ float lds[kJoinWaves][64 * V];
   const int64_t n = count_of(A.num, A.max_ids);
-  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
-  const int index = static_cast<int>(blockIdx.y) * LANES + lane;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int index = static_cast<int>(blockIdx.y) * 64 + lane;
   const Columns<V> c(index, A.dim);
   const int64_t width = A.part_width;
   const float* part = A.part + static_cast<int64_t>(index) * V;
   float sum[V] = {};
   if (blockIdx.x < short_blocks) {
-    const int64_t b = static_cast<int64_t>(blockIdx.x) * kGroups + group, p1 = (b + 1) * kTokens;
-    uint32_t key = static_cast<uint32_t>(A.num_rows);
-    bool begins = false;
-    int blocks = 0;  // behind b that have some of the run
-    if (p1 < n) {
-      key = A.sorted[p1 - 1].x;
-      begins = key < A.num_rows && (b == 0 || A.sorted[b * kTokens - 1].x != key);
-      const int64_t p = p1 + (lane % kJoinShort) * kTokens;
-      const bool goes_on = lane < kJoinShort && p < n && A.sorted[p < n ? p : p1].x == key;
-      const uint64_t set = __ballot(goes_on) >> (threadIdx.x & 63 & ~(LANES - 1));
-      blocks = __popcll(set & ((1ull << kJoinShort) - 1));
-    }
-    const bool joins = begins && blocks > 0 && blocks < kJoinShort;
-    if (!joins) return;
-    int64_t row = key;
-    if (A.row_ids) row = rank_of_row(A, key);
+    const int64_t b = static_cast<int64_t>(blockIdx.x) * kJoinWaves + wave, p1 = (b + 1) * kBlockTokens;
+    if (p1 >= n) return;
+    const uint32_t key = A.sorted[p1 - 1].x;
+    if (key >= A.num_rows || (b > 0 && A.sorted[b * kBlockTokens - 1].x == key)) return;  // begins before the block
+    const int64_t p = p1 + lane * kBlockTokens;
+    const int blocks = __popcll(__ballot(lane < kJoinShort && p < n && A.sorted[p < n ? p : p1].x == key));  // behind b that have some of the run
+    if (blocks == 0 || blocks == kJoinShort) return;
+    const int64_t row = A.row_ids ? rank_of_row(A, key) : static_cast<int64_t>(key);
     if (c.dup == V) return;
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = part[(2 * b + 1) * width + j];
@@ -492,32 +482,31 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(EmbedGradArgs A, ui
     return;
   }
   const int64_t m = (static_cast<int64_t>(blockIdx.x - short_blocks) + 1) * kJoinShort;
-  if (m * kTokens >= n) return;
-  const uint32_t key = A.sorted[m * kTokens].x;
-  if (key >= A.num_rows || A.sorted[m * kTokens - 1].x != key) return;
-  const int64_t first = wave_sorted_bound(A.sorted, 0, m * kTokens, key), b = first / kTokens;
-  const int64_t last = (wave_sorted_bound(A.sorted, m * kTokens, n, key + 1) - 1) / kTokens;
+  if (m * kBlockTokens >= n) return;
+  const uint32_t key = A.sorted[m * kBlockTokens].x;
+  if (key >= A.num_rows || A.sorted[m * kBlockTokens - 1].x != key) return;
+  const int64_t b = wave_sorted_bound(A.sorted, 0, m * kBlockTokens, key) / kBlockTokens;
+  const int64_t last = (wave_sorted_bound(A.sorted, m * kBlockTokens, n, key + 1) - 1) / kBlockTokens;
   if (m - b > kJoinShort || last - b < kJoinShort) return;
-  int64_t row = key;
-  if (A.row_ids) row = rank_of_row(A, key);
+  const int64_t row = A.row_ids ? rank_of_row(A, key) : static_cast<int64_t>(key);
   if (c.dup < V) {
-    if (group == 0) {
+    if (wave == 0) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[j] = part[(2 * b + 1) * width + j];
     }
-#pragma unroll 4
-    for (int64_t q = b + 1 + group; q <= last; q += kGroups) {
+#pragma unroll 8
+    for (int64_t q = b + 1 + wave; q <= last; q += kJoinWaves) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[j] += part[2 * q * width + j];
     }
   }
 #pragma unroll
-  for (int j = 0; j < V; ++j) lds[group][j * LANES + lane] = sum[j];
+  for (int j = 0; j < V; ++j) lds[wave][j * 64 + lane] = sum[j];
   __syncthreads();
-  if (group != 0 || c.dup == V) return;
-  for (int g = 1; g < kGroups; ++g) {
+  if (wave != 0 || c.dup == V) return;
+  for (int w = 1; w < kJoinWaves; ++w) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) sum[j] += lds[g][j * LANES + lane];
+    for (int j = 0; j < V; ++j) sum[j] += lds[w][j * 64 + lane];
   }
   write_grad<TG, V>(A, row, c, sum);
 }

@@ -39,8 +39,7 @@ __global__ void __launch_bounds__(kThreads) k_layer_norm(NormArgs A) {
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const Columns<V> c(k * LANES + lane, A.dim);
-    Elems<T, V> e = {};
-    if (c.dup < V) e = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
+    const Elems<T, V> e = *reinterpret_cast<const Elems<T, V>*>(x + c.start);  // a column that there is not: the last ones again
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       v[k][j] = as_float(e.v[j]);
@@ -153,9 +152,9 @@ __global__ void __launch_bounds__(kThreads) k_layer_norm_grad(NormGradArgs A) {
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const Columns<V> c(k * LANES + lane, A.dim);
+    load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w[k]);
 #pragma unroll
-    for (int j = 0; j < V; ++j) w[k][j] = dw[k][j] = db[k][j] = 0.f;
-    if (c.dup < V) load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w[k]);
+    for (int j = 0; j < V; ++j) dw[k][j] = db[k][j] = 0.f;
   }
   for (int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES; row < n;
        row += static_cast<int64_t>(gridDim.x) * kGroups) {
@@ -167,11 +166,8 @@ __global__ void __launch_bounds__(kThreads) k_layer_norm_grad(NormGradArgs A) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const Columns<V> c(k * LANES + lane, A.dim);
-      Elems<T, V> ex = {}, ey = {};
-      if (c.dup < V) {
-        ex = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
-        ey = *reinterpret_cast<const Elems<T, V>*>(dy + c.start);
-      }
+      const Elems<T, V> ex = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
+      const Elems<T, V> ey = *reinterpret_cast<const Elems<T, V>*>(dy + c.start);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         h[k][j] = (as_float(ex.v[j]) - m) * r;

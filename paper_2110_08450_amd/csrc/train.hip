@@ -47,38 +47,25 @@ void launch_embedding(const EmbedArgs& A, unsigned blocks, bool vectors, hipStre
   else k_embedding<TI, TO, 1><<<blocks, kThreads, 0, st>>>(A);
 }
 
-// How the sums of a gradient are dealt: V columns a lane, LANES lanes a group, kThreads / LANES groups a block.
+// Blocks of k_embed_sums for the tokens, tiles of 64 * V columns, and floats of a row of partial sums.
 struct GradShape {
-  int vector, lanes;
-  int64_t tokens, blocks, tiles, width;  // tokens of a block, blocks, tiles of columns, floats of a row of partial sums
+  int64_t blocks, tiles, width;
 };
-GradShape grad_shape(int64_t max_ids, int32_t dim, int vector) {
-  GradShape S;
-  S.vector = dim < vector ? 1 : vector;
-  const int64_t vectors = ceil_div(dim, S.vector);
-  S.lanes = vectors <= 16 ? 16 : vectors <= 32 ? 32 : 64;
-  S.tokens = kThreads / S.lanes * kGradTokens;
-  S.blocks = ceil_div(max_ids, S.tokens);
-  S.tiles = ceil_div(vectors, S.lanes);
-  S.width = vectors * S.vector;
-  return S;
+GradShape grad_shape(int64_t max_ids, int32_t dim) {
+  const int V = grad_columns(dim);
+  const int64_t vectors = ceil_div(dim, V);
+  return {ceil_div(max_ids, kBlockTokens), ceil_div(vectors, 64), vectors * V};
 }
-// 16 bytes of the wider of the two types: whole vectors are read and written, neither wider than an instruction.
-inline int grad_vector(int32_t dy_dtype, int32_t grad_dtype) { return type_bytes(dy_dtype) == 2 && type_bytes(grad_dtype) == 2 ? 8 : 4; }
 
 struct EmbedScratch {
-  int64_t rec[2], hist, total, part, tile_runs, bytes;
+  int64_t rec[2], hist, total, part, tile_runs, block_runs, bytes;
   int64_t tiles, run_tiles;
 };
 EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
   EmbedScratch S;
   S.tiles = ceil_div(max_ids, kSortTile);
   S.run_tiles = ceil_div(max_ids, kRunTile);
-  int64_t part = 0;
-  for (const int v : {4, 8}) {
-    const GradShape G = grad_shape(max_ids, dim, v);
-    if (G.blocks * G.width > part) part = G.blocks * G.width;
-  }
+  const GradShape G = grad_shape(max_ids, dim);
   int64_t at = 0;
   const auto take = [&at](int64_t bytes) {
     const int64_t here = at;
@@ -89,8 +76,9 @@ EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
   S.rec[1] = take(8 * max_ids);
   S.hist = take(4 * kSortBins * S.tiles);
   S.total = take(4 * kSortBins);
-  S.part = take(4 * 2 * part);
+  S.part = take(4 * 2 * G.blocks * G.width);
   S.tile_runs = take(4 * S.run_tiles);
+  S.block_runs = take(4 * G.blocks);
   S.bytes = at;
   return S;
 }
@@ -111,30 +99,28 @@ const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* id
   return A.in;
 }
 
-template <typename TD, typename TG, int V, int LANES>
+template <typename TD, typename TG, int V>
 void launch_embed_sums(EmbedGradArgs A, const GradShape& G, bool clear, hipStream_t st) {
-  A.sum_blocks = static_cast<uint32_t>(G.blocks);
+  A.sum_blocks = G.blocks > 0 ? static_cast<uint32_t>(G.blocks) : 1u;  // without tokens there is one, which has no tile
+  A.tiles = G.blocks > 0 ? static_cast<uint32_t>(G.tiles) : 0u;
   // a block clears about 32 KiB, of at most a row a thread
   const int64_t rows = (32 << 10) / (A.dim * static_cast<int64_t>(sizeof(TG)));
-  A.clear_rows = static_cast<int32_t>(rows < 1 ? 1 : rows > kThreads ? kThreads : rows);
-  A.tiles = G.blocks > 0 ? static_cast<uint32_t>(G.tiles) : 0u;
-  if (G.blocks == 0) A.sum_blocks = 1;  // none of whose tiles there is
+  A.clear_rows = static_cast<int32_t>(rows < 1 ? 1 : rows > kGradThreads ? kGradThreads : rows);
   const int64_t blocks = G.blocks * G.tiles + (clear ? ceil_div(A.num_rows, A.clear_rows) : 0);
   if (blocks == 0) return;
-  k_embed_sums<TD, TG, V, LANES><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(A);
+  k_embed_sums<TD, TG, V><<<static_cast<unsigned>(blocks), kGradThreads, 0, st>>>(A);
   if (G.blocks < 2) return;
-  const uint32_t joins = static_cast<uint32_t>(ceil_div(G.blocks, kJoinThreads / LANES));
+  const uint32_t joins = static_cast<uint32_t>(ceil_div(G.blocks, kJoinWaves));
   const unsigned longs = static_cast<unsigned>((G.blocks - 1) / kJoinShort);
-  k_embed_join<TG, V, LANES><<<dim3(joins + longs, static_cast<unsigned>(G.tiles)), kJoinThreads, 0, st>>>(A, joins);
+  k_embed_join<TG, V><<<dim3(joins + longs, static_cast<unsigned>(G.tiles)), kJoinThreads, 0, st>>>(A, joins);
 }
 
 template <typename TD, typename TG>
 void launch_embed_grad(const EmbedGradArgs& A, const GradShape& G, bool clear, hipStream_t st) {
-  constexpr int V = sizeof(TD) == 2 && sizeof(TG) == 2 ? 8 : 4;
-  if (G.vector == 1) launch_embed_sums<TD, TG, 1, 16>(A, G, clear, st);
-  else if (G.lanes == 16) launch_embed_sums<TD, TG, V, 16>(A, G, clear, st);
-  else if (G.lanes == 32) launch_embed_sums<TD, TG, V, 32>(A, G, clear, st);
-  else launch_embed_sums<TD, TG, V, 64>(A, G, clear, st);
+  const int V = grad_columns(A.dim);
+  if (V == 1) launch_embed_sums<TD, TG, 1>(A, G, clear, st);
+  else if (V == 2) launch_embed_sums<TD, TG, 2>(A, G, clear, st);
+  else launch_embed_sums<TD, TG, 4>(A, G, clear, st);
 }
 
 int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids, int64_t max_ids, const void* d_dy, int64_t dy_stride,
@@ -151,7 +137,7 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
   if (max_ids == 0 && !rows_only && accumulate) return SMFG_OK;
   const EmbedScratch S = embed_scratch(max_ids, dim);
   if (max_ids > 0 && scratch_bytes < S.bytes) return SMFG_ERR_CAPACITY;
-  const GradShape G = grad_shape(max_ids, dim, grad_vector(dy_dtype, grad_dtype));
+  const GradShape G = grad_shape(max_ids, dim);
   uint8_t* scratch = static_cast<uint8_t*>(d_scratch);
   EmbedGradArgs A = {};
   A.num = d_num_ids;
@@ -169,6 +155,7 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
   A.row_ids = d_row_ids;
   A.num_unique = d_num_unique;
   A.tile_runs = reinterpret_cast<uint32_t*>(scratch + S.tile_runs);
+  A.block_runs = reinterpret_cast<uint32_t*>(scratch + S.block_runs);
   A.run_tiles = S.run_tiles;
   if (max_ids > 0) A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, st);
   if (rows_only) {
