@@ -68,110 +68,231 @@ __global__ void __launch_bounds__(kThreads) k_embedding(EmbedArgs A) {
 
 // ---- ids sorted by row -------------------------------------------------------------------------
 //
-// A stable sort by digits of 8 bits from the lowest on, three launches a digit: count (per tile of kSortTile tokens), scan
-// (a block per digit over the tiles, then every tile adds the totals of the smaller digits), scatter.  The order of equal ids is that
-// of their tokens, so that a row's sum has one order, whatever the schedule.
-constexpr int kSortTile = 4096;
-constexpr int kSortTurns = kSortTile / kThreads;
-constexpr int kSortBits = 8;
-constexpr int kSortBins = 1 << kSortBits;
-
+// (row, token), stable: equal ids stay in the order of their tokens, so that a row's sum has one order, whatever the schedule.
+//
+// Up to kSmallSort ids: every token counts the ids that belong before its own, in one launch.  More: digits of at most kSortBits
+// bits from the lowest on, a launch that counts the digits of every tile and one that scatters.  Up to kSortColumns tiles the block
+// that scatters adds up the counts of all tiles itself (118 tiles of 4096: 1.5 us instead of the 3 to 5 of another launch); more
+// of them are scanned by a launch between the two.
 struct SortArgs {
   const void* ids;      // first digit: the ids
   int32_t id_bytes;
-  int32_t shift;
+  int32_t shift, bits;
   int64_t num_rows;
   const int64_t* num;
   int64_t max_ids;
   const uint2* in;      // other digits: (row, token)
   uint2* out;
-  uint32_t* hist;       // [bins][tiles]
-  uint32_t* total;      // [bins]
+  uint16_t* hist;       // [tiles][bins]
+  uint32_t* starts;     // [tiles][bins] where a tile's records of a digit begin, if scanned
   int32_t tiles;
 };
+
+constexpr int kSmallSort = 8192;
+constexpr int kSmallTokens = 64;   // tokens of a block of k_sort_small
 
 __device__ __forceinline__ uint2 sort_record(const SortArgs& A, int64_t i) {
   return A.in ? A.in[i] : make_uint2(row_of_id(A.ids, A.id_bytes, i, A.num_rows), static_cast<uint32_t>(i));
 }
 
-static __global__ void __launch_bounds__(kThreads) k_sort_count(SortArgs A) {
+// A lane has a token, a wave a share of the ids to compare with: four at a time, the same for all lanes.  Two instructions a
+// comparison: of equal ids those before the block's tokens count, those behind them do not, and only among its own it depends on the lane.
+constexpr int kSmallThreads = 512;
+template <typename Counts>
+__device__ __forceinline__ uint32_t count_keys(const uint4* keys, int from, int to, int wave, Counts counts) {
+  uint32_t c = 0;
+#pragma unroll 4
+  for (int q = from + wave; q < to; q += kSmallThreads / 64) {
+    const uint4 k = keys[q];
+    c += counts(k.x, 4 * q) ? 1u : 0u;
+    c += counts(k.y, 4 * q + 1) ? 1u : 0u;
+    c += counts(k.z, 4 * q + 2) ? 1u : 0u;
+    c += counts(k.w, 4 * q + 3) ? 1u : 0u;
+  }
+  return c;
+}
+static __global__ void __launch_bounds__(kSmallThreads) k_sort_small(SortArgs A) {
+  constexpr int kWaves = kSmallThreads / 64;
+  __shared__ uint4 keys[kSmallSort / 4];
+  __shared__ uint32_t smaller[kWaves][64];
+  const int n = static_cast<int>(count_of(A.num, A.max_ids));
+  const int i0 = static_cast<int>(blockIdx.x) * kSmallTokens;
+  if (i0 >= n) return;
+  uint32_t* flat = reinterpret_cast<uint32_t*>(keys);
+  const int padded = (n + kSmallTokens - 1) / kSmallTokens * kSmallTokens;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < padded; i += kSmallThreads) {
+    const uint32_t key = row_of_id(A.ids, A.id_bytes, i < A.max_ids ? i : 0, A.num_rows);
+    flat[i] = i < n ? key : ~0u;
+  }
+  __syncthreads();
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = i0 + lane;
+  const uint32_t key = flat[i];
+  uint32_t count = count_keys(keys, 0, i0 / 4, wave, [&](uint32_t k, int) { return k <= key; });
+  count += count_keys(keys, i0 / 4, (i0 + kSmallTokens) / 4, wave, [&](uint32_t k, int j) { return k < key || (k == key && j < i); });
+  count += count_keys(keys, (i0 + kSmallTokens) / 4, padded / 4, wave, [&](uint32_t k, int) { return k < key; });
+  smaller[wave][lane] = count;
+  __syncthreads();
+  if (wave != 0 || i >= n) return;
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) count += smaller[w][lane];
+  A.out[count] = make_uint2(key, static_cast<uint32_t>(i));
+}
+
+constexpr int kSortThreads = 1024;
+constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kSortTurns = 4;
+constexpr int kSortTile = kSortThreads * kSortTurns;
+constexpr int kSortBits = 9;
+constexpr int kSortBins = 1 << kSortBits;
+constexpr int kSortColumns = 256;
+
+static __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs A) {
   __shared__ uint32_t count[kSortBins];
   const int64_t n = count_of(A.num, A.max_ids);
-  count[threadIdx.x] = 0;
-  __syncthreads();
+  const int bins = 1 << A.bits;
   const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile;
+  uint32_t digit[kSortTurns];
+#pragma unroll
   for (int k = 0; k < kSortTurns; ++k) {
-    const int64_t i = base + k * kThreads + threadIdx.x;
-    if (i < n) atomicAdd(&count[(sort_record(A, i).x >> A.shift) & (kSortBins - 1)], 1u);
+    const int64_t i = base + k * kSortThreads + threadIdx.x;
+    digit[k] = (sort_record(A, i < A.max_ids ? i : A.max_ids - 1).x >> A.shift) & (bins - 1);
+  }
+  if (threadIdx.x < kSortBins) count[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kSortTurns; ++k)
+    if (base + k * kSortThreads + threadIdx.x < n) atomicAdd(&count[digit[k]], 1u);
+  __syncthreads();
+  if (static_cast<int>(threadIdx.x) < bins)
+    A.hist[static_cast<int64_t>(blockIdx.x) * bins + threadIdx.x] = static_cast<uint16_t>(count[threadIdx.x]);
+}
+
+// Where the records of every tile and digit begin: a block has 64 digits, its waves take turns of tiles.  Two passes over the counts: totals of
+// the digits (every block those of all digits), then the running sums.
+static __global__ void __launch_bounds__(kSortThreads) k_sort_scan(SortArgs A) {
+  __shared__ uint32_t lds[kSortWaves], sums[kSortWaves][64], begin[kSortBins];
+  const int bins = 1 << A.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t all = 0;
+  for (int d0 = 0; d0 < bins; d0 += 64) {
+    uint32_t s = 0;
+    const int d = d0 + lane;
+    for (int64_t t = wave; t < A.tiles; t += kSortWaves) s += d < bins ? A.hist[t * bins + d] : 0u;
+    __syncthreads();
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && d < bins) {
+      s = 0;
+      for (int w = 0; w < kSortWaves; ++w) s += sums[w][lane];
+      begin[d] = s;
+    }
   }
   __syncthreads();
-  A.hist[static_cast<int64_t>(threadIdx.x) * A.tiles + blockIdx.x] = count[threadIdx.x];
-}
-
-static __global__ void __launch_bounds__(kThreads) k_sort_scan(SortArgs A) {
-  __shared__ uint32_t lds[kThreads / 64];
-  uint32_t* h = A.hist + static_cast<int64_t>(blockIdx.x) * A.tiles;
-  uint32_t before = 0;
-  for (int t0 = 0; t0 < A.tiles; t0 += kThreads) {
-    const int t = t0 + threadIdx.x;
-    const uint32_t c = t < A.tiles ? h[t] : 0u;
-    uint32_t sum;
-    const uint32_t ex = block_exscan(c, lds, sum);
-    if (t < A.tiles) h[t] = before + ex;
-    before += sum;
+  const uint32_t ex = block_exscan<kSortThreads>(static_cast<int>(threadIdx.x) < bins ? begin[threadIdx.x] : 0u, lds, all);
+  __syncthreads();
+  if (static_cast<int>(threadIdx.x) < bins) begin[threadIdx.x] = ex;
+  __syncthreads();
+  const int d = static_cast<int>(blockIdx.x) * 64 + lane;
+  uint32_t at = d < bins ? begin[d] : 0u;
+  for (int64_t t0 = 0; t0 < A.tiles; t0 += kSortWaves) {
+    const int64_t t = t0 + wave;
+    const uint32_t c = t < A.tiles && d < bins ? A.hist[t * bins + d] : 0u;
+    __syncthreads();
+    sums[wave][lane] = c;
+    __syncthreads();
+    uint32_t here = at;
+    for (int w = 0; w < kSortWaves; ++w) {
+      if (w < wave) here += sums[w][lane];
+      at += sums[w][lane];
+    }
+    if (t < A.tiles && d < bins) A.starts[t * bins + d] = here;
   }
-  if (threadIdx.x == 0) A.total[blockIdx.x] = before;
 }
 
-static __global__ void __launch_bounds__(kThreads) k_sort_scatter(SortArgs A) {
-  constexpr int kWaves = kThreads / 64;
-  __shared__ uint32_t next[kWaves][kSortBins];  // records of a wave so far, later where its next record goes
-  __shared__ uint32_t lds[kWaves];
-  const int64_t n = count_of(A.num, A.max_ids);
+static __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs A) {
+  __shared__ uint32_t next[kSortWaves][kSortBins];  // records of a wave so far, later where its next record goes
+  __shared__ uint32_t sums[kSortWaves][2 * kSortBins];
+  __shared__ uint32_t lds[kSortWaves];
+  const int bins = 1 << A.bits, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile;
-  if (base >= n) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int q = 0; q < kWaves; ++q) next[q][threadIdx.x] = 0;
-  __syncthreads();
-  // a wave has consecutive records, 64 a turn: its rank among equal digits of the wave
+  // a wave has consecutive records, 64 a turn
   uint2 rec[kSortTurns];
+#pragma unroll
+  for (int k = 0; k < kSortTurns; ++k) {
+    const int64_t i = base + (wave * kSortTurns + k) * 64 + lane;
+    rec[k] = sort_record(A, i < A.max_ids ? i : A.max_ids - 1);
+  }
+  for (int i = threadIdx.x; i < kSortWaves * kSortBins; i += kSortThreads) next[0][i] = 0;
+  const int64_t n = count_of(A.num, A.max_ids);
+  if (base >= n) return;
+  // where the tile's records of a digit begin: behind all smaller digits, and those of the tiles before; in pairs of digits, the tiles
+  // dealt to groups of threads
+  uint32_t at = 0;
+  const int pairs = bins / 2, groups = kSortThreads / pairs < kSortWaves ? kSortThreads / pairs : kSortWaves;
+  if (!A.starts) {
+    const int pair = static_cast<int>(threadIdx.x) % pairs, group = static_cast<int>(threadIdx.x) / pairs;
+    if (group < groups) {
+      uint32_t all0 = 0, all1 = 0, before0 = 0, before1 = 0;
+      const int mine = static_cast<int>(blockIdx.x);
+#pragma unroll 8
+      for (int t = group; t < A.tiles; t += groups) {
+        const uint32_t c = reinterpret_cast<const uint32_t*>(A.hist)[t * pairs + pair];
+        all0 += c & 0xFFFFu;
+        all1 += c >> 16;
+        before0 += t < mine ? c & 0xFFFFu : 0u;
+        before1 += t < mine ? c >> 16 : 0u;
+      }
+      sums[group][2 * pair] = all0;
+      sums[group][2 * pair + 1] = all1;
+      sums[group][kSortBins + 2 * pair] = before0;
+      sums[group][kSortBins + 2 * pair + 1] = before1;
+    }
+  } else if (static_cast<int>(threadIdx.x) < bins) {
+    at = A.starts[static_cast<int64_t>(blockIdx.x) * bins + threadIdx.x];
+  }
+  __syncthreads();
+  // its rank among equal digits of the wave
   uint32_t rank[kSortTurns];
 #pragma unroll
   for (int k = 0; k < kSortTurns; ++k) {
-    const int64_t i = base + (wave * kSortTurns + k) * 64 + lane;
-    const bool live = i < n;
-    rec[k] = live ? sort_record(A, i) : make_uint2(0, 0);
-    const uint32_t digit = (rec[k].x >> A.shift) & (kSortBins - 1);
-    uint64_t same = __ballot(live);
+    const bool live = base + (wave * kSortTurns + k) * 64 + lane < n;
+    const uint32_t digit = (rec[k].x >> A.shift) & (bins - 1);
+    const uint64_t all = __ballot(live);
+    uint32_t same0 = static_cast<uint32_t>(all), same1 = static_cast<uint32_t>(all >> 32);
 #pragma unroll
-    for (int b = 0; b < kSortBits; ++b) {
-      const uint64_t set = __ballot((digit >> b) & 1u);
-      same &= (digit >> b) & 1u ? set : ~set;
+    for (int b = 0; b < kSortBits; ++b) {  // a bit that no digit has changes nothing
+      const uint64_t set = __ballot(digit & (1u << b));
+      const uint32_t mine = static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(digit), b, 1));
+      same0 &= ~(static_cast<uint32_t>(set) ^ mine);
+      same1 &= ~(static_cast<uint32_t>(set >> 32) ^ mine);
     }
-    const uint32_t below = __popcll(same & ((1ull << lane) - 1));
-    rank[k] = 0;
-    if (live) rank[k] = next[wave][digit] + below;  // every lane reads before the first of each digit adds
+    const uint32_t below = __builtin_amdgcn_mbcnt_hi(same1, __builtin_amdgcn_mbcnt_lo(same0, 0));
+    uint32_t* slot = &next[wave][digit];
+    rank[k] = *slot + below;  // every lane reads before the first of each digit adds
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (live && below == 0) next[wave][digit] += __popcll(same);
+    if (live && below == 0) *slot = rank[k] + __popc(same0) + __popc(same1);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  uint32_t all = 0;
+  if (!A.starts && static_cast<int>(threadIdx.x) < bins)
+    for (int g = 0; g < groups; ++g) {
+      all += sums[g][threadIdx.x];
+      at += sums[g][kSortBins + threadIdx.x];
+    }
+  uint32_t total;
+  at += block_exscan<kSortThreads>(all, lds, total);
+  if (static_cast<int>(threadIdx.x) < bins) {
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = next[w][threadIdx.x];
+      next[w][threadIdx.x] = at;
+      at += c;
+    }
   }
   __syncthreads();
-  // where the tile's records of each digit begin: behind all smaller digits, and those of the tiles before
-  uint32_t all;
-  const uint32_t digits_before = block_exscan(A.total[threadIdx.x], lds, all);
-  uint32_t at = digits_before + A.hist[static_cast<int64_t>(threadIdx.x) * A.tiles + blockIdx.x];
 #pragma unroll
-  for (int q = 0; q < kWaves; ++q) {
-    const uint32_t c = next[q][threadIdx.x];
-    next[q][threadIdx.x] = at;
-    at += c;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < kSortTurns; ++k) {
-    const int64_t i = base + (wave * kSortTurns + k) * 64 + lane;
-    if (i < n) A.out[next[wave][(rec[k].x >> A.shift) & (kSortBins - 1)] + rank[k]] = rec[k];
-  }
+  for (int k = 0; k < kSortTurns; ++k)
+    if (base + (wave * kSortTurns + k) * 64 + lane < n) A.out[next[wave][(rec[k].x >> A.shift) & (bins - 1)] + rank[k]] = rec[k];
 }
 
 // ---- sums over runs of equal rows --------------------------------------------------------------
@@ -213,6 +334,7 @@ struct EmbedGradArgs {
   int64_t* num_unique;
   uint32_t* tile_runs;     // runs that begin in a tile of kRunTile sorted tokens
   uint32_t* block_runs;    // runs that begin in a block's tile before it
+  uint32_t* tail_rank;     // rank of the run that begins in a block and goes on behind it
   int64_t run_tiles;
 };
 
@@ -421,6 +543,7 @@ __global__ void __launch_bounds__(kGradThreads) k_embed_sums(EmbedGradArgs A) {
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j) part[A.part_width + j] = sum[j];
+      if (A.row_ids && index == 0) A.tail_rank[block] = rank;
     }
   }
   // the run that began before the block
@@ -434,17 +557,6 @@ __global__ void __launch_bounds__(kGradThreads) k_embed_sums(EmbedGradArgs A) {
 #pragma unroll
     for (int j = 0; j < V; ++j) part[j] = sum[j];
   }
-}
-
-// Place of a touched row among their ascending ids.
-__device__ __forceinline__ int64_t rank_of_row(const EmbedGradArgs& A, uint32_t row) {
-  int64_t lo = 0, hi = *A.num_unique;
-  while (lo < hi) {
-    const int64_t mid = lo + (hi - lo) / 2;
-    if (static_cast<uint32_t>(A.row_ids[mid]) < row) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo;
 }
 
 // Runs that cross blocks of k_embed_sums: one that ends within kJoinShort blocks behind the one it begins in by a wave, a
@@ -470,7 +582,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(EmbedGradArgs A, ui
     const int64_t p = p1 + lane * kBlockTokens;
     const int blocks = __popcll(__ballot(lane < kJoinShort && p < n && A.sorted[p < n ? p : p1].x == key));  // behind b that have some of the run
     if (blocks == 0 || blocks == kJoinShort) return;
-    const int64_t row = A.row_ids ? rank_of_row(A, key) : static_cast<int64_t>(key);
+    const int64_t row = A.row_ids ? static_cast<int64_t>(A.tail_rank[b]) : static_cast<int64_t>(key);
     if (c.dup == V) return;
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = part[(2 * b + 1) * width + j];
@@ -485,10 +597,19 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(EmbedGradArgs A, ui
   if (m * kBlockTokens >= n) return;
   const uint32_t key = A.sorted[m * kBlockTokens].x;
   if (key >= A.num_rows || A.sorted[m * kBlockTokens - 1].x != key) return;
-  const int64_t b = wave_sorted_bound(A.sorted, 0, m * kBlockTokens, key) / kBlockTokens;
-  const int64_t last = (wave_sorted_bound(A.sorted, m * kBlockTokens, n, key + 1) - 1) / kBlockTokens;
+  // the block it begins in: as many before m as end with the run; the last block that begins with it
+  const int64_t p = (m - lane) * kBlockTokens - 1;
+  const int64_t b = m - __popcll(__ballot(lane <= kJoinShort && p >= 0 && A.sorted[p < 0 ? 0 : p].x == key));
+  int64_t last = m;
+  for (int64_t step = 1, hi = (n - 1) / kBlockTokens; last < hi;) {  // it is in [last, hi]
+    step = (hi - last + 63) / 64;
+    const int64_t q = last + (lane + 1) * step;
+    const int more = __popcll(__ballot(q <= hi && A.sorted[(q <= hi ? q : hi) * kBlockTokens].x == key));
+    last += more * step;
+    hi = last + step - 1 < hi ? last + step - 1 : hi;
+  }
   if (m - b > kJoinShort || last - b < kJoinShort) return;
-  const int64_t row = A.row_ids ? rank_of_row(A, key) : static_cast<int64_t>(key);
+  const int64_t row = A.row_ids ? static_cast<int64_t>(A.tail_rank[b]) : static_cast<int64_t>(key);
   if (c.dup < V) {
     if (wave == 0) {
 #pragma unroll

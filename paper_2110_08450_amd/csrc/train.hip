@@ -58,7 +58,7 @@ GradShape grad_shape(int64_t max_ids, int32_t dim) {
 }
 
 struct EmbedScratch {
-  int64_t rec[2], hist, total, part, tile_runs, block_runs, bytes;
+  int64_t rec[2], hist, starts, part, tile_runs, block_runs, tail_rank, bytes;
   int64_t tiles, run_tiles;
 };
 EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
@@ -74,26 +74,42 @@ EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
   };
   S.rec[0] = take(8 * max_ids);
   S.rec[1] = take(8 * max_ids);
-  S.hist = take(4 * kSortBins * S.tiles);
-  S.total = take(4 * kSortBins);
+  S.hist = take(max_ids > kSmallSort ? 2 * kSortBins * S.tiles : 0);
+  S.starts = take(S.tiles > kSortColumns ? 4 * kSortBins * S.tiles : 0);
   S.part = take(4 * 2 * G.blocks * G.width);
   S.tile_runs = take(4 * S.run_tiles);
   S.block_runs = take(4 * G.blocks);
+  S.tail_rank = take(4 * G.blocks);
   S.bytes = at;
   return S;
 }
 
-// (row, token) of the call's ids, sorted by row.
+// (row, token) of the call's ids, sorted by row.  num_rows itself, which stands for no row, is a key as well.
 const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* ids, int32_t id_bytes, const int64_t* num, int64_t max_ids,
                          int64_t num_rows, hipStream_t st) {
-  SortArgs A = {ids, id_bytes, 0, num_rows, num, max_ids, nullptr, nullptr, reinterpret_cast<uint32_t*>(scratch + S.hist),
-                reinterpret_cast<uint32_t*>(scratch + S.total), static_cast<int32_t>(S.tiles)};
-  int b = 0;
-  for (; A.shift == 0 || num_rows >> A.shift != 0; A.shift += kSortBits, b ^= 1) {
-    A.out = reinterpret_cast<uint2*>(scratch + S.rec[b]);
-    k_sort_count<<<static_cast<unsigned>(S.tiles), kThreads, 0, st>>>(A);
-    k_sort_scan<<<kSortBins, kThreads, 0, st>>>(A);
-    k_sort_scatter<<<static_cast<unsigned>(S.tiles), kThreads, 0, st>>>(A);
+  SortArgs A = {};
+  A.ids = ids;
+  A.id_bytes = id_bytes;
+  A.num_rows = num_rows;
+  A.num = num;
+  A.max_ids = max_ids;
+  A.hist = reinterpret_cast<uint16_t*>(scratch + S.hist);
+  A.tiles = static_cast<int32_t>(S.tiles);
+  if (S.tiles > kSortColumns) A.starts = reinterpret_cast<uint32_t*>(scratch + S.starts);
+  A.out = reinterpret_cast<uint2*>(scratch + S.rec[0]);
+  if (max_ids <= kSmallSort) {
+    k_sort_small<<<static_cast<unsigned>(ceil_div(max_ids, kSmallTokens)), kSmallThreads, 0, st>>>(A);
+    return A.out;
+  }
+  int key_bits = 0;
+  while (num_rows >> key_bits != 0) ++key_bits;
+  const int passes = (key_bits + kSortBits - 1) / kSortBits;
+  A.bits = (key_bits + passes - 1) / passes;
+  for (int p = 0; p < passes; ++p, A.shift += A.bits) {
+    A.out = reinterpret_cast<uint2*>(scratch + S.rec[p & 1]);
+    k_sort_count<<<static_cast<unsigned>(S.tiles), kSortThreads, 0, st>>>(A);
+    if (A.starts) k_sort_scan<<<static_cast<unsigned>(ceil_div(1 << A.bits, 64)), kSortThreads, 0, st>>>(A);
+    k_sort_scatter<<<static_cast<unsigned>(S.tiles), kSortThreads, 0, st>>>(A);
     A.in = A.out;
   }
   return A.in;
@@ -156,6 +172,7 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
   A.num_unique = d_num_unique;
   A.tile_runs = reinterpret_cast<uint32_t*>(scratch + S.tile_runs);
   A.block_runs = reinterpret_cast<uint32_t*>(scratch + S.block_runs);
+  A.tail_rank = reinterpret_cast<uint32_t*>(scratch + S.tail_rank);
   A.run_tiles = S.run_tiles;
   if (max_ids > 0) A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, st);
   if (rows_only) {

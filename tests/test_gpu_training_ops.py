@@ -101,11 +101,16 @@ def ids_of(kind, n, rows, seed):
 
 def sums_of(ids, dy, rows, scale):
     """Per row of the table: sums, sums of magnitudes and numbers of its tokens, in 64 bits."""
-    ok = (ids >= 0) & (ids < rows)
-    i, d = ids[ok].long(), dy[ok].double()
-    out = torch.zeros((rows, dy.shape[1]), dtype=torch.float64, device=DEV)
-    mag = torch.zeros_like(out)
-    return (out.index_add_(0, i, d) * scale, mag.index_add_(0, i, d.abs()) * abs(scale), torch.bincount(i, minlength=rows))
+    ids, dy = ids.cpu().numpy().astype(np.int64), dy.double().cpu().numpy()
+    live = np.nonzero((ids >= 0) & (ids < rows))[0]
+    live = live[np.argsort(ids[live], kind="stable")]
+    k = np.bincount(ids[live], minlength=rows)
+    out, mag = np.zeros((2, rows, dy.shape[1]))
+    if live.size:
+        touched, at = np.nonzero(k)[0], np.concatenate([[0], np.cumsum(k[k > 0])[:-1]])
+        out[touched] = np.add.reduceat(dy[live], at, axis=0) * scale
+        mag[touched] = np.add.reduceat(np.abs(dy[live]), at, axis=0) * abs(scale)
+    return [torch.from_numpy(a).to(DEV) for a in (out, mag, k)]
 
 
 GRADS = [(1, 0, 1, 1, F32, F32, "uniform", 0), (5, 3, 9, 3, F16, F32, "uniform", 1), (64, 0, 300, 7, BF16, BF16, "mixed", 0),
@@ -114,7 +119,8 @@ GRADS = [(1, 0, 1, 1, F32, F32, "uniform", 0), (5, 3, 9, 3, F16, F32, "uniform",
          (20_000, 1, 3, 256, F16, F32, "uniform", 0), (3000, 0, 50, 1025, BF16, F32, "mixed", 1), (2500, 100, 2_000_000, 64, F16, F16, "uniform", 0),
          (700, 4, 17, 4096, F32, F32, "mixed", 0), (300, 0, 5, 8199, F16, F32, "same", 0), (5000, 0, 999, 128, BF16, BF16, "outside", 0),
          (0, 700, 40, 16, F32, F32, "uniform", 0), (150_000, 0, 4096, 16, F32, F32, "mixed", 0), (260_000, 1, 100, 33, F16, F32, "same", 0),
-         (8192, 0, 16_777_217, 8, F32, F32, "uniform", 0)]
+         (8192, 0, 16_777_217, 8, F32, F32, "uniform", 0), (4100, 3000, 130_000, 12, F16, F32, "backwards", 0),
+         (1_300_000, 5000, 700_000, 4, F32, F32, "mixed", 0), (1_050_000, 0, 3, 2, F16, F32, "uniform", 0)]
 
 
 @pytest.mark.parametrize("n,spare,rows,dim,dtype,gtype,kind,pad", GRADS)
