@@ -140,14 +140,15 @@ struct NormGradArgs {
 };
 
 // As k_layer_norm, a block striding over rows: a lane's columns are the same in each of them, so the sums for dw and db stay in
-// its registers until the block is done, and leave it once, as a slice of `part`.
+// its registers until the block is done, and leave it once, as a slice of `part`.  A row is asked for while the one before is worked on.
 template <typename T, int V, int NV, int LANES>
 __global__ void __launch_bounds__(kThreads) k_layer_norm_grad(NormGradArgs A) {
-  __shared__ float lds[kThreads / 64];
+  __shared__ float lds[2][2][kThreads / 64];
   constexpr int kGroups = kThreads / LANES;
   const int lane = threadIdx.x % LANES;
-  const int64_t n = count_of(A.num, A.max_rows);
+  const int64_t n = count_of(A.num, A.max_rows), step = static_cast<int64_t>(gridDim.x) * kGroups;
   const float inv = 1.f / static_cast<float>(A.dim);
+  const bool ragged = A.dim % V != 0;
   float w[NV][V], dw[NV][V], db[NV][V];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
@@ -156,31 +157,66 @@ __global__ void __launch_bounds__(kThreads) k_layer_norm_grad(NormGradArgs A) {
 #pragma unroll
     for (int j = 0; j < V; ++j) dw[k][j] = db[k][j] = 0.f;
   }
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES; row < n;
-       row += static_cast<int64_t>(gridDim.x) * kGroups) {
-    const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
-    const T* dy = static_cast<const T*>(A.dy) + row * A.dy_stride;
-    const float m = A.mean[row], r = A.rstd[row];
-    float h[NV][V], g[NV][V];
-    float s1 = 0.f, s2 = 0.f;
+  const T* const x = static_cast<const T*>(A.x);
+  const T* const dy = static_cast<const T*>(A.dy);
+  Elems<T, V> ex[NV], ey[NV];
+  float m = 0.f, r = 0.f;
+  const auto load = [&](int64_t row) {
+    m = A.mean[row];
+    r = A.rstd[row];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const Columns<V> c(k * LANES + lane, A.dim);
-      const Elems<T, V> ex = *reinterpret_cast<const Elems<T, V>*>(x + c.start);
-      const Elems<T, V> ey = *reinterpret_cast<const Elems<T, V>*>(dy + c.start);
+      ex[k] = *reinterpret_cast<const Elems<T, V>*>(x + row * A.x_stride + c.start);
+      ey[k] = *reinterpret_cast<const Elems<T, V>*>(dy + row * A.dy_stride + c.start);
+    }
+  };
+  int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES;
+  if (row < n) load(row);
+  for (int turn = 0; row < n; row += step, turn ^= 1) {
+    float h[NV][V], g[NV][V];
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const Columns<V> c(k * LANES + lane, A.dim);
+      float s1 = 0.f, s2 = 0.f;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        h[k][j] = (as_float(ex.v[j]) - m) * r;
-        const float d = as_float(ey.v[j]);
+        h[k][j] = (as_float(ex[k].v[j]) - m) * r;
+        const float d = as_float(ey[k].v[j]);
         dw[k][j] += d * h[k][j];
         db[k][j] += d;
         g[k][j] = d * w[k][j];
-        s1 += j >= c.dup ? g[k][j] : 0.f;
-        s2 += j >= c.dup ? g[k][j] * h[k][j] : 0.f;
+        if (ragged && j < c.dup) continue;
+        s1 += g[k][j];
+        s2 += g[k][j] * h[k][j];
+      }
+      s[0] += c.dup < V ? s1 : 0.f;
+      s[1] += c.dup < V ? s2 : 0.f;
+    }
+    const float scale = r;
+    if (row + step < n) load(row + step);
+    if (!A.dx) continue;
+    // both sums at once; the array of the turn before is still being read
+#pragma unroll
+    for (int o = 1; o < (LANES < 64 ? LANES : 64); o <<= 1) {
+      s[0] += __shfl_xor(s[0], o, 64);
+      s[1] += __shfl_xor(s[1], o, 64);
+    }
+    if constexpr (LANES > 64) {
+      if ((threadIdx.x & 63) == 0) {
+        lds[turn][0][threadIdx.x >> 6] = s[0];
+        lds[turn][1][threadIdx.x >> 6] = s[1];
+      }
+      __syncthreads();
+      s[0] = s[1] = 0.f;
+#pragma unroll
+      for (int q = 0; q < LANES / 64; ++q) {
+        s[0] += lds[turn][0][q];
+        s[1] += lds[turn][1][q];
       }
     }
-    if (!A.dx) continue;
-    const float c1 = group_sum<LANES>(s1, lds) * inv, c2 = group_sum<LANES>(s2, lds) * inv;
+    const float c1 = s[0] * inv, c2 = s[1] * inv;
     T* dx = static_cast<T*>(A.dx) + row * A.dx_stride;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -188,7 +224,7 @@ __global__ void __launch_bounds__(kThreads) k_layer_norm_grad(NormGradArgs A) {
       if (c.dup == V) continue;
       Elems<T, V> e;
 #pragma unroll
-      for (int j = 0; j < V; ++j) e.v[j] = from_float<T>(r * (g[k][j] - c1 - h[k][j] * c2));
+      for (int j = 0; j < V; ++j) e.v[j] = from_float<T>(scale * (g[k][j] - c1 - h[k][j] * c2));
       *reinterpret_cast<Elems<T, V>*>(dx + c.start) = e;
     }
   }
@@ -305,21 +341,33 @@ __global__ void __launch_bounds__(kThreads) k_norm_grad_columns(NormGradArgs A) 
     }
 }
 
-// dw and db (either may be null) from the slices' sums: 32 columns to a block, their slices dealt to its 8 rows of threads.
-constexpr int kJoinCols = 32;
-constexpr int kJoinRows = kThreads / kJoinCols;
+// dw and db (either may be null) from the slices' sums: 16 columns to a block, the slices dealt to its 64 rows of threads (with 8 rows of
+// threads 1024 slices of 602 sums took 35 us, the 128 loads of a thread one after the other).
+constexpr int kNormJoinCols = 16;
+constexpr int kNormJoinThreads = 1024;
+constexpr int kNormJoinRows = kNormJoinThreads / kNormJoinCols;
 template <typename P>
-__global__ void __launch_bounds__(kThreads) k_norm_grad_join(const float* __restrict__ part, int32_t slices, int32_t dim, P* dw, P* db) {
-  __shared__ float lds[kThreads];
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kJoinCols + threadIdx.x % kJoinCols, width = 2 * static_cast<int64_t>(dim);
+__global__ void __launch_bounds__(kNormJoinThreads) k_norm_grad_join(const float* __restrict__ part, int32_t slices, int32_t dim, P* dw, P* db) {
+  __shared__ float lds[kNormJoinThreads];
+  const int64_t width = 2 * static_cast<int64_t>(dim), i = static_cast<int64_t>(blockIdx.x) * kNormJoinCols + threadIdx.x % kNormJoinCols;
+  const float* p = part + (i < width ? i : width - 1);
   float s = 0.f;
-  if (i < width)
-    for (int q = threadIdx.x / kJoinCols; q < slices; q += kJoinRows) s += part[q * width + i];
+#pragma unroll 8
+  for (int q = threadIdx.x / kNormJoinCols; q < slices; q += kNormJoinRows) s += p[q * width];
   lds[threadIdx.x] = s;
   __syncthreads();
-  if (threadIdx.x >= kJoinCols || i >= width) return;
+  if (threadIdx.x < 128) {
+    s = 0.f;
 #pragma unroll
-  for (int q = 1; q < kJoinRows; ++q) s += lds[q * kJoinCols + threadIdx.x];
+    for (int q = 0; q < 8; ++q) s += lds[(threadIdx.x / kNormJoinCols + 8 * q) * kNormJoinCols + threadIdx.x % kNormJoinCols];
+  }
+  __syncthreads();
+  if (threadIdx.x < 128) lds[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x >= kNormJoinCols || i >= width) return;
+  s = 0.f;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) s += lds[q * kNormJoinCols + threadIdx.x];
   P* out = i < dim ? dw : db;
   if (out) out[i < dim ? i : i - dim] = from_float<P>(s);
 }

@@ -218,10 +218,10 @@ struct LaunchNorm {
   }
 };
 
-// Blocks, and slices of the weight's gradient, of the launch over max_rows rows of dim columns: the most that 4 MiB of sums hold.
+// Blocks, and slices of the weight's gradient, of the launch over max_rows rows of dim columns: the most that 16 MiB of sums hold.
 constexpr int kNormSlices = 1024;
 int64_t norm_slices(int64_t max_rows, int32_t dim) {
-  int64_t s = (int64_t(4) << 20) / (8 * static_cast<int64_t>(dim));
+  int64_t s = (int64_t(16) << 20) / (8 * static_cast<int64_t>(dim));
   if (s < 256) s = 256;
   if (s > kNormSlices) s = kNormSlices;
   return s < max_rows ? s : max_rows;
@@ -393,10 +393,10 @@ int smfg_layer_norm_grad(const void* d_dy, int64_t dy_stride, const void* d_x, i
     });
   }
   if (sums) {
-    const unsigned blocks = static_cast<unsigned>(ceil_div(2 * static_cast<int64_t>(dim), kJoinCols));
+    const unsigned blocks = static_cast<unsigned>(ceil_div(2 * static_cast<int64_t>(dim), kNormJoinCols));
     with_type(param_dtype, [&](auto p) {
       using P = decltype(p);
-      k_norm_grad_join<P><<<blocks, kThreads, 0, st>>>(part, static_cast<int32_t>(slices), dim, static_cast<P*>(d_dw), static_cast<P*>(d_db));
+      k_norm_grad_join<P><<<blocks, kNormJoinThreads, 0, st>>>(part, static_cast<int32_t>(slices), dim, static_cast<P*>(d_dw), static_cast<P*>(d_db));
     });
   }
   return hip_err(hipGetLastError());
