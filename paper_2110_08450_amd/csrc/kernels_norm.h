@@ -25,37 +25,57 @@ struct NormArgs {
   float* rstd;
 };
 
-// A group of LANES lanes has a row in its registers, NV vectors of V columns a lane: read once, centred before it is squared.
+// Threads of a block whose groups of LANES lanes have a row each.
+constexpr int norm_threads(int lanes) { return lanes > kThreads ? lanes : kThreads; }
+
+// A group of LANES lanes has a row in its registers, NV vectors of V columns a lane: read once, centred before it is squared.  The row and
+// the parameters are on their way together with the number of rows: a launch has no more groups than the arrays have rows.
 template <typename T, int V, int NV, int LANES>
-__global__ void __launch_bounds__(kThreads) k_layer_norm(NormArgs A) {
-  __shared__ float lds[kThreads / 64];
-  constexpr int kGroups = kThreads / LANES;
+__global__ void __launch_bounds__(norm_threads(LANES)) k_layer_norm(NormArgs A) {
+  __shared__ float lds[norm_threads(LANES) / 64];
+  constexpr int kGroups = norm_threads(LANES) / LANES;
   const int lane = threadIdx.x % LANES;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES;
+  const bool ragged = A.dim % V != 0;
+  const T* x = static_cast<const T*>(A.x) + (row < A.max_rows ? row : A.max_rows - 1) * A.x_stride;
+  Elems<T, V> e[NV];
+  float w[NV][V], b[NV][V];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) e[k] = *reinterpret_cast<const Elems<T, V>*>(x + Columns<V>(k * LANES + lane, A.dim).start);
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const Columns<V> c(k * LANES + lane, A.dim);
+    load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w[k]);
+    load_params<T, V>(A.b, A.float_params != 0, c.start, 0.f, b[k]);
+  }
   if (row >= count_of(A.num, A.max_rows)) return;
-  const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
   float v[NV][V];
   float s = 0.f;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const Columns<V> c(k * LANES + lane, A.dim);
-    const Elems<T, V> e = *reinterpret_cast<const Elems<T, V>*>(x + c.start);  // a column that there is not: the last ones again
+    float part = 0.f;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      v[k][j] = as_float(e.v[j]);
-      s += j >= c.dup ? v[k][j] : 0.f;
+      v[k][j] = as_float(e[k].v[j]);
+      if (ragged && j < c.dup) continue;
+      part += v[k][j];
     }
+    s += c.dup < V ? part : 0.f;
   }
   const float m = group_sum<LANES>(s, lds) / static_cast<float>(A.dim);
   s = 0.f;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const Columns<V> c(k * LANES + lane, A.dim);
+    float part = 0.f;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       v[k][j] -= m;
-      s += j >= c.dup ? v[k][j] * v[k][j] : 0.f;
+      if (ragged && j < c.dup) continue;
+      part += v[k][j] * v[k][j];
     }
+    s += c.dup < V ? part : 0.f;
   }
   const float r = 1.f / sqrtf(group_sum<LANES>(s, lds) / static_cast<float>(A.dim) + A.eps);
   if (lane == 0) {
@@ -67,13 +87,10 @@ __global__ void __launch_bounds__(kThreads) k_layer_norm(NormArgs A) {
   for (int k = 0; k < NV; ++k) {
     const Columns<V> c(k * LANES + lane, A.dim);
     if (c.dup == V) continue;
-    float w[V], b[V];
-    load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w);
-    load_params<T, V>(A.b, A.float_params != 0, c.start, 0.f, b);
-    Elems<T, V> e;
+    Elems<T, V> o;
 #pragma unroll
-    for (int j = 0; j < V; ++j) e.v[j] = from_float<T>(v[k][j] * r * w[j] + b[j]);
-    *reinterpret_cast<Elems<T, V>*>(y + c.start) = e;
+    for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(v[k][j] * r * w[k][j] + b[k][j]);
+    *reinterpret_cast<Elems<T, V>*>(y + c.start) = o;
   }
 }
 
@@ -142,9 +159,9 @@ struct NormGradArgs {
 // As k_layer_norm, a block striding over rows: a lane's columns are the same in each of them, so the sums for dw and db stay in
 // its registers until the block is done, and leave it once, as a slice of `part`.  A row is asked for while the one before is worked on.
 template <typename T, int V, int NV, int LANES>
-__global__ void __launch_bounds__(kThreads) k_layer_norm_grad(NormGradArgs A) {
-  __shared__ float lds[2][2][kThreads / 64];
-  constexpr int kGroups = kThreads / LANES;
+__global__ void __launch_bounds__(norm_threads(LANES)) k_layer_norm_grad(NormGradArgs A) {
+  __shared__ float lds[2][2][norm_threads(LANES) / 64];
+  constexpr int kGroups = norm_threads(LANES) / LANES;
   const int lane = threadIdx.x % LANES;
   const int64_t n = count_of(A.num, A.max_rows), step = static_cast<int64_t>(gridDim.x) * kGroups;
   const float inv = 1.f / static_cast<float>(A.dim);

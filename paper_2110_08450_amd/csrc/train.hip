@@ -202,8 +202,8 @@ bool with_row_shape(int32_t dim, F f) {
   else if (vectors <= 128) f.template operator()<V, 2, 64>();
   else if (vectors <= 256) f.template operator()<V, 1, 256>();
   else if (vectors <= 512) f.template operator()<V, 2, 256>();
-  else if (vectors <= 1024) f.template operator()<V, 4, 256>();
-  else if (V == 4 && vectors <= 2048) f.template operator()<V, V == 4 ? 8 : 4, 256>();
+  else if (vectors <= 1024) f.template operator()<V, 2, 512>();
+  else if (V == 4 && vectors <= 2048) f.template operator()<V, V == 4 ? 4 : 2, 512>();
   else return false;
   return true;
 }
@@ -214,7 +214,7 @@ struct LaunchNorm {
   hipStream_t st;
   template <int V, int NV, int LANES>
   void operator()() const {
-    k_layer_norm<T, V, NV, LANES><<<static_cast<unsigned>(ceil_div(A.max_rows, kThreads / LANES)), kThreads, 0, st>>>(A);
+    k_layer_norm<T, V, NV, LANES><<<static_cast<unsigned>(ceil_div(A.max_rows, norm_threads(LANES) / LANES)), norm_threads(LANES), 0, st>>>(A);
   }
 };
 
@@ -234,9 +234,9 @@ struct LaunchNormGrad {
   hipStream_t st;
   template <int V, int NV, int LANES>
   void operator()() const {
-    const int64_t blocks = ceil_div(A.max_rows, kThreads / LANES);
+    const int64_t blocks = ceil_div(A.max_rows, norm_threads(LANES) / LANES);
     if (blocks < slices) slices = blocks;
-    k_layer_norm_grad<T, V, NV, LANES><<<static_cast<unsigned>(slices), kThreads, 0, st>>>(A);
+    k_layer_norm_grad<T, V, NV, LANES><<<static_cast<unsigned>(slices), norm_threads(LANES), 0, st>>>(A);
   }
 };
 
