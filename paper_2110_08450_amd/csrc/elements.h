@@ -61,14 +61,13 @@ __device__ __forceinline__ void load_params(const void* p, bool is_float, int c,
   }
 }
 
-// Sum over groups of LANES lanes, in every lane; LANES of a whole block go through `lds`, a float per wave, which the
-// next sum may use again.
+// Sum over groups of LANES lanes, in every lane; LANES of a whole block go through `lds`, a float per wave.  Between two sums through the
+// same array has to be one through another: its barrier tells that the first has been read.
 template <int LANES>
 __device__ __forceinline__ float group_sum(float x, float* lds) {
 #pragma unroll
   for (int o = 1; o < (LANES < 64 ? LANES : 64); o <<= 1) x += __shfl_xor(x, o, 64);
   if constexpr (LANES > 64) {
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
     x = 0.f;

@@ -12,8 +12,7 @@ namespace smfg_dev {
 // The table is indexed by a scalar register, and the compiler may split such an address between two of them; scalar loads drop
 // the lowest two bits of each, so every index step has to be whole words (a table of bytes made pointers beside it garbage).
 constexpr int kClipTensors = 84;
-constexpr int kClipVector = 8;
-constexpr int kClipStep = kThreads * kClipVector;  // elements of a block's turn; chunks are whole turns
+constexpr int64_t kClipLeast = 2048, kClipMost = 65536;  // elements of a block
 struct ClipTensor {
   const void* src;
   void* dst;
@@ -50,25 +49,47 @@ __device__ __forceinline__ int64_t elements_of(const ClipTensor& T) {
   return n;
 }
 
+// A chunk by a block: rounds of TURNS vectors a thread, vector(i, k) for all of them and then done(i, k), i the vector's first element; the
+// rest vector by vector, and single(i) for what is no whole one.
+template <int V, int TURNS, typename Vector, typename Done, typename Single>
+__device__ __forceinline__ void for_chunk(int64_t from, int64_t to, Vector vector, Done done, Single single) {
+  constexpr int kRound = kThreads * V * TURNS;
+  int64_t at = from;
+  for (; at + kRound <= to; at += kRound) {
+#pragma unroll
+    for (int k = 0; k < TURNS; ++k) vector(at + (k * kThreads + static_cast<int>(threadIdx.x)) * V, k);
+#pragma unroll
+    for (int k = 0; k < TURNS; ++k) done(at + (k * kThreads + static_cast<int>(threadIdx.x)) * V, k);
+  }
+  for (; at < to; at += kThreads * V) {
+    const int64_t i = at + static_cast<int>(threadIdx.x) * V;
+    if (i + V <= to) {
+      vector(i, 0);
+      done(i, 0);
+    } else {
+      for (int64_t q = i; q < to; ++q) single(q);
+    }
+  }
+}
+constexpr int kClipTurns = 4;
+
 // Squares are added in 64 bits: those of floats from 1e19 on are beyond a float's range, and a sum over 10^9 elements keeps its digits.
 template <typename T>
 __device__ __forceinline__ double sum_of_squares(const T* src, int64_t from, int64_t to) {
+  constexpr int V = 16 / sizeof(T);
   double s = 0.0;
-  for (int64_t i = from + static_cast<int64_t>(threadIdx.x) * kClipVector; i < to; i += kClipStep) {
-    if (i + kClipVector <= to) {
-      const Elems<T, kClipVector> e = *reinterpret_cast<const Elems<T, kClipVector>*>(src + i);
+  Elems<T, V> e[kClipTurns];
+  const auto add = [&](T x) {
+    const double d = as_float(x);
+    s += d * d;
+  };
+  for_chunk<V, kClipTurns>(
+      from, to, [&](int64_t i, int k) { e[k] = *reinterpret_cast<const Elems<T, V>*>(src + i); },
+      [&](int64_t, int k) {
 #pragma unroll
-      for (int j = 0; j < kClipVector; ++j) {
-        const double d = as_float(e.v[j]);
-        s += d * d;
-      }
-    } else {
-      for (int64_t q = i; q < to; ++q) {
-        const double d = as_float(src[q]);
-        s += d * d;
-      }
-    }
-  }
+        for (int j = 0; j < V; ++j) add(e[k].v[j]);
+      },
+      [&](int64_t i) { add(src[i]); });
   return s;
 }
 
@@ -100,6 +121,7 @@ static __global__ void __launch_bounds__(kClipNormThreads) k_clip_norm(const dou
                                                                 float* factor) {
   __shared__ double lds[kClipNormThreads / 64];
   double s = 0.0;
+#pragma unroll 8
   for (int64_t i = threadIdx.x; i < parts; i += kClipNormThreads) s += part[i];
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o, 64);
@@ -113,19 +135,20 @@ static __global__ void __launch_bounds__(kClipNormThreads) k_clip_norm(const dou
   *factor = static_cast<float>(scale * (__builtin_isinf(max_norm) || c >= 1.0 ? 1.0 : c));  // NaN stays NaN
 }
 
+// Vectors of 16 bytes of the wider type, so that the lanes of an instruction read and write bytes without a gap.
 template <typename TS, typename TD>
 __device__ __forceinline__ void scaled_copy(const TS* src, TD* dst, int64_t from, int64_t to, float f) {
-  for (int64_t i = from + static_cast<int64_t>(threadIdx.x) * kClipVector; i < to; i += kClipStep) {
-    if (i + kClipVector <= to) {
-      const Elems<TS, kClipVector> e = *reinterpret_cast<const Elems<TS, kClipVector>*>(src + i);
-      Elems<TD, kClipVector> o;
+  constexpr int V = 16 / (sizeof(TS) > sizeof(TD) ? sizeof(TS) : sizeof(TD));
+  Elems<TS, V> e[kClipTurns];
+  for_chunk<V, kClipTurns>(
+      from, to, [&](int64_t i, int k) { e[k] = *reinterpret_cast<const Elems<TS, V>*>(src + i); },
+      [&](int64_t i, int k) {
+        Elems<TD, V> o;
 #pragma unroll
-      for (int j = 0; j < kClipVector; ++j) o.v[j] = from_float<TD>(f * as_float(e.v[j]));
-      *reinterpret_cast<Elems<TD, kClipVector>*>(dst + i) = o;
-    } else {
-      for (int64_t q = i; q < to; ++q) dst[q] = from_float<TD>(f * as_float(src[q]));
-    }
-  }
+        for (int j = 0; j < V; ++j) o.v[j] = from_float<TD>(f * as_float(e[k].v[j]));
+        *reinterpret_cast<Elems<TD, V>*>(dst + i) = o;
+      },
+      [&](int64_t i) { dst[i] = from_float<TD>(f * as_float(src[i])); });
 }
 
 static __global__ void __launch_bounds__(kThreads) k_clip_scale(ClipArgs A) {

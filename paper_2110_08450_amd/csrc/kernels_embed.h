@@ -53,8 +53,9 @@ __global__ void __launch_bounds__(kThreads) k_embedding(EmbedArgs A) {
 #pragma unroll
   for (int k = 0; k < kEmbedTurns; ++k) {
     // row 0 stands for one that there is not: a load under a condition is waited for before the next
-    e[k] = *reinterpret_cast<const Elems<TI, V>*>(static_cast<const TI*>(A.table) + (id[k] < A.num_rows ? id[k] : 0u) * A.table_stride +
+    const Elems<TI, V>* p = reinterpret_cast<const Elems<TI, V>*>(static_cast<const TI*>(A.table) + (id[k] < A.num_rows ? id[k] : 0u) * A.table_stride +
                                                   Columns<V>(at[k], A.dim).start);
+    e[k] = *p;
   }
 #pragma unroll
   for (int k = 0; k < kEmbedTurns; ++k) {
@@ -62,7 +63,8 @@ __global__ void __launch_bounds__(kThreads) k_embedding(EmbedArgs A) {
     Elems<TO, V> o;
 #pragma unroll
     for (int j = 0; j < V; ++j) o.v[j] = from_float<TO>(id[k] < A.num_rows ? A.scale * as_float(e[k].v[j]) : 0.f);
-    *reinterpret_cast<Elems<TO, V>*>(static_cast<TO*>(A.out) + (row0 + row[k]) * A.out_stride + Columns<V>(at[k], A.dim).start) = o;
+    Elems<TO, V>* p = reinterpret_cast<Elems<TO, V>*>(static_cast<TO*>(A.out) + (row0 + row[k]) * A.out_stride + Columns<V>(at[k], A.dim).start);
+    *p = o;
   }
 }
 

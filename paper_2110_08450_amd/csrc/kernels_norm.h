@@ -28,69 +28,77 @@ struct NormArgs {
 // Threads of a block whose groups of LANES lanes have a row each.
 constexpr int norm_threads(int lanes) { return lanes > kThreads ? lanes : kThreads; }
 
-// A group of LANES lanes has a row in its registers, NV vectors of V columns a lane: read once, centred before it is squared.  The row and
-// the parameters are on their way together with the number of rows: a launch has no more groups than the arrays have rows.
+// A group of LANES lanes has a row in its registers, NV vectors of V columns a lane: read once, centred before it is squared.  A block
+// strides over rows, so that the parameters stay in registers, and asks for a row while the one before is worked on; the first is on its
+// way together with the number of rows, as a launch has no more groups than the arrays have rows.
 template <typename T, int V, int NV, int LANES>
 __global__ void __launch_bounds__(norm_threads(LANES)) k_layer_norm(NormArgs A) {
-  __shared__ float lds[norm_threads(LANES) / 64];
+  __shared__ float lds[2][norm_threads(LANES) / 64];
   constexpr int kGroups = norm_threads(LANES) / LANES;
   const int lane = threadIdx.x % LANES;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES;
   const bool ragged = A.dim % V != 0;
-  const T* x = static_cast<const T*>(A.x) + (row < A.max_rows ? row : A.max_rows - 1) * A.x_stride;
+  const T* const x = static_cast<const T*>(A.x);
   Elems<T, V> e[NV];
   float w[NV][V], b[NV][V];
+  const auto load = [&](int64_t i) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) e[k] = *reinterpret_cast<const Elems<T, V>*>(x + Columns<V>(k * LANES + lane, A.dim).start);
+    for (int k = 0; k < NV; ++k) e[k] = *reinterpret_cast<const Elems<T, V>*>(x + i * A.x_stride + Columns<V>(k * LANES + lane, A.dim).start);
+  };
+  load(row < A.max_rows ? row : A.max_rows - 1);
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const Columns<V> c(k * LANES + lane, A.dim);
     load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w[k]);
     load_params<T, V>(A.b, A.float_params != 0, c.start, 0.f, b[k]);
   }
-  if (row >= count_of(A.num, A.max_rows)) return;
-  float v[NV][V];
-  float s = 0.f;
+  const int64_t n = count_of(A.num, A.max_rows);
+  for (; row < n; row += step) {
+    float v[NV][V];
+    float s = 0.f;
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const Columns<V> c(k * LANES + lane, A.dim);
-    float part = 0.f;
+    for (int k = 0; k < NV; ++k) {
+      const Columns<V> c(k * LANES + lane, A.dim);
+      float part = 0.f;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      v[k][j] = as_float(e[k].v[j]);
-      if (ragged && j < c.dup) continue;
-      part += v[k][j];
+      for (int j = 0; j < V; ++j) {
+        v[k][j] = as_float(e[k].v[j]);
+        if (ragged && j < c.dup) continue;
+        part += v[k][j];
+      }
+      s += c.dup < V ? part : 0.f;
     }
-    s += c.dup < V ? part : 0.f;
-  }
-  const float m = group_sum<LANES>(s, lds) / static_cast<float>(A.dim);
-  s = 0.f;
+    if (row + step < n) load(row + step);
+    const float m = group_sum<LANES>(s, lds[0]) / static_cast<float>(A.dim);
+    s = 0.f;
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const Columns<V> c(k * LANES + lane, A.dim);
-    float part = 0.f;
+    for (int k = 0; k < NV; ++k) {
+      const Columns<V> c(k * LANES + lane, A.dim);
+      float part = 0.f;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      v[k][j] -= m;
-      if (ragged && j < c.dup) continue;
-      part += v[k][j] * v[k][j];
+      for (int j = 0; j < V; ++j) {
+        v[k][j] -= m;
+        if (ragged && j < c.dup) continue;
+        part += v[k][j] * v[k][j];
+      }
+      s += c.dup < V ? part : 0.f;
     }
-    s += c.dup < V ? part : 0.f;
-  }
-  const float r = 1.f / sqrtf(group_sum<LANES>(s, lds) / static_cast<float>(A.dim) + A.eps);
-  if (lane == 0) {
-    if (A.mean) A.mean[row] = m;
-    if (A.rstd) A.rstd[row] = r;
-  }
-  T* y = static_cast<T*>(A.y) + row * A.y_stride;
+    const float r = 1.f / sqrtf(group_sum<LANES>(s, lds[1]) / static_cast<float>(A.dim) + A.eps);
+    if (lane == 0) {
+      if (A.mean) A.mean[row] = m;
+      if (A.rstd) A.rstd[row] = r;
+    }
+    T* y = static_cast<T*>(A.y) + row * A.y_stride;
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const Columns<V> c(k * LANES + lane, A.dim);
-    if (c.dup == V) continue;
-    Elems<T, V> o;
+    for (int k = 0; k < NV; ++k) {
+      const Columns<V> c(k * LANES + lane, A.dim);
+      if (c.dup == V) continue;
+      Elems<T, V> o;
 #pragma unroll
-    for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(v[k][j] * r * w[k][j] + b[k][j]);
-    *reinterpret_cast<Elems<T, V>*>(y + c.start) = o;
+      for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(v[k][j] * r * w[k][j] + b[k][j]);
+      *reinterpret_cast<Elems<T, V>*>(y + c.start) = o;
+    }
   }
 }
 
@@ -98,7 +106,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_layer_norm(NormArgs A) 
 // one before are written once, as y may be x.
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads) k_layer_norm_long(NormArgs A) {
-  __shared__ float lds[kThreads / 64];
+  __shared__ float lds[2][kThreads / 64];
   const int64_t row = blockIdx.x;
   if (row >= count_of(A.num, A.max_rows)) return;
   const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
@@ -110,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) k_layer_norm_long(NormArgs A) {
 #pragma unroll
     for (int j = 0; j < V; ++j) s += j >= c.dup ? as_float(e.v[j]) : 0.f;
   }
-  const float m = group_sum<kThreads>(s, lds) / static_cast<float>(A.dim);
+  const float m = group_sum<kThreads>(s, lds[0]) / static_cast<float>(A.dim);
   s = 0.f;
   for (int i = threadIdx.x; i < vectors; i += kThreads) {
     const Columns<V> c(i, A.dim);
@@ -121,7 +129,7 @@ __global__ void __launch_bounds__(kThreads) k_layer_norm_long(NormArgs A) {
       s += j >= c.dup ? d * d : 0.f;
     }
   }
-  const float r = 1.f / sqrtf(group_sum<kThreads>(s, lds) / static_cast<float>(A.dim) + A.eps);
+  const float r = 1.f / sqrtf(group_sum<kThreads>(s, lds[1]) / static_cast<float>(A.dim) + A.eps);
   if (threadIdx.x == 0) {
     if (A.mean) A.mean[row] = m;
     if (A.rstd) A.rstd[row] = r;
@@ -294,7 +302,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_layer_norm_grad(NormGra
 // Rows that outgrow the registers of a block: dx by a block per row, which reads it twice; the sums by k_norm_grad_columns.
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads) k_layer_norm_grad_long(NormGradArgs A) {
-  __shared__ float lds[kThreads / 64];
+  __shared__ float lds[2][kThreads / 64];
   const int64_t row = blockIdx.x;
   if (row >= count_of(A.num, A.max_rows)) return;
   const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
@@ -316,7 +324,7 @@ __global__ void __launch_bounds__(kThreads) k_layer_norm_grad_long(NormGradArgs 
       s2 += j >= c.dup ? g * h : 0.f;
     }
   }
-  const float c1 = group_sum<kThreads>(s1, lds) * inv, c2 = group_sum<kThreads>(s2, lds) * inv;
+  const float c1 = group_sum<kThreads>(s1, lds[0]) * inv, c2 = group_sum<kThreads>(s2, lds[1]) * inv;
   for (int i = threadIdx.x; i < vectors; i += kThreads) {
     const Columns<V> c(i, A.dim);
     const Elems<T, V> ex = *reinterpret_cast<const Elems<T, V>*>(x + c.start);

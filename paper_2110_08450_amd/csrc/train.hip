@@ -191,7 +191,8 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
 // ---- layer norm ---------------------------------------------------------------------------------
 
 // How rows of `vectors` vectors are dealt: LANES lanes and NV vectors a lane; f.template operator()<V, NV, LANES>.
-template <typename T, typename F>
+// most: the largest LANES * NV that the registers hold.
+template <typename T, int most, typename F>
 bool with_row_shape(int32_t dim, F f) {
   constexpr int V = kVec<T>;
   if (dim < V) return f.template operator()<1, 1, 16>(), true;
@@ -202,19 +203,25 @@ bool with_row_shape(int32_t dim, F f) {
   else if (vectors <= 128) f.template operator()<V, 2, 64>();
   else if (vectors <= 256) f.template operator()<V, 1, 256>();
   else if (vectors <= 512) f.template operator()<V, 2, 256>();
+  else if (vectors <= 768) f.template operator()<V, 3, 256>();
   else if (vectors <= 1024) f.template operator()<V, 2, 512>();
-  else if (V == 4 && vectors <= 2048) f.template operator()<V, V == 4 ? 4 : 2, 512>();
+  else if (vectors <= 1536) f.template operator()<V, 3, 512>();
+  else if (most >= 2048 && vectors <= 2048) f.template operator()<V, most >= 2048 ? 4 : 3, 512>();
   else return false;
   return true;
 }
 
+// Blocks of k_layer_norm at most.  Rows of 256 to 8192 halfs, 128 MiB of them: 52 to 57 us with 1024 to 4096 blocks, 60 to 67 with a block for
+// every row or group of rows, whose parameters are more bytes than the row; rows of floats 95 to 108 with either.
+constexpr unsigned kNormBlocks = 2048;
 template <typename T>
 struct LaunchNorm {
   const NormArgs& A;
   hipStream_t st;
   template <int V, int NV, int LANES>
   void operator()() const {
-    k_layer_norm<T, V, NV, LANES><<<static_cast<unsigned>(ceil_div(A.max_rows, norm_threads(LANES) / LANES)), norm_threads(LANES), 0, st>>>(A);
+    const unsigned blocks = blocks_for(A.max_rows, norm_threads(LANES) / LANES, kNormBlocks);
+    k_layer_norm<T, V, NV, LANES><<<blocks, norm_threads(LANES), 0, st>>>(A);
   }
 };
 
@@ -254,12 +261,13 @@ bool bad_grads(const smfg_grad_t* g, int32_t n) {
   return false;
 }
 
-// Elements of a block: about 4096 blocks, of 1 to 16 turns.
+// Elements of a block: as few as a turn of its threads, as many as leave 4096 blocks, or 64 Ki.
 int64_t clip_chunk(const smfg_grad_t* g, int32_t n) {
   double all = 0;
   for (int i = 0; i < n; ++i) all += static_cast<double>(g[i].numel);
-  const int64_t turns = static_cast<int64_t>(all / 4096 / kClipStep);
-  return (turns < 1 ? 1 : turns > 16 ? 16 : turns) * kClipStep;
+  int64_t chunk = kClipLeast;
+  while (chunk < kClipMost && all > 4096.0 * static_cast<double>(2 * chunk)) chunk *= 2;
+  return chunk;
 }
 int64_t clip_blocks(const smfg_grad_t* g, int32_t n, int64_t chunk) {
   int64_t b = 0;
@@ -352,7 +360,7 @@ int smfg_layer_norm(const void* d_x, int64_t x_stride, int32_t dtype, const int6
   const NormArgs A = {d_x, x_stride, d_num_rows, max_rows, dim, param_dtype == SMFG_DTYPE_F32, d_w, d_b, eps, d_y, y_stride, d_mean, d_rstd};
   with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    if (!with_row_shape<T>(dim, LaunchNorm<T>{A, st})) k_layer_norm_long<T, kVec<T>><<<static_cast<unsigned>(max_rows), kThreads, 0, st>>>(A);
+    if (!with_row_shape<T, 2048>(dim, LaunchNorm<T>{A, st})) k_layer_norm_long<T, kVec<T>><<<static_cast<unsigned>(max_rows), kThreads, 0, st>>>(A);
   });
   return hip_err(hipGetLastError());
 }
@@ -384,7 +392,7 @@ int smfg_layer_norm_grad(const void* d_dy, int64_t dy_stride, const void* d_x, i
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
       constexpr int V = kVec<T>;
-      if (with_row_shape<T>(dim, LaunchNormGrad<T>{A, slices, st})) return;
+      if (with_row_shape<T, sizeof(T) == 4 ? 2048 : 1536>(dim, LaunchNormGrad<T>{A, slices, st})) return;
       if (sums) {
         if (slices > 64) slices = 64;
         k_norm_grad_columns<T, V><<<dim3(static_cast<unsigned>(ceil_div(ceil_div(dim, V), kThreads)), static_cast<unsigned>(slices)), kThreads, 0, st>>>(A);
