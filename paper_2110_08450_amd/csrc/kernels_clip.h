@@ -8,10 +8,12 @@
 
 namespace smfg_dev {
 
-// The tensors of a launch, in its arguments.  Block first_block + q of a tensor has its elements [q * chunk, (q + 1) * chunk).
+// Up to kClipTensors tensors are in the arguments of the launches themselves.  More are written to a table in the scratch first, kClipTensors a
+// launch, so that squares and scaling are one launch each: 290 tensors of 400 M halfs in four launches each took 743 us, one each 698: most of the
+// difference is at their ends, where a launch no longer fills the chip.
 // The table is indexed by a scalar register, and the compiler may split such an address between two of them; scalar loads drop
 // the lowest two bits of each, so every index step has to be whole words (a table of bytes made pointers beside it garbage).
-constexpr int kClipTensors = 84;
+constexpr int kClipTensors = 80;
 constexpr int64_t kClipLeast = 2048, kClipMost = 65536;  // elements of a block
 struct ClipTensor {
   const void* src;
@@ -19,12 +21,14 @@ struct ClipTensor {
   int64_t numel;
   const int64_t* rows;  // or null: the tensor counts up to *rows * row_elems elements
   int64_t row_elems;
-  uint32_t first_block;
-  int32_t type;         // of src | of dst << 4
+  uint32_t first_block;  // block first_block + q has elements [q * chunk, (q + 1) * chunk)
+  int32_t type;          // of src | of dst << 4
 };
 struct ClipArgs {
   ClipTensor t[kClipTensors];
-  int32_t tensors;
+  ClipTensor* table;    // of all tensors, or null: t has them all
+  int32_t tensors;      // of the table, or of t
+  int32_t first, here;  // tensors of the table that t has, for k_clip_table
   uint32_t blocks;
   int64_t chunk;
   double* part;         // a block's sum of squares
@@ -32,13 +36,30 @@ struct ClipArgs {
 };
 static_assert(sizeof(ClipTensor) == 48 && sizeof(ClipArgs) <= 4096, "kernel arguments are limited to 4 KB");
 
-__device__ __forceinline__ int tensor_of_block(const ClipArgs& A) {
+static __global__ void __launch_bounds__(64) k_clip_table(ClipArgs A) {
+  for (int i = threadIdx.x; i < A.here; i += 64) A.table[A.first + i] = A.t[i];
+}
+
+// The last tensor that begins at the block or before it.
+template <bool TABLE>
+__device__ __forceinline__ ClipTensor tensor_of_block(const ClipArgs& A, uint32_t block) {
   const int lane = threadIdx.x & 63;
-  int t = -1;  // the last tensor that begins at this block or before
+  if constexpr (!TABLE) {
+    int t = -1;
 #pragma unroll
-  for (int i = 0; i < kClipTensors; i += 64)
-    t += __popcll(__ballot(i + lane < A.tensors && blockIdx.x >= A.t[i + lane < A.tensors ? i + lane : 0].first_block));
-  return t;
+    for (int i = 0; i < kClipTensors; i += 64)
+      t += __popcll(__ballot(i + lane < A.tensors && block >= A.t[i + lane < A.tensors ? i + lane : 0].first_block));
+    return A.t[t];
+  } else {
+    int lo = 0, hi = A.tensors;  // it is in [lo, hi)
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+      const int begun = __popcll(__ballot(at < hi && block >= A.table[at < hi ? at : lo].first_block));
+      lo += (begun - 1) * step;
+      hi = lo + step < hi ? lo + step : hi;
+    }
+    return A.table[lo];
+  }
 }
 __device__ __forceinline__ int64_t elements_of(const ClipTensor& T) {
   int64_t n = T.numel;
@@ -49,25 +70,42 @@ __device__ __forceinline__ int64_t elements_of(const ClipTensor& T) {
   return n;
 }
 
+// The elements of a block: those of its chunk, shifted back to where `base` is a multiple of 16 bytes, so that all vectors but the first chunk's
+// single elements are aligned and rounds are whole (400 M halfs in 60 tensors at any address: 651 -> 645 us; with a few single elements at every chunk instead 665).
+struct ClipRange {
+  int64_t from, to;
+  int ahead;  // single elements before the first vector
+};
+template <typename T>
+__device__ __forceinline__ ClipRange range_of(const T* base, uint32_t q, int64_t chunk, int64_t numel, int64_t n) {
+  const int past = static_cast<int>(reinterpret_cast<uintptr_t>(base) & 15) / static_cast<int>(sizeof(T));
+  const int64_t from = q == 0 ? 0 : q * chunk - past;
+  const bool last = (q + 1) * chunk >= numel;
+  const int64_t to = last ? numel : (q + 1) * chunk - past;
+  const int ahead = q == 0 && past > 0 ? 16 / static_cast<int>(sizeof(T)) - past : 0;
+  return {from, to < n ? to : n, ahead};
+}
+
 // A chunk by a block: rounds of TURNS vectors a thread, vector(i, k) for all of them and then done(i, k), i the vector's first element; the
 // rest vector by vector, and single(i) for what is no whole one.
 template <int V, int TURNS, typename Vector, typename Done, typename Single>
-__device__ __forceinline__ void for_chunk(int64_t from, int64_t to, Vector vector, Done done, Single single) {
+__device__ __forceinline__ void for_chunk(const ClipRange& R, Vector vector, Done done, Single single) {
   constexpr int kRound = kThreads * V * TURNS;
-  int64_t at = from;
-  for (; at + kRound <= to; at += kRound) {
+  int64_t at = R.from + R.ahead < R.to ? R.from + R.ahead : R.to;
+  if (static_cast<int>(threadIdx.x) < at - R.from) single(R.from + static_cast<int>(threadIdx.x));
+  for (; at + kRound <= R.to; at += kRound) {
 #pragma unroll
     for (int k = 0; k < TURNS; ++k) vector(at + (k * kThreads + static_cast<int>(threadIdx.x)) * V, k);
 #pragma unroll
     for (int k = 0; k < TURNS; ++k) done(at + (k * kThreads + static_cast<int>(threadIdx.x)) * V, k);
   }
-  for (; at < to; at += kThreads * V) {
+  for (; at < R.to; at += kThreads * V) {
     const int64_t i = at + static_cast<int>(threadIdx.x) * V;
-    if (i + V <= to) {
+    if (i + V <= R.to) {
       vector(i, 0);
       done(i, 0);
     } else {
-      for (int64_t q = i; q < to; ++q) single(q);
+      for (int64_t q = i; q < R.to; ++q) single(q);
     }
   }
 }
@@ -75,7 +113,7 @@ constexpr int kClipTurns = 4;
 
 // Squares are added in 64 bits: those of floats from 1e19 on are beyond a float's range, and a sum over 10^9 elements keeps its digits.
 template <typename T>
-__device__ __forceinline__ double sum_of_squares(const T* src, int64_t from, int64_t to) {
+__device__ __forceinline__ double sum_of_squares(const T* src, uint32_t q, int64_t chunk, int64_t numel, int64_t n) {
   constexpr int V = 16 / sizeof(T);
   double s = 0.0;
   Elems<T, V> e[kClipTurns];
@@ -84,7 +122,7 @@ __device__ __forceinline__ double sum_of_squares(const T* src, int64_t from, int
     s += d * d;
   };
   for_chunk<V, kClipTurns>(
-      from, to, [&](int64_t i, int k) { e[k] = *reinterpret_cast<const Elems<T, V>*>(src + i); },
+      range_of(src, q, chunk, numel, n), [&](int64_t i, int k) { e[k] = *reinterpret_cast<const Elems<T, V>*>(src + i); },
       [&](int64_t, int k) {
 #pragma unroll
         for (int j = 0; j < V; ++j) add(e[k].v[j]);
@@ -93,16 +131,17 @@ __device__ __forceinline__ double sum_of_squares(const T* src, int64_t from, int
   return s;
 }
 
-static __global__ void __launch_bounds__(kThreads) k_clip_squares(ClipArgs A) {
+template <bool TABLE>
+__global__ void __launch_bounds__(kThreads) k_clip_squares(ClipArgs A) {
   __shared__ double lds[kThreads / 64];
-  const ClipTensor T = A.t[tensor_of_block(A)];
-  const int64_t n = elements_of(T), from = static_cast<int64_t>(blockIdx.x - T.first_block) * A.chunk;
-  const int64_t to = from + A.chunk < n ? from + A.chunk : n;
+  const ClipTensor T = tensor_of_block<TABLE>(A, blockIdx.x);
+  const int64_t n = elements_of(T);
+  const uint32_t q = blockIdx.x - T.first_block;
   double s;
   switch (T.type & 15) {
-    case SMFG_DTYPE_F32: s = sum_of_squares(static_cast<const float*>(T.src), from, to); break;
-    case SMFG_DTYPE_F16: s = sum_of_squares(static_cast<const _Float16*>(T.src), from, to); break;
-    default: s = sum_of_squares(static_cast<const __bf16*>(T.src), from, to); break;
+    case SMFG_DTYPE_F32: s = sum_of_squares(static_cast<const float*>(T.src), q, A.chunk, T.numel, n); break;
+    case SMFG_DTYPE_F16: s = sum_of_squares(static_cast<const _Float16*>(T.src), q, A.chunk, T.numel, n); break;
+    default: s = sum_of_squares(static_cast<const __bf16*>(T.src), q, A.chunk, T.numel, n); break;
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o, 64);
@@ -137,11 +176,11 @@ static __global__ void __launch_bounds__(kClipNormThreads) k_clip_norm(const dou
 
 // Vectors of 16 bytes of the wider type, so that the lanes of an instruction read and write bytes without a gap.
 template <typename TS, typename TD>
-__device__ __forceinline__ void scaled_copy(const TS* src, TD* dst, int64_t from, int64_t to, float f) {
+__device__ __forceinline__ void scaled_copy(const TS* src, TD* dst, uint32_t q, int64_t chunk, int64_t numel, int64_t n, float f) {
   constexpr int V = 16 / (sizeof(TS) > sizeof(TD) ? sizeof(TS) : sizeof(TD));
   Elems<TS, V> e[kClipTurns];
   for_chunk<V, kClipTurns>(
-      from, to, [&](int64_t i, int k) { e[k] = *reinterpret_cast<const Elems<TS, V>*>(src + i); },
+      range_of(dst, q, chunk, numel, n), [&](int64_t i, int k) { e[k] = *reinterpret_cast<const Elems<TS, V>*>(src + i); },
       [&](int64_t i, int k) {
         Elems<TD, V> o;
 #pragma unroll
@@ -151,19 +190,22 @@ __device__ __forceinline__ void scaled_copy(const TS* src, TD* dst, int64_t from
       [&](int64_t i) { dst[i] = from_float<TD>(f * as_float(src[i])); });
 }
 
-static __global__ void __launch_bounds__(kThreads) k_clip_scale(ClipArgs A) {
-  const ClipTensor T = A.t[tensor_of_block(A)];
+// The last elements first: they are what the sum of squares has left in the caches.
+template <bool TABLE>
+__global__ void __launch_bounds__(kThreads) k_clip_scale(ClipArgs A) {
+  const uint32_t block = A.blocks - 1 - blockIdx.x;
+  const ClipTensor T = tensor_of_block<TABLE>(A, block);
   const float f = *A.factor;
   if (f == 1.f && T.src == T.dst) return;  // in place, nothing to clip
-  const int64_t n = elements_of(T), from = static_cast<int64_t>(blockIdx.x - T.first_block) * A.chunk;
-  const int64_t to = from + A.chunk < n ? from + A.chunk : n;
+  const int64_t n = elements_of(T);
+  const uint32_t q = block - T.first_block;
   constexpr int F32 = SMFG_DTYPE_F32, F16 = SMFG_DTYPE_F16, BF16 = SMFG_DTYPE_BF16;
   switch (T.type) {
-    case F32 | F32 << 4: scaled_copy(static_cast<const float*>(T.src), static_cast<float*>(T.dst), from, to, f); break;
-    case F16 | F16 << 4: scaled_copy(static_cast<const _Float16*>(T.src), static_cast<_Float16*>(T.dst), from, to, f); break;
-    case F16 | F32 << 4: scaled_copy(static_cast<const _Float16*>(T.src), static_cast<float*>(T.dst), from, to, f); break;
-    case BF16 | BF16 << 4: scaled_copy(static_cast<const __bf16*>(T.src), static_cast<__bf16*>(T.dst), from, to, f); break;
-    default: scaled_copy(static_cast<const __bf16*>(T.src), static_cast<float*>(T.dst), from, to, f); break;
+    case F32 | F32 << 4: scaled_copy(static_cast<const float*>(T.src), static_cast<float*>(T.dst), q, A.chunk, T.numel, n, f); break;
+    case F16 | F16 << 4: scaled_copy(static_cast<const _Float16*>(T.src), static_cast<_Float16*>(T.dst), q, A.chunk, T.numel, n, f); break;
+    case F16 | F32 << 4: scaled_copy(static_cast<const _Float16*>(T.src), static_cast<float*>(T.dst), q, A.chunk, T.numel, n, f); break;
+    case BF16 | BF16 << 4: scaled_copy(static_cast<const __bf16*>(T.src), static_cast<__bf16*>(T.dst), q, A.chunk, T.numel, n, f); break;
+    default: scaled_copy(static_cast<const __bf16*>(T.src), static_cast<float*>(T.dst), q, A.chunk, T.numel, n, f); break;
   }
 }
 

@@ -275,29 +275,26 @@ int64_t clip_blocks(const smfg_grad_t* g, int32_t n, int64_t chunk) {
   return b;
 }
 
-// Calls f with the tensors that fit a launch, until there are no more.
-template <typename F>
-void for_clip_launches(const smfg_grad_t* g, int32_t n, int64_t chunk, double* part, const float* factor, F f) {
-  ClipArgs A;
-  A.chunk = chunk;
-  A.factor = factor;
-  for (int i = 0; i < n;) {
-    A.tensors = 0;
-    A.blocks = 0;
-    A.part = part;
-    for (; i < n && A.tensors < kClipTensors; ++i) {
-      if (g[i].numel == 0) continue;
-      const int64_t blocks = ceil_div(g[i].numel, chunk);
-      if (A.blocks + blocks > 0x7FFFFFFF) break;
-      void* const out = g[i].out ? g[i].out : const_cast<void*>(g[i].grad);
-      A.t[A.tensors++] = {g[i].grad, out, g[i].numel, g[i].d_rows, g[i].d_rows ? g[i].row_elems : 1, A.blocks,
-                          g[i].dtype | (g[i].out ? g[i].out_dtype : g[i].dtype) << 4};
-      A.blocks += static_cast<uint32_t>(blocks);
-    }
-    if (A.tensors == 0) break;
-    f(A);
-    part += A.blocks;
-  }
+int clip_tensors(const smfg_grad_t* g, int32_t n) {
+  int m = 0;
+  for (int i = 0; i < n; ++i) m += g[i].numel > 0;
+  return m;
+}
+
+// Scratch: the factor, the table of more tensors than the arguments hold, the blocks' sums.
+struct ClipScratch {
+  int64_t table, part, bytes, blocks, chunk;
+  int32_t tensors;
+};
+ClipScratch clip_scratch(const smfg_grad_t* g, int32_t n) {
+  ClipScratch S;
+  S.chunk = clip_chunk(g, n);
+  S.blocks = clip_blocks(g, n, S.chunk);
+  S.tensors = clip_tensors(g, n);
+  S.table = 256;
+  S.part = S.table + (S.tensors > kClipTensors ? up256(static_cast<int64_t>(sizeof(ClipTensor)) * S.tensors) : 0);
+  S.bytes = S.part + up256(8 * S.blocks);
+  return S;
 }
 
 }  // namespace
@@ -412,7 +409,7 @@ int smfg_layer_norm_grad(const void* d_dy, int64_t dy_stride, const void* d_x, i
 
 int64_t smfg_clip_grad_norm_scratch_bytes(const smfg_grad_t* grads, int32_t num_grads) {
   if (num_grads < 0 || (num_grads > 0 && !grads) || bad_grads(grads, num_grads)) return -1;
-  return 256 + up256(8 * clip_blocks(grads, num_grads, clip_chunk(grads, num_grads)));
+  return clip_scratch(grads, num_grads).bytes;
 }
 
 int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale, float max_norm, float* d_norm, void* d_scratch,
@@ -422,14 +419,44 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
     return SMFG_ERR_INVALID_ARG;
   for (int i = 0; i < num_grads; ++i)
     if (grads[i].numel > 0 && !grads[i].grad) return SMFG_ERR_NULL_PTR;
-  const int64_t chunk = clip_chunk(grads, num_grads), parts = clip_blocks(grads, num_grads, chunk);
-  if (scratch_bytes < 256 + up256(8 * parts)) return SMFG_ERR_CAPACITY;
+  const ClipScratch S = clip_scratch(grads, num_grads);
+  if (S.blocks > 0x7FFFFFFF) return SMFG_ERR_INVALID_ARG;
+  if (scratch_bytes < S.bytes) return SMFG_ERR_CAPACITY;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  uint8_t* scratch = static_cast<uint8_t*>(d_scratch);
   float* factor = static_cast<float*>(d_scratch);
-  double* part = reinterpret_cast<double*>(static_cast<uint8_t*>(d_scratch) + 256);
-  for_clip_launches(grads, num_grads, chunk, part, factor, [&](const ClipArgs& A) { k_clip_squares<<<A.blocks, kThreads, 0, st>>>(A); });
-  k_clip_norm<<<1, kClipNormThreads, 0, st>>>(part, parts, scale, max_norm, d_norm, factor);
-  for_clip_launches(grads, num_grads, chunk, part, factor, [&](const ClipArgs& A) { k_clip_scale<<<A.blocks, kThreads, 0, st>>>(A); });
+  double* part = reinterpret_cast<double*>(scratch + S.part);
+  const bool table = S.tensors > kClipTensors;
+  ClipArgs A;
+  A.table = table ? reinterpret_cast<ClipTensor*>(scratch + S.table) : nullptr;
+  A.tensors = S.tensors;
+  A.first = A.here = 0;
+  A.blocks = 0;
+  A.chunk = S.chunk;
+  A.part = part;
+  A.factor = factor;
+  for (int i = 0; i < num_grads; ++i) {
+    const smfg_grad_t& g = grads[i];
+    if (g.numel == 0) continue;
+    if (A.here == kClipTensors) {
+      k_clip_table<<<1, 64, 0, st>>>(A);
+      A.first += A.here;
+      A.here = 0;
+    }
+    A.t[A.here++] = {g.grad, g.out ? g.out : const_cast<void*>(g.grad), g.numel, g.d_rows, g.d_rows ? g.row_elems : 1, A.blocks,
+                     g.dtype | (g.out ? g.out_dtype : g.dtype) << 4};
+    A.blocks += static_cast<uint32_t>(ceil_div(g.numel, S.chunk));
+  }
+  if (table) k_clip_table<<<1, 64, 0, st>>>(A);
+  if (A.blocks > 0) {
+    if (table) k_clip_squares<true><<<A.blocks, kThreads, 0, st>>>(A);
+    else k_clip_squares<false><<<A.blocks, kThreads, 0, st>>>(A);
+  }
+  k_clip_norm<<<1, kClipNormThreads, 0, st>>>(part, S.blocks, scale, max_norm, d_norm, factor);
+  if (A.blocks > 0) {
+    if (table) k_clip_scale<true><<<A.blocks, kThreads, 0, st>>>(A);
+    else k_clip_scale<false><<<A.blocks, kThreads, 0, st>>>(A);
+  }
   return hip_err(hipGetLastError());
 }
 
