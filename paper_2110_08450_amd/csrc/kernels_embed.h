@@ -310,11 +310,17 @@ constexpr int kGradTokens = 16;
 constexpr int kGradWaves = 8;
 constexpr int kGradThreads = 64 * kGradWaves;
 constexpr int kBlockTokens = kGradWaves * kGradTokens;
+// Up to kTinyIds ids are the work of one block a tile of columns, of twice the waves, which sorts them itself: one launch instead of three, or
+// of four for touched rows alone.
+constexpr int kTinyIds = 256;
+constexpr int kTinyThreads = 1024;
 constexpr int kRunTile = 1024;     // a multiple of every block's tokens
 constexpr int kScanTiles = 1024;   // more run tiles than that are scanned by a launch of their own
 constexpr int grad_columns(int dim) { return dim <= 64 ? 1 : dim <= 128 ? 2 : 4; }
 
 struct EmbedGradArgs {
+  const void* ids;         // for up to kTinyIds of them
+  int32_t id_bytes;
   const uint2* sorted;     // (row, token)
   const int64_t* num;
   int64_t max_ids;
@@ -425,16 +431,25 @@ __device__ __forceinline__ int64_t wave_sorted_bound(const uint2* sorted, int64_
 }
 
 // Rows of the whole table's gradient that no token names: zeros.
-template <typename TG, int V>
+template <typename TG, int V, bool TINY>
 __device__ __forceinline__ void clear_rows(const EmbedGradArgs& A, int64_t n, uint32_t block, uint32_t* lds) {
   const int64_t r0 = static_cast<int64_t>(block) * A.clear_rows;
   const int rows = static_cast<int>(A.num_rows - r0 < A.clear_rows ? A.num_rows - r0 : A.clear_rows);
-  const int64_t lo = wave_sorted_bound(A.sorted, 0, n, static_cast<uint32_t>(r0));
-  const int64_t hi = wave_sorted_bound(A.sorted, lo, n, static_cast<uint32_t>(r0 + rows));
-  if (static_cast<int>(threadIdx.x) < rows) {
-    const uint32_t key = static_cast<uint32_t>(r0) + threadIdx.x;
-    const int64_t p = sorted_bound(A.sorted, lo, hi, key);
-    lds[threadIdx.x] = p < hi && A.sorted[p].x == key;
+  if constexpr (TINY) {
+    if (static_cast<int>(threadIdx.x) < rows) lds[threadIdx.x] = 0;
+    __syncthreads();
+    if (threadIdx.x < n) {
+      const int64_t at = static_cast<int64_t>(row_of_id(A.ids, A.id_bytes, threadIdx.x, A.num_rows)) - r0;
+      if (at >= 0 && at < rows) lds[at] = 1;
+    }
+  } else {
+    const int64_t lo = wave_sorted_bound(A.sorted, 0, n, static_cast<uint32_t>(r0));
+    const int64_t hi = wave_sorted_bound(A.sorted, lo, n, static_cast<uint32_t>(r0 + rows));
+    if (static_cast<int>(threadIdx.x) < rows) {
+      const uint32_t key = static_cast<uint32_t>(r0) + threadIdx.x;
+      const int64_t p = sorted_bound(A.sorted, lo, hi, key);
+      lds[threadIdx.x] = p < hi && A.sorted[p].x == key;
+    }
   }
   __syncthreads();
   const uint32_t per_row = static_cast<uint32_t>((A.dim + V - 1) / V);
@@ -445,15 +460,40 @@ __device__ __forceinline__ void clear_rows(const EmbedGradArgs& A, int64_t n, ui
   }
 }
 
-template <typename TD, typename TG, int V>
-__global__ void __launch_bounds__(kGradThreads) k_embed_sums(EmbedGradArgs A) {
-  __shared__ float heads[kGradWaves][64 * V];
-  __shared__ uint32_t goes_on[kGradWaves];  // the wave's tokens are all of one run, that began before them and goes on behind them
-  __shared__ uint32_t lds[kGradThreads];
+// The ids in sorted[1 ..], between two entries that stand for no row.  By the block: four threads a token compare its row with a quarter of the others each.
+__device__ __forceinline__ void sort_tiny(const EmbedGradArgs& A, int n, uint2* sorted, uint32_t* keys, uint32_t (*smaller)[kTinyIds]) {
+  const uint32_t none = static_cast<uint32_t>(A.num_rows);
+  const int i = threadIdx.x % kTinyIds, quarter = threadIdx.x / kTinyIds;
+  if (quarter == 0) {
+    const uint32_t key = row_of_id(A.ids, A.id_bytes, i < A.max_ids ? i : 0, A.num_rows);
+    keys[i] = i < n ? key : none;
+  }
+  if (threadIdx.x == 0) sorted[0] = sorted[kTinyIds + 1] = make_uint2(none, 0);
+  __syncthreads();
+  const uint32_t key = keys[i];
+  uint32_t count = 0;
+#pragma unroll 8
+  for (int q = 0; q < kTinyIds / 4; ++q) {
+    const int j = quarter * (kTinyIds / 4) + q;
+    const uint32_t k = keys[j];
+    count += (k < key) | ((k == key) & (j < i)) ? 1u : 0u;
+  }
+  smaller[quarter][i] = count;
+  __syncthreads();
+  if (quarter == 0) sorted[1 + smaller[0][i] + smaller[1][i] + smaller[2][i] + smaller[3][i]] = make_uint2(key, i < n ? static_cast<uint32_t>(i) : 0u);
+  __syncthreads();
+}
+
+template <typename TD, typename TG, int V, bool TINY>
+__global__ void __launch_bounds__(TINY ? kTinyThreads : kGradThreads) k_embed_sums(EmbedGradArgs A) {
+  constexpr int kWaves = (TINY ? kTinyThreads : kGradThreads) / 64;
+  __shared__ float heads[kWaves][64 * V];
+  __shared__ uint32_t goes_on[kWaves];  // the wave's tokens are all of one run, that began before them and goes on behind them
+  __shared__ uint32_t lds[kWaves * 64];
   const uint32_t tile = blockIdx.x / A.sum_blocks, block = blockIdx.x - tile * A.sum_blocks;
   const int64_t n = count_of(A.num, A.max_ids);
   if (tile >= A.tiles) {
-    clear_rows<TG, V>(A, n, blockIdx.x - A.sum_blocks * A.tiles, lds);
+    clear_rows<TG, V, TINY>(A, n, blockIdx.x - A.sum_blocks * A.tiles, lds);
     return;
   }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -462,11 +502,19 @@ __global__ void __launch_bounds__(kGradThreads) k_embed_sums(EmbedGradArgs A) {
   const int index = static_cast<int>(tile) * 64 + lane;
   const Columns<V> c(index, A.dim);
   // the wave's tokens, one to a lane, from lane 1 on; lane 0 has the one before, lane kGradTokens + 1 the one behind
-  const int64_t at = p0 - 1 + lane;
-  uint2 mine = A.sorted[at < 0 ? 0 : at < A.max_ids ? at : A.max_ids - 1];
-  if (lane > kGradTokens + 1 || at < 0 || at >= n) mine = make_uint2(none, 0);
+  uint2 mine;
   uint32_t rank = 0, all = 0;
-  if (A.row_ids) rank = share_of_runs(A, block, all);
+  if constexpr (TINY) {
+    __shared__ uint2 sorted[kTinyIds + 2];
+    __shared__ uint32_t keys[kTinyIds], smaller[4][kTinyIds];
+    sort_tiny(A, static_cast<int>(n), sorted, keys, smaller);
+    mine = lane <= kGradTokens + 1 ? sorted[wave * kGradTokens + lane] : make_uint2(none, 0);
+  } else {
+    const int64_t at = p0 - 1 + lane;
+    mine = A.sorted[at < 0 ? 0 : at < A.max_ids ? at : A.max_ids - 1];
+    if (lane > kGradTokens + 1 || at < 0 || at >= n) mine = make_uint2(none, 0);
+    if (A.row_ids) rank = share_of_runs(A, block, all);
+  }
   // Every row is read, also a padded place's and for columns that there are not (the last ones again), and dropped later: loads under a
   // condition are waited for one by one.  Token 0 stands for those behind the last.
   const TD* dy = static_cast<const TD*>(A.dy);
@@ -480,24 +528,26 @@ __global__ void __launch_bounds__(kGradThreads) k_embed_sums(EmbedGradArgs A) {
     const uint32_t left = __shfl_up(mine.x, 1, 64);  // by all lanes: not in the condition
     const bool begins = lane >= 1 && lane <= kGradTokens && mine.x < none && mine.x != left;
     const uint64_t set = __ballot(begins);
+    if constexpr (!TINY) {
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      rank += __shfl_xor(rank, o, 64);
-      if (block == 0) all += __shfl_xor(all, o, 64);
+      for (int o = 1; o < 64; o <<= 1) {
+        rank += __shfl_xor(rank, o, 64);
+        if (block == 0) all += __shfl_xor(all, o, 64);
+      }
     }
     if (lane == 0) {
       lds[wave] = rank;
-      lds[kGradWaves + wave] = all;
-      lds[2 * kGradWaves + wave] = __popcll(set);
+      lds[kWaves + wave] = TINY ? __popcll(set) : all;
+      lds[2 * kWaves + wave] = __popcll(set);
     }
     __syncthreads();
     rank = all = 0;
-    for (int w = 0; w < kGradWaves; ++w) {
-      rank += lds[w] + (w < wave ? lds[2 * kGradWaves + w] : 0u);
-      all += lds[kGradWaves + w];
+    for (int w = 0; w < kWaves; ++w) {
+      rank += lds[w] + (w < wave ? lds[2 * kWaves + w] : 0u);
+      all += lds[kWaves + w];
     }
     rank = __builtin_amdgcn_readfirstlane(rank);
-    if (blockIdx.x == 0 && threadIdx.x == 0 && !A.scanned) *A.num_unique = all;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && (TINY || !A.scanned)) *A.num_unique = all;
     if (begins && tile == 0) A.row_ids[rank + __popcll(set & ((1ull << lane) - 1))] = static_cast<int32_t>(mine.x);
   }
   if (b0 >= n) return;
@@ -535,12 +585,12 @@ __global__ void __launch_bounds__(kGradThreads) k_embed_sums(EmbedGradArgs A) {
   // the run that goes on behind the wave's tokens, unless it began before them
   if (open && !head) {
     int w = wave + 1;
-    for (; w < kGradWaves; ++w) {
+    for (; w < kWaves; ++w) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[j] += heads[w][j * 64 + lane];
       if (!goes_on[w]) break;
     }
-    if (w < kGradWaves) {
+    if (w < kWaves) {
       write_grad<TG, V>(A, A.row_ids ? static_cast<int64_t>(rank) : static_cast<int64_t>(key), c, sum);
     } else {
 #pragma unroll
@@ -552,7 +602,7 @@ __global__ void __launch_bounds__(kGradThreads) k_embed_sums(EmbedGradArgs A) {
   if (wave == 0 && began_before) {
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = heads[0][j * 64 + lane];
-    for (int w = 0; w + 1 < kGradWaves && goes_on[w]; ++w) {
+    for (int w = 0; w + 1 < kWaves && goes_on[w]; ++w) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[j] += heads[w + 1][j * 64 + lane];
     }

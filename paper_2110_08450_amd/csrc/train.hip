@@ -122,9 +122,15 @@ void launch_embed_sums(EmbedGradArgs A, const GradShape& G, bool clear, hipStrea
   // a block clears about 32 KiB, of at most a row a thread
   const int64_t rows = (32 << 10) / (A.dim * static_cast<int64_t>(sizeof(TG)));
   A.clear_rows = static_cast<int32_t>(rows < 1 ? 1 : rows > kGradThreads ? kGradThreads : rows);
-  const int64_t blocks = G.blocks * G.tiles + (clear ? ceil_div(A.num_rows, A.clear_rows) : 0);
+  const bool tiny = A.max_ids <= kTinyIds;
+  if (tiny) A.sum_blocks = 1;
+  const int64_t blocks = static_cast<int64_t>(A.sum_blocks) * A.tiles + (clear ? ceil_div(A.num_rows, A.clear_rows) : 0);
   if (blocks == 0) return;
-  k_embed_sums<TD, TG, V><<<static_cast<unsigned>(blocks), kGradThreads, 0, st>>>(A);
+  if (tiny) {
+    k_embed_sums<TD, TG, V, true><<<static_cast<unsigned>(blocks), kTinyThreads, 0, st>>>(A);
+    return;
+  }
+  k_embed_sums<TD, TG, V, false><<<static_cast<unsigned>(blocks), kGradThreads, 0, st>>>(A);
   if (G.blocks < 2) return;
   const uint32_t joins = static_cast<uint32_t>(ceil_div(G.blocks, kJoinWaves));
   const unsigned longs = static_cast<unsigned>((G.blocks - 1) / kJoinShort);
@@ -174,10 +180,13 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
   A.block_runs = reinterpret_cast<uint32_t*>(scratch + S.block_runs);
   A.tail_rank = reinterpret_cast<uint32_t*>(scratch + S.tail_rank);
   A.run_tiles = S.run_tiles;
-  if (max_ids > 0) A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, st);
-  if (rows_only) {
+  A.ids = d_ids;
+  A.id_bytes = id_bytes;
+  const bool tiny = max_ids <= kTinyIds;
+  if (!tiny) A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, st);
+  if (rows_only && (max_ids == 0 || !tiny)) {
     if (max_ids > 0) k_embed_runs<<<static_cast<unsigned>(S.run_tiles), kThreads, 0, st>>>(A);
-    A.scanned = S.run_tiles == 0 || S.run_tiles > kScanTiles;
+    A.scanned = max_ids == 0 || S.run_tiles > kScanTiles;
     if (A.scanned) k_embed_scan<<<1, kThreads, 0, st>>>(A);
   }
   with_type(dy_dtype, [&](auto t) {
@@ -435,6 +444,9 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
   A.chunk = S.chunk;
   A.part = part;
   A.factor = factor;
+  A.norm = d_norm;
+  A.scale = scale;
+  A.max_norm = max_norm;
   for (int i = 0; i < num_grads; ++i) {
     const smfg_grad_t& g = grads[i];
     if (g.numel == 0) continue;
@@ -452,7 +464,7 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
     if (table) k_clip_squares<true><<<A.blocks, kThreads, 0, st>>>(A);
     else k_clip_squares<false><<<A.blocks, kThreads, 0, st>>>(A);
   }
-  k_clip_norm<<<1, kClipNormThreads, 0, st>>>(part, S.blocks, scale, max_norm, d_norm, factor);
+  if (A.blocks == 0 || A.blocks > kClipJoin) k_clip_norm<<<1, kClipNormThreads, 0, st>>>(A);
   if (A.blocks > 0) {
     if (table) k_clip_scale<true><<<A.blocks, kThreads, 0, st>>>(A);
     else k_clip_scale<false><<<A.blocks, kThreads, 0, st>>>(A);
