@@ -390,21 +390,30 @@ __device__ __forceinline__ uint32_t share_of_runs(const EmbedGradArgs& A, uint32
   return x;
 }
 
-// V columns of a row of the gradient from their sum; those that the vector before has as well are left to it.
+// V columns of a row of the gradient from their sum and, where it is added to, what they hold; those that the vector before has as well are
+// left to it.
 template <typename TG, int V>
-__device__ __forceinline__ void write_grad(const EmbedGradArgs& A, int64_t row, const Columns<V>& c, const float (&sum)[V]) {
-  TG* g = static_cast<TG*>(A.grad) + row * A.grad_stride + c.start;
-  if (c.dup == 0) {
-    Elems<TG, V> e = {};
-    if (A.accumulate) e = *reinterpret_cast<const Elems<TG, V>*>(g);
+__device__ __forceinline__ TG* grad_at(const EmbedGradArgs& A, int64_t row, const Columns<V>& c) {
+  return static_cast<TG*>(A.grad) + row * A.grad_stride + c.start;
+}
+template <typename TG, int V>
+__device__ __forceinline__ void write_grad(const EmbedGradArgs& A, int64_t row, const Columns<V>& c, const float (&sum)[V], Elems<TG, V> e) {
+  TG* g = grad_at<TG, V>(A, row, c);
 #pragma unroll
-    for (int j = 0; j < V; ++j) e.v[j] = from_float<TG>(as_float(e.v[j]) + A.scale * sum[j]);
+  for (int j = 0; j < V; ++j) e.v[j] = from_float<TG>(as_float(e.v[j]) + A.scale * sum[j]);
+  if (c.dup == 0) {
     *reinterpret_cast<Elems<TG, V>*>(g) = e;
   } else if (c.dup < V) {
 #pragma unroll
     for (int j = 0; j < V; ++j)
-      if (j >= c.dup) g[j] = from_float<TG>((A.accumulate ? as_float(g[j]) : 0.f) + A.scale * sum[j]);
+      if (j >= c.dup) g[j] = e.v[j];
   }
+}
+template <typename TG, int V>
+__device__ __forceinline__ void write_grad(const EmbedGradArgs& A, int64_t row, const Columns<V>& c, const float (&sum)[V]) {
+  Elems<TG, V> e = {};
+  if (A.accumulate) e = *reinterpret_cast<const Elems<TG, V>*>(grad_at<TG, V>(A, row, c));
+  write_grad<TG, V>(A, row, c, sum, e);
 }
 
 // First sorted place whose row is at least `key`, in [lo, hi].
@@ -484,7 +493,9 @@ __device__ __forceinline__ void sort_tiny(const EmbedGradArgs& A, int n, uint2* 
   __syncthreads();
 }
 
-template <typename TD, typename TG, int V, bool TINY>
+// ADD: the sums are added to what the rows hold, which is asked for a few tokens ahead, whether a token ends a run or not: asked for only where
+// one does, every row was waited for in turn.  (No other wave writes a row that a run of this one ends in.)
+template <typename TD, typename TG, int V, bool TINY, bool ADD>
 __global__ void __launch_bounds__(TINY ? kTinyThreads : kGradThreads) k_embed_sums(EmbedGradArgs A) {
   constexpr int kWaves = (TINY ? kTinyThreads : kGradThreads) / 64;
   __shared__ float heads[kWaves][64 * V];
@@ -556,8 +567,19 @@ __global__ void __launch_bounds__(TINY ? kTinyThreads : kGradThreads) k_embed_su
   const bool began_before = first < none && first == before, open = key < none && key == behind;
   bool head = began_before;
   float sum[V] = {};
+  constexpr int kAhead = kGradTokens / V;  // 16 registers of rows that are added to
+  Elems<TG, V> held[ADD ? kAhead : 1];
 #pragma unroll
   for (int u = 0; u < kGradTokens; ++u) {
+    if constexpr (ADD) {
+      if (u % kAhead == 0) {
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+          const uint32_t row = __builtin_amdgcn_readlane(mine.x, u + q + 1);
+          held[q] = *reinterpret_cast<const Elems<TG, V>*>(grad_at<TG, V>(A, row < none ? row : 0u, c));
+        }
+      }
+    }
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] += as_float(e[u].v[j]);
     const uint32_t here = __builtin_amdgcn_readlane(mine.x, u + 1), next = __builtin_amdgcn_readlane(mine.x, u + 2);
@@ -567,7 +589,9 @@ __global__ void __launch_bounds__(TINY ? kTinyThreads : kGradThreads) k_embed_su
 #pragma unroll
         for (int j = 0; j < V; ++j) heads[wave][j * 64 + lane] = sum[j];
       } else {
-        write_grad<TG, V>(A, A.row_ids ? static_cast<int64_t>(rank++) : static_cast<int64_t>(here), c, sum);
+        const int64_t row = A.row_ids ? static_cast<int64_t>(rank++) : static_cast<int64_t>(here);
+        if constexpr (ADD) write_grad<TG, V>(A, row, c, sum, held[u % kAhead]);
+        else write_grad<TG, V>(A, row, c, sum, {});
       }
     }
     head = false;

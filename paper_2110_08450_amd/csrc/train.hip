@@ -126,11 +126,14 @@ void launch_embed_sums(EmbedGradArgs A, const GradShape& G, bool clear, hipStrea
   if (tiny) A.sum_blocks = 1;
   const int64_t blocks = static_cast<int64_t>(A.sum_blocks) * A.tiles + (clear ? ceil_div(A.num_rows, A.clear_rows) : 0);
   if (blocks == 0) return;
+  const unsigned b = static_cast<unsigned>(blocks);
   if (tiny) {
-    k_embed_sums<TD, TG, V, true><<<static_cast<unsigned>(blocks), kTinyThreads, 0, st>>>(A);
+    if (A.accumulate) k_embed_sums<TD, TG, V, true, true><<<b, kTinyThreads, 0, st>>>(A);
+    else k_embed_sums<TD, TG, V, true, false><<<b, kTinyThreads, 0, st>>>(A);
     return;
   }
-  k_embed_sums<TD, TG, V, false><<<static_cast<unsigned>(blocks), kGradThreads, 0, st>>>(A);
+  if (A.accumulate) k_embed_sums<TD, TG, V, false, true><<<b, kGradThreads, 0, st>>>(A);
+  else k_embed_sums<TD, TG, V, false, false><<<b, kGradThreads, 0, st>>>(A);
   if (G.blocks < 2) return;
   const uint32_t joins = static_cast<uint32_t>(ceil_div(G.blocks, kJoinWaves));
   const unsigned longs = static_cast<unsigned>((G.blocks - 1) / kJoinShort);
