@@ -237,12 +237,14 @@ struct LaunchNorm {
   }
 };
 
-// Blocks, and slices of the weight's gradient, of the launch over max_rows rows of dim columns: the most that 16 MiB of sums hold.
-constexpr int kNormSlices = 1024;
+// Slices of the weight's gradient.  Rows in registers: the blocks of the launch, 16 MiB of sums, but 256 to 1024 (16 K rows of 4096 in 128 blocks
+// 169 us, 256 131, 512 with the next row on its way 80).  Longer rows: 64 at most, as the columns alone are many threads.
+constexpr int kNormSlices = 1024, kNormLongSlices = 64, kNormLongDim = 16384;
 int64_t norm_slices(int64_t max_rows, int32_t dim) {
   int64_t s = (int64_t(16) << 20) / (8 * static_cast<int64_t>(dim));
-  if (s < 256) s = 256;
-  if (s > kNormSlices) s = kNormSlices;
+  const int64_t least = dim <= kNormLongDim ? 256 : 1, most = dim <= kNormLongDim ? kNormSlices : kNormLongSlices;
+  if (s < least) s = least;
+  if (s > most) s = most;
   return s < max_rows ? s : max_rows;
 }
 
@@ -403,7 +405,7 @@ int smfg_layer_norm_grad(const void* d_dy, int64_t dy_stride, const void* d_x, i
       constexpr int V = kVec<T>;
       if (with_row_shape<T, sizeof(T) == 4 ? 2048 : 1536>(dim, LaunchNormGrad<T>{A, slices, st})) return;
       if (sums) {
-        if (slices > 64) slices = 64;
+        if (slices > kNormLongSlices) slices = kNormLongSlices;
         k_norm_grad_columns<T, V><<<dim3(static_cast<unsigned>(ceil_div(ceil_div(dim, V), kThreads)), static_cast<unsigned>(slices)), kThreads, 0, st>>>(A);
       }
       if (d_dx) k_layer_norm_grad_long<T, V><<<static_cast<unsigned>(max_rows), kThreads, 0, st>>>(A);
