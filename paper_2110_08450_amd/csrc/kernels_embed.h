@@ -74,8 +74,9 @@ __global__ void __launch_bounds__(kThreads) k_embedding(EmbedArgs A) {
 //
 // Up to kSmallSort ids: every token counts the ids that belong before its own, in one launch.  More: digits of at most kSortBits
 // bits from the lowest on, a launch that counts the digits of every tile and one that scatters.  Up to kSortColumns tiles the block
-// that scatters adds up the counts of all tiles itself (118 tiles of 4096: 1.5 us instead of the 3 to 5 of another launch); more
-// of them are scanned by a launch between the two.
+// that scatters adds up the counts of all tiles itself; more of them are scanned by a launch between the two.  A thread has TURNS
+// records of a tile, two as long as the tiles are few enough then, else four: a digit of 16 K, 154 K and 480 K ids 8.8, 10.3 and 14.9 us with two,
+// 10.9, 12.8 and 16.4 with four, of 900 K 17.2 with four, 28 with two that add up 440 tiles.
 struct SortArgs {
   const void* ids;      // first digit: the ids
   int32_t id_bytes;
@@ -86,7 +87,8 @@ struct SortArgs {
   const uint2* in;      // other digits: (row, token)
   uint2* out;
   uint16_t* hist;       // [tiles][bins]
-  uint32_t* starts;     // [tiles][bins] where a tile's records of a digit begin, if scanned
+  uint32_t* starts;     // [tiles][bins] records of a digit in the tiles before, if scanned
+  uint32_t* totals;     // [bins] records of a digit, if scanned
   int32_t tiles;
 };
 
@@ -144,13 +146,13 @@ static __global__ void __launch_bounds__(kSmallThreads) k_sort_small(SortArgs A)
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortTurns = 4;
-constexpr int kSortTile = kSortThreads * kSortTurns;
 constexpr int kSortBits = 9;
 constexpr int kSortBins = 1 << kSortBits;
 constexpr int kSortColumns = 256;
 
-static __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs A) {
+template <int TURNS>
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs A) {
+  constexpr int kSortTurns = TURNS, kSortTile = kSortThreads * TURNS;
   __shared__ uint32_t count[kSortBins];
   const int64_t n = count_of(A.num, A.max_ids);
   const int bins = 1 << A.bits;
@@ -171,48 +173,49 @@ static __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs A) 
     A.hist[static_cast<int64_t>(blockIdx.x) * bins + threadIdx.x] = static_cast<uint16_t>(count[threadIdx.x]);
 }
 
-// Where the records of every tile and digit begin: a block has 64 digits, its waves take turns of tiles.  Two passes over the counts: totals of
-// the digits (every block those of all digits), then the running sums.
+// Records of every digit in the tiles before each, and in all of them: a block has kScanPairs pairs of digits, 64 groups of threads a range of the
+// tiles each, whose counts are read once for their sum and once for the running one.
+constexpr int kScanPairs = 16;
 static __global__ void __launch_bounds__(kSortThreads) k_sort_scan(SortArgs A) {
-  __shared__ uint32_t lds[kSortWaves], sums[kSortWaves][64], begin[kSortBins];
-  const int bins = 1 << A.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t all = 0;
-  for (int d0 = 0; d0 < bins; d0 += 64) {
-    uint32_t s = 0;
-    const int d = d0 + lane;
-    for (int64_t t = wave; t < A.tiles; t += kSortWaves) s += d < bins ? A.hist[t * bins + d] : 0u;
-    __syncthreads();
-    sums[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && d < bins) {
-      s = 0;
-      for (int w = 0; w < kSortWaves; ++w) s += sums[w][lane];
-      begin[d] = s;
-    }
+  static_assert(kSortThreads / kScanPairs == 64, "the groups' sums are scanned by a wave");
+  __shared__ uint32_t sums[64][2 * kScanPairs + 1];
+  const int pairs = (1 << A.bits) / 2, pair = static_cast<int>(blockIdx.x) * kScanPairs + static_cast<int>(threadIdx.x) % kScanPairs;
+  const int group = static_cast<int>(threadIdx.x) / kScanPairs, here = static_cast<int>(threadIdx.x) % kScanPairs;
+  const int64_t each = (A.tiles + 63) / 64, from = group * each, to = from + each < A.tiles ? from + each : A.tiles;
+  const uint32_t* hist = reinterpret_cast<const uint32_t*>(A.hist) + (pair < pairs ? pair : 0);
+  uint32_t s0 = 0, s1 = 0;
+#pragma unroll 8
+  for (int64_t t = from; t < to; ++t) {
+    const uint32_t c = hist[t * pairs];
+    s0 += c & 0xFFFFu;
+    s1 += c >> 16;
+  }
+  sums[group][2 * here] = s0;
+  sums[group][2 * here + 1] = s1;
+  __syncthreads();
+  const int lane = threadIdx.x & 63;
+  for (int d = threadIdx.x >> 6; d < 2 * kScanPairs; d += kSortWaves) {
+    const uint32_t s = sums[lane][d], in = wave_inscan(s);
+    sums[lane][d] = in - s;
+    const int digit = static_cast<int>(blockIdx.x) * 2 * kScanPairs + d;
+    if (lane == 63 && digit < 2 * pairs) A.totals[digit] = in;
   }
   __syncthreads();
-  const uint32_t ex = block_exscan<kSortThreads>(static_cast<int>(threadIdx.x) < bins ? begin[threadIdx.x] : 0u, lds, all);
-  __syncthreads();
-  if (static_cast<int>(threadIdx.x) < bins) begin[threadIdx.x] = ex;
-  __syncthreads();
-  const int d = static_cast<int>(blockIdx.x) * 64 + lane;
-  uint32_t at = d < bins ? begin[d] : 0u;
-  for (int64_t t0 = 0; t0 < A.tiles; t0 += kSortWaves) {
-    const int64_t t = t0 + wave;
-    const uint32_t c = t < A.tiles && d < bins ? A.hist[t * bins + d] : 0u;
-    __syncthreads();
-    sums[wave][lane] = c;
-    __syncthreads();
-    uint32_t here = at;
-    for (int w = 0; w < kSortWaves; ++w) {
-      if (w < wave) here += sums[w][lane];
-      at += sums[w][lane];
-    }
-    if (t < A.tiles && d < bins) A.starts[t * bins + d] = here;
+  if (pair >= pairs) return;
+  s0 = sums[group][2 * here];
+  s1 = sums[group][2 * here + 1];
+#pragma unroll 8
+  for (int64_t t = from; t < to; ++t) {
+    const uint32_t c = hist[t * pairs];
+    reinterpret_cast<uint2*>(A.starts)[t * pairs + pair] = make_uint2(s0, s1);
+    s0 += c & 0xFFFFu;
+    s1 += c >> 16;
   }
 }
 
-static __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs A) {
+template <int TURNS>
+__global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs A) {
+  constexpr int kSortTurns = TURNS, kSortTile = kSortThreads * TURNS;
   __shared__ uint32_t next[kSortWaves][kSortBins];  // records of a wave so far, later where in the tile its next record goes
   __shared__ union {
     uint32_t sums[kSortWaves][2 * kSortBins];
@@ -234,7 +237,7 @@ static __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs A
   if (base >= n) return;
   // where the tile's records of a digit begin: behind all smaller digits, and those of the tiles before; in pairs of digits, the tiles
   // dealt to groups of threads
-  uint32_t at = 0;
+  uint32_t at = 0, all = 0;
   const int pairs = bins / 2, groups = kSortThreads / pairs < kSortWaves ? kSortThreads / pairs : kSortWaves;
   if (!A.starts) {
     const int pair = static_cast<int>(threadIdx.x) % pairs, group = static_cast<int>(threadIdx.x) / pairs;
@@ -256,6 +259,7 @@ static __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs A
     }
   } else if (static_cast<int>(threadIdx.x) < bins) {
     at = A.starts[static_cast<int64_t>(blockIdx.x) * bins + threadIdx.x];
+    all = A.totals[threadIdx.x];
   }
   __syncthreads();
   // its rank among equal digits of the wave
@@ -264,8 +268,8 @@ static __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs A
   for (int k = 0; k < kSortTurns; ++k) {
     const bool live = base + (wave * kSortTurns + k) * 64 + lane < n;
     const uint32_t digit = (rec[k].x >> A.shift) & (bins - 1);
-    const uint64_t all = __ballot(live);
-    uint32_t same0 = static_cast<uint32_t>(all), same1 = static_cast<uint32_t>(all >> 32);
+    const uint64_t lives = __ballot(live);
+    uint32_t same0 = static_cast<uint32_t>(lives), same1 = static_cast<uint32_t>(lives >> 32);
 #pragma unroll
     for (int b = 0; b < kSortBits; ++b) {  // a bit that no digit has changes nothing
       const uint64_t set = __ballot(digit & (1u << b));
@@ -281,7 +285,6 @@ static __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs A
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
   __syncthreads();  // a digit's records are those of all waves
-  uint32_t all = 0;
   if (!A.starts && static_cast<int>(threadIdx.x) < bins)
     for (int g = 0; g < groups; ++g) {
       all += s.sums[g][threadIdx.x];

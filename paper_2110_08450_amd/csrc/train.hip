@@ -58,12 +58,14 @@ GradShape grad_shape(int64_t max_ids, int32_t dim) {
 }
 
 struct EmbedScratch {
-  int64_t rec[2], hist, starts, part, tile_runs, block_runs, tail_rank, bytes;
+  int64_t rec[2], hist, starts, totals, part, tile_runs, block_runs, tail_rank, bytes;
   int64_t tiles, run_tiles;
+  int turns;
 };
 EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
   EmbedScratch S;
-  S.tiles = ceil_div(max_ids, kSortTile);
+  S.turns = max_ids <= 2 * kSortThreads * kSortColumns ? 2 : 4;
+  S.tiles = ceil_div(max_ids, S.turns * kSortThreads);
   S.run_tiles = ceil_div(max_ids, kRunTile);
   const GradShape G = grad_shape(max_ids, dim);
   int64_t at = 0;
@@ -76,6 +78,7 @@ EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
   S.rec[1] = take(8 * max_ids);
   S.hist = take(max_ids > kSmallSort ? 2 * kSortBins * S.tiles : 0);
   S.starts = take(S.tiles > kSortColumns ? 4 * kSortBins * S.tiles : 0);
+  S.totals = take(4 * kSortBins);
   S.part = take(4 * 2 * G.blocks * G.width);
   S.tile_runs = take(4 * S.run_tiles);
   S.block_runs = take(4 * G.blocks);
@@ -96,6 +99,7 @@ const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* id
   A.hist = reinterpret_cast<uint16_t*>(scratch + S.hist);
   A.tiles = static_cast<int32_t>(S.tiles);
   if (S.tiles > kSortColumns) A.starts = reinterpret_cast<uint32_t*>(scratch + S.starts);
+  A.totals = reinterpret_cast<uint32_t*>(scratch + S.totals);
   A.out = reinterpret_cast<uint2*>(scratch + S.rec[0]);
   if (max_ids <= kSmallSort) {
     k_sort_small<<<static_cast<unsigned>(ceil_div(max_ids, kSmallTokens)), kSmallThreads, 0, st>>>(A);
@@ -107,9 +111,12 @@ const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* id
   A.bits = (key_bits + passes - 1) / passes;
   for (int p = 0; p < passes; ++p, A.shift += A.bits) {
     A.out = reinterpret_cast<uint2*>(scratch + S.rec[p & 1]);
-    k_sort_count<<<static_cast<unsigned>(S.tiles), kSortThreads, 0, st>>>(A);
-    if (A.starts) k_sort_scan<<<static_cast<unsigned>(ceil_div(1 << A.bits, 64)), kSortThreads, 0, st>>>(A);
-    k_sort_scatter<<<static_cast<unsigned>(S.tiles), kSortThreads, 0, st>>>(A);
+    const unsigned tiles = static_cast<unsigned>(S.tiles);
+    if (S.turns == 2) k_sort_count<2><<<tiles, kSortThreads, 0, st>>>(A);
+    else k_sort_count<4><<<tiles, kSortThreads, 0, st>>>(A);
+    if (A.starts) k_sort_scan<<<static_cast<unsigned>(ceil_div(1 << A.bits, 2 * kScanPairs)), kSortThreads, 0, st>>>(A);
+    if (S.turns == 2) k_sort_scatter<2><<<tiles, kSortThreads, 0, st>>>(A);
+    else k_sort_scatter<4><<<tiles, kSortThreads, 0, st>>>(A);
     A.in = A.out;
   }
   return A.in;
