@@ -90,7 +90,30 @@ struct SortArgs {
   uint32_t* starts;     // [tiles][bins] records of a digit in the tiles before, if scanned
   uint32_t* totals;     // [bins] records of a digit, if scanned
   int32_t tiles;
+  // rows of the whole table's gradient that the blocks behind the sort's own set to zero meanwhile, in units of 2 bytes
+  uint32_t own_blocks;
+  uint16_t* clear;
+  int64_t clear_rows, clear_width, clear_stride;
 };
+
+// The sort leaves most of the chip idle and waits for memory, so part of the gradient is cleared beside each of its launches, where most rows
+// are untouched (see early_clear): 16 K tokens of 1024 columns into 50 K rows of floats 72.6 -> 69.0 us, 300 K of 64 into 2 M 172 -> 149.  A block has every gridDim - own_blocks-th
+// vector, or row where rows are apart.
+__device__ __forceinline__ void clear_beside(const SortArgs& A) {
+  typedef Elems<uint16_t, 8> Vector;
+  const uint32_t block = blockIdx.x - A.own_blocks, blocks = gridDim.x - A.own_blocks;
+  const bool whole = A.clear_stride == A.clear_width;  // one long row
+  const int64_t rows = whole ? 1 : A.clear_rows, width = whole ? A.clear_width * A.clear_rows : A.clear_width;
+  const int64_t step = static_cast<int64_t>(whole ? blocks : 1u) * blockDim.x, first = static_cast<int64_t>(whole ? block : 0u) * blockDim.x + threadIdx.x;
+  for (int64_t r = whole ? 0 : block; r < rows; r += blocks) {
+    uint16_t* row = A.clear + r * A.clear_stride;
+    if (width >= 8) {
+      for (int64_t i = first; i * 8 < width; i += step) *reinterpret_cast<Vector*>(row + (i * 8 + 8 <= width ? i * 8 : width - 8)) = {};
+    } else {
+      for (int64_t i = first; i < width; i += step) row[i] = 0;
+    }
+  }
+}
 
 constexpr int kSmallSort = 8192;
 constexpr int kSmallTokens = 32;   // tokens of a block of k_sort_small
@@ -118,6 +141,7 @@ __device__ __forceinline__ uint32_t count_keys(const uint4* keys, int from, int 
   return c;
 }
 static __global__ void __launch_bounds__(kSmallThreads) k_sort_small(SortArgs A) {
+  if (blockIdx.x >= A.own_blocks) return clear_beside(A);
   __shared__ uint4 keys[kSmallSort / 4];
   __shared__ uint32_t smaller[kSmallShares][kSmallTokens];
   const int n = static_cast<int>(count_of(A.num, A.max_ids));
@@ -152,6 +176,7 @@ constexpr int kSortColumns = 256;
 
 template <int TURNS>
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs A) {
+  if (blockIdx.x >= A.own_blocks) return clear_beside(A);
   constexpr int kSortTurns = TURNS, kSortTile = kSortThreads * TURNS;
   __shared__ uint32_t count[kSortBins];
   const int64_t n = count_of(A.num, A.max_ids);
@@ -215,6 +240,7 @@ static __global__ void __launch_bounds__(kSortThreads) k_sort_scan(SortArgs A) {
 
 template <int TURNS>
 __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs A) {
+  if (blockIdx.x >= A.own_blocks) return clear_beside(A);
   constexpr int kSortTurns = TURNS, kSortTile = kSortThreads * TURNS;
   __shared__ uint32_t next[kSortWaves][kSortBins];  // records of a wave so far, later where in the tile its next record goes
   __shared__ union {

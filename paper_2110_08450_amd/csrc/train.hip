@@ -87,9 +87,29 @@ EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
   return S;
 }
 
+// A matrix to be cleared beside the sort, base null: none.
+struct Clear {
+  void* base;
+  int64_t rows, dim, stride, elem_bytes;
+};
+
+// Blocks of a launch of the sort, with those that clear its share (part of parts) of the matrix: about 64 KiB each.
+unsigned sort_blocks(SortArgs& A, int64_t own, const Clear& c, int part, int parts) {
+  A.own_blocks = static_cast<uint32_t>(own);
+  A.clear = nullptr;
+  if (!c.base) return A.own_blocks;
+  const int64_t units = c.elem_bytes / 2, from = c.rows * part / parts, to = c.rows * (part + 1) / parts;
+  A.clear = static_cast<uint16_t*>(c.base) + from * c.stride * units;
+  A.clear_rows = to - from;
+  A.clear_width = c.dim * units;
+  A.clear_stride = c.stride * units;
+  if (to == from) return A.own_blocks;
+  return A.own_blocks + blocks_for(A.clear_rows * A.clear_width, 32 << 10, 1u << 20);
+}
+
 // (row, token) of the call's ids, sorted by row.  num_rows itself, which stands for no row, is a key as well.
 const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* ids, int32_t id_bytes, const int64_t* num, int64_t max_ids,
-                         int64_t num_rows, hipStream_t st) {
+                         int64_t num_rows, const Clear& clear, hipStream_t st) {
   SortArgs A = {};
   A.ids = ids;
   A.id_bytes = id_bytes;
@@ -102,7 +122,8 @@ const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* id
   A.totals = reinterpret_cast<uint32_t*>(scratch + S.totals);
   A.out = reinterpret_cast<uint2*>(scratch + S.rec[0]);
   if (max_ids <= kSmallSort) {
-    k_sort_small<<<static_cast<unsigned>(ceil_div(max_ids, kSmallTokens)), kSmallThreads, 0, st>>>(A);
+    const unsigned blocks = sort_blocks(A, ceil_div(max_ids, kSmallTokens), clear, 0, 1);
+    k_sort_small<<<blocks, kSmallThreads, 0, st>>>(A);
     return A.out;
   }
   int key_bits = 0;
@@ -111,12 +132,13 @@ const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* id
   A.bits = (key_bits + passes - 1) / passes;
   for (int p = 0; p < passes; ++p, A.shift += A.bits) {
     A.out = reinterpret_cast<uint2*>(scratch + S.rec[p & 1]);
-    const unsigned tiles = static_cast<unsigned>(S.tiles);
-    if (S.turns == 2) k_sort_count<2><<<tiles, kSortThreads, 0, st>>>(A);
-    else k_sort_count<4><<<tiles, kSortThreads, 0, st>>>(A);
+    unsigned blocks = sort_blocks(A, S.tiles, clear, 2 * p, 2 * passes);
+    if (S.turns == 2) k_sort_count<2><<<blocks, kSortThreads, 0, st>>>(A);
+    else k_sort_count<4><<<blocks, kSortThreads, 0, st>>>(A);
     if (A.starts) k_sort_scan<<<static_cast<unsigned>(ceil_div(1 << A.bits, 2 * kScanPairs)), kSortThreads, 0, st>>>(A);
-    if (S.turns == 2) k_sort_scatter<2><<<tiles, kSortThreads, 0, st>>>(A);
-    else k_sort_scatter<4><<<tiles, kSortThreads, 0, st>>>(A);
+    blocks = sort_blocks(A, S.tiles, clear, 2 * p + 1, 2 * passes);
+    if (S.turns == 2) k_sort_scatter<2><<<blocks, kSortThreads, 0, st>>>(A);
+    else k_sort_scatter<4><<<blocks, kSortThreads, 0, st>>>(A);
     A.in = A.out;
   }
   return A.in;
@@ -154,6 +176,10 @@ void launch_embed_grad(const EmbedGradArgs& A, const GradShape& G, bool clear, h
   else if (V == 2) launch_embed_sums<TD, TG, 2>(A, G, clear, st);
   else launch_embed_sums<TD, TG, 4>(A, G, clear, st);
 }
+
+// Is the whole gradient cleared beside the sort, and the touched rows written over?  Else only the untouched ones are, beside the sums.  At most half
+// of the rows are written twice.
+bool early_clear(int64_t max_ids, int64_t num_rows) { return num_rows >= 2 * max_ids; }
 
 int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids, int64_t max_ids, const void* d_dy, int64_t dy_stride,
                    int32_t dy_dtype, int32_t dim, float scale, void* d_grad, int64_t num_rows, int64_t grad_stride, int32_t grad_dtype,
@@ -193,7 +219,13 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
   A.ids = d_ids;
   A.id_bytes = id_bytes;
   const bool tiny = max_ids <= kTinyIds;
-  if (!tiny) A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, st);
+  bool clear = !rows_only && !accumulate;
+  if (!tiny) {
+    const bool early = clear && early_clear(max_ids, num_rows);
+    const Clear c = {early ? d_grad : nullptr, num_rows, dim, grad_stride, type_bytes(grad_dtype)};
+    A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, c, st);
+    clear = clear && !early;
+  }
   if (rows_only && (max_ids == 0 || !tiny)) {
     if (max_ids > 0) k_embed_runs<<<static_cast<unsigned>(S.run_tiles), kThreads, 0, st>>>(A);
     A.scanned = max_ids == 0 || S.run_tiles > kScanTiles;
@@ -201,8 +233,8 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
   }
   with_type(dy_dtype, [&](auto t) {
     using T = decltype(t);
-    if (grad_dtype == SMFG_DTYPE_F32) launch_embed_grad<T, float>(A, G, !rows_only && !accumulate, st);
-    else launch_embed_grad<T, T>(A, G, !rows_only && !accumulate, st);
+    if (grad_dtype == SMFG_DTYPE_F32) launch_embed_grad<T, float>(A, G, clear, st);
+    else launch_embed_grad<T, T>(A, G, clear, st);
   });
   return hip_err(hipGetLastError());
 }
