@@ -120,7 +120,9 @@ GRADS = [(1, 0, 1, 1, F32, F32, "uniform", 0), (5, 3, 9, 3, F16, F32, "uniform",
          (700, 4, 17, 4096, F32, F32, "mixed", 0), (300, 0, 5, 8199, F16, F32, "same", 0), (5000, 0, 999, 128, BF16, BF16, "outside", 0),
          (0, 700, 40, 16, F32, F32, "uniform", 0), (150_000, 0, 4096, 16, F32, F32, "mixed", 0), (260_000, 1, 100, 33, F16, F32, "same", 0),
          (8192, 0, 16_777_217, 8, F32, F32, "uniform", 0), (4100, 3000, 130_000, 12, F16, F32, "backwards", 0),
-         (1_300_000, 5000, 700_000, 4, F32, F32, "mixed", 0), (1_050_000, 0, 3, 2, F16, F32, "uniform", 0)]
+         (1_300_000, 5000, 700_000, 4, F32, F32, "mixed", 0), (1_050_000, 0, 3, 2, F16, F32, "uniform", 0),
+         (600, 3, 5000, 3, F16, F16, "uniform", 1), (700, 0, 1500, 5, BF16, BF16, "mixed", 0), (256, 0, 64, 200, F16, F32, "same", 0),
+         (257, 0, 64, 64, F32, F32, "mixed", 0), (40_000, 0, 90_000, 33, F16, F16, "mixed", 7)]
 
 
 @pytest.mark.parametrize("n,spare,rows,dim,dtype,gtype,kind,pad", GRADS)
@@ -296,6 +298,25 @@ def test_layer_norm_of_constant_rows_and_infinities():
         assert y[2].isnan().all() and y[4].isnan().all()
 
 
+def test_layer_norm_of_rows_2_31_elements_apart():
+    """Row offsets pass 32 bits in elements and in bytes, of the input and of the output."""
+    n, dim, apart = 4, 72, 2 ** 31 + 8
+    buf = torch.empty((n - 1) * apart + dim, dtype=F16, device=DEV)
+    x = buf.as_strided((n, dim), (apart, 1))
+    x.copy_(torch.randn((n, dim), device=DEV, generator=gen(1)).half())
+    want, m, r, tol, _, _ = norm_of(x, torch.ones(dim, device=DEV), torch.zeros(dim, device=DEV), 1e-5)
+    dy = torch.randn((n, dim), device=DEV, generator=gen(2)).half()
+    y, mean, rstd = torch.empty((n, dim), dtype=F16, device=DEV), m.float(), r.float()
+    dx = torch.empty_like(y)
+    smfg.layer_norm_grad(dy, x, count(n), n, None, mean, rstd, dx, None, None, None)
+    wx, _, _, tx, _, _ = norm_grad_of(dy, x, torch.ones(dim, device=DEV), mean, rstd)
+    check(dx, wx, rounded(tx, wx, F16))
+    smfg.layer_norm(x, count(n), n, None, None, 1e-5, y)
+    check(y, want, rounded(tol, want, F16))
+    smfg.layer_norm(x, count(n), n, None, None, 1e-5, x)
+    assert torch.equal(x, y)
+
+
 def norm_grad_of(dy, x, w, mean, rstd):
     """(dx, dw, db, their tolerances before a rounding) in 64 bits, for the given statistics."""
     n, dim = x.shape
@@ -425,6 +446,17 @@ def test_clip_grad_norm_of_counted_rows():
         want = was[:m].double() * (2.0 / (n64 + 1e-6))
         check(g[:m], want, rounded(4 * U * want.abs(), want, F32))
         assert g[m:].isnan().all()
+
+
+def test_clip_grad_norm_of_more_than_2_32_elements():
+    n = 2 ** 32 + 4099
+    g = torch.zeros(n, dtype=F16, device=DEV)
+    at = torch.tensor([0, 2 ** 31 + 1, 2 ** 32, n - 1], device=DEV)
+    g[at] = torch.tensor([3.0, 4.0, 12.0, 84.0], device=DEV).half()  # 85 in all
+    norm = torch.zeros(1, device=DEV)
+    smfg.clip_grad_norm(smfg.grad_list([g]), 42.5, norm)
+    assert abs(float(norm) - 85) <= 2 * U * 85
+    assert g[at].tolist() == [1.5, 2.0, 6.0, 42.0] and int(torch.count_nonzero(g[:2 ** 31])) == 1 and int(torch.count_nonzero(g[2 ** 31:])) == 3
 
 
 def test_clip_grad_norm_of_large_infinite_and_nan_gradients():
