@@ -30,7 +30,9 @@ struct EmbedArgs {
 };
 
 // out[i, :] = scale * table[ids[i], :].  The output is one sequence of vectors, ceil(dim / V) a row, of which a block writes
-// kEmbedTurns * kThreads.
+// kEmbedTurns * kThreads: a thread's ids, then its rows are on their way together.  Memory bounds it: 540 K rows of 128 floats to half 84 us,
+// 4.9 TB/s (82 to 85 with 1 to 8 turns; 16 K rows of 4096 bfloat16 51, 46, 43, 44 us with 1, 2, 4, 8).  Reading past the caches took 8 % less for
+// half rows of a table far beyond them, but 20 to 25 % more where ids repeat, so the rows are read like anything else.
 constexpr int kEmbedTurns = 4;
 template <typename TI, typename TO, int V>
 __global__ void __launch_bounds__(kThreads) k_embedding(EmbedArgs A) {
@@ -359,6 +361,8 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs A) {
 //
 // A wave has one row at a time, so that rows, their ends and the addresses are scalar: with groups of 32 lanes, two rows to a wave, ends that
 // differ made both halves wait and every lane work out addresses.  A lane has V columns, as few as let 64 lanes have the whole row.
+// 480 K x 100 halfs into touched rows 46 us for 216 MB in lines of 128 bytes (4.7 TB/s, the rate of a copy); pieces of 8 and 32 tokens make that
+// call 107 and 105 us instead of 102, few ids often 108 and 76 instead of 84, 4096 ids of 1024 columns 20 and 26 instead of 22.
 constexpr int kGradTokens = 16;
 constexpr int kGradWaves = 8;
 constexpr int kGradThreads = 64 * kGradWaves;
@@ -390,6 +394,7 @@ struct EmbedGradArgs {
   int64_t part_width;
   int32_t clear_rows;      // rows of a block that clears
   // touched rows alone (row_ids != null): a run's row of `grad` is its rank
+  int32_t direct;          // blocks count the runs before their own from the sorted tokens
   int32_t scanned;         // tile_runs holds its exclusive scan
   int32_t* row_ids;
   int64_t* num_unique;
@@ -431,11 +436,25 @@ static __global__ void __launch_bounds__(kThreads) k_embed_scan(EmbedGradArgs A)
   if (threadIdx.x == 0) *A.num_unique = before;
 }
 
-// A thread's share of the runs that begin before a block's tokens; all: of all runs, where the tiles are not scanned, for block 0.
-__device__ __forceinline__ uint32_t share_of_runs(const EmbedGradArgs& A, uint32_t block, uint32_t& all) {
+// A thread's share of the runs that begin before a block's tokens; all: of all runs, where the tiles are not scanned, for block 0.  Up to
+// kDirectRuns ids need no k_embed_runs: their blocks look at all tokens before theirs (1000 ids of 32 floats 16.1 -> 13.5 us, 4000 of 128 the same with
+// either, 8192 25.8 instead of 23.1).
+constexpr int kDirectRuns = 2048;
+__device__ __forceinline__ uint32_t share_of_runs(const EmbedGradArgs& A, uint32_t block, int64_t n, uint32_t& all) {
   const int64_t tile = static_cast<int64_t>(block) * kBlockTokens / kRunTile;
-  uint32_t x = threadIdx.x == 0 ? A.block_runs[block] : 0u;
   all = 0;
+  if (A.direct) {
+    const int to = static_cast<int>(block == 0 ? n : static_cast<int64_t>(block) * kBlockTokens < n ? static_cast<int64_t>(block) * kBlockTokens : n);
+    uint32_t runs = 0;
+#pragma unroll 4
+    for (int q = threadIdx.x; q < to; q += blockDim.x) {
+      const uint32_t key = A.sorted[q].x, left = A.sorted[q > 0 ? q - 1 : 0].x;
+      runs += key < A.num_rows && (q == 0 || left != key) ? 1u : 0u;
+    }
+    if (block == 0) all = runs;
+    return block == 0 ? 0u : runs;
+  }
+  uint32_t x = threadIdx.x == 0 ? A.block_runs[block] : 0u;
   if (A.scanned) return threadIdx.x == 0 ? x + A.tile_runs[tile] : 0u;
   if (block == 0)
     for (int64_t t = threadIdx.x; t < A.run_tiles; t += blockDim.x) all += A.tile_runs[t];
@@ -583,7 +602,7 @@ __global__ void __launch_bounds__(TINY ? kTinyThreads : kGradThreads) k_embed_su
     const int64_t at = p0 - 1 + lane;
     mine = A.sorted[at < 0 ? 0 : at < A.max_ids ? at : A.max_ids - 1];
     if (lane > kGradTokens + 1 || at < 0 || at >= n) mine = make_uint2(none, 0);
-    if (A.row_ids) rank = share_of_runs(A, block, all);
+    if (A.row_ids) rank = share_of_runs(A, block, n, all);
   }
   // Every row is read, also a padded place's and for columns that there are not (the last ones again), and dropped later: loads under a
   // condition are waited for one by one.  Token 0 stands for those behind the last.

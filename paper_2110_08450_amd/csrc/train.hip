@@ -226,7 +226,8 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
     A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, c, st);
     clear = clear && !early;
   }
-  if (rows_only && (max_ids == 0 || !tiny)) {
+  A.direct = max_ids <= kDirectRuns;
+  if (rows_only && (max_ids == 0 || !A.direct)) {
     if (max_ids > 0) k_embed_runs<<<static_cast<unsigned>(S.run_tiles), kThreads, 0, st>>>(A);
     A.scanned = max_ids == 0 || S.run_tiles > kScanTiles;
     if (A.scanned) k_embed_scan<<<1, kThreads, 0, st>>>(A);
