@@ -32,7 +32,7 @@ struct EmbedArgs {
 // out[i, :] = scale * table[ids[i], :].  The output is one sequence of vectors, ceil(dim / V) a row, of which a block writes
 // kEmbedTurns * kThreads: a thread's ids, then its rows are on their way together.  Memory bounds it: 540 K rows of 128 floats to half 84 us,
 // 4.9 TB/s (82 to 85 with 1 to 8 turns; 16 K rows of 4096 bfloat16 51, 46, 43, 44 us with 1, 2, 4, 8).  Reading past the caches took 8 % less for
-// half rows of a table far beyond them, but 20 to 25 % more where ids repeat, so the rows are read like anything else.
+// half rows of a table far beyond them, but 20 to 27 % more where ids repeat, so the rows are read like anything else.
 constexpr int kEmbedTurns = 4;
 template <typename TI, typename TO, int V>
 __global__ void __launch_bounds__(kThreads) k_embedding(EmbedArgs A) {
@@ -99,7 +99,8 @@ struct SortArgs {
 };
 
 // The sort leaves most of the chip idle and waits for memory, so part of the gradient is cleared beside each of its launches, where most rows
-// are untouched (see early_clear): 16 K tokens of 1024 columns into 50 K rows of floats 72.6 -> 69.0 us, 300 K of 64 into 2 M 172 -> 149.  A block has every gridDim - own_blocks-th
+// are untouched (see early_clear): 16 K tokens of 1024 columns into 50 K rows of floats 72.6 -> 69.0 us, 300 K of 64 into 2 M 172 -> 149.  A block has
+// every gridDim - own_blocks-th
 // vector, or row where rows are apart.
 __device__ __forceinline__ void clear_beside(const SortArgs& A) {
   typedef Elems<uint16_t, 8> Vector;
