@@ -427,13 +427,20 @@ DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 class Scratch:
-    """Device memory that a call works in; keep it from call to call, one per call that may be in flight."""
+    """Device memory that a call works in; keep it from call to call, one per call that may be in flight.  A call on a stream that is handed
+    to it marks the memory as in use there, so that it may be dropped before the call has run."""
 
     def __init__(self, nbytes: int, where: str, device=None):
         if nbytes < 0:
             raise SmfgError(ERR_INVALID_ARG, where)
         self.nbytes = nbytes
         self.data = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device if device is not None else "cuda")
+
+    def on(self, stream: Optional[torch.cuda.Stream]) -> int:
+        """Address for a call on the stream."""
+        if stream is not None:
+            self.data.record_stream(stream)
+        return self.data.data_ptr()
 
 
 def _raw_stream(stream: Optional[torch.cuda.Stream]) -> int:
@@ -485,7 +492,7 @@ def embedding_grad(ids: torch.Tensor, num_ids: torch.Tensor, max_ids: int, grad_
     g, gs, gt = _matrix(grad_table, 1, "grad_table")
     rc = lib().smfg_embedding_grad(_vector(ids, max_ids, ids.dtype, "ids"), ids.element_size(), _vector(num_ids, 1, torch.int64, "num_ids"),
                                    max_ids, d, ds, dt, grad_out.shape[1], scale, g, grad_table.shape[0], gs, gt, int(bool(accumulate)),
-                                   ws.data.data_ptr(), ws.nbytes, _raw_stream(stream))
+                                   ws.on(stream), ws.nbytes, _raw_stream(stream))
     _check(rc, "smfg_embedding_grad")
 
 
@@ -500,7 +507,7 @@ def embedding_grad_rows(ids: torch.Tensor, num_ids: torch.Tensor, max_ids: int, 
     g, gs, gt = _matrix(grad_rows, max_ids, "grad_rows")
     rc = lib().smfg_embedding_grad_rows(_vector(ids, max_ids, ids.dtype, "ids"), ids.element_size(), _vector(num_ids, 1, torch.int64, "num_ids"),
                                         max_ids, d, ds, dt, grad_out.shape[1], scale, num_rows, _vector(row_ids, max_ids, torch.int32, "row_ids"),
-                                        _vector(num_unique, 1, torch.int64, "num_unique"), g, gs, gt, ws.data.data_ptr(), ws.nbytes,
+                                        _vector(num_unique, 1, torch.int64, "num_unique"), g, gs, gt, ws.on(stream), ws.nbytes,
                                         _raw_stream(stream))
     _check(rc, "smfg_embedding_grad_rows")
 
@@ -544,7 +551,7 @@ def layer_norm_grad(grad_y: torch.Tensor, x: torch.Tensor, num_rows: torch.Tenso
     rc = lib().smfg_layer_norm_grad(d, ds, a, as_, at, _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, dim, _vector(weight, dim, pd, "weight"),
                                     DTYPES[pd], _vector(mean, max_rows, torch.float32, "mean"), _vector(rstd, max_rows, torch.float32, "rstd"), gx, gs,
                                     _vector(grad_weight, dim, pd, "grad_weight"), _vector(grad_bias, dim, pd, "grad_bias"),
-                                    ws.data.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0, _raw_stream(stream))
+                                    ws.on(stream) if ws is not None else None, ws.nbytes if ws is not None else 0, _raw_stream(stream))
     _check(rc, "smfg_layer_norm_grad")
 
 
@@ -583,7 +590,7 @@ def grad_list(grads: Sequence[torch.Tensor], outs: Optional[Sequence[Optional[to
 def clip_grad_norm(grads: GradList, max_norm: float, norm: torch.Tensor, scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
     """norm (float32, one element) = the 2-norm of all gradients times scale; every gradient is multiplied by
     scale * min(1, max_norm / (norm + 1e-6)).  max_norm may be infinite."""
-    rc = lib().smfg_clip_grad_norm(grads.c, grads.n, scale, max_norm, _vector(norm, 1, torch.float32, "norm"), grads.scratch.data.data_ptr(),
+    rc = lib().smfg_clip_grad_norm(grads.c, grads.n, scale, max_norm, _vector(norm, 1, torch.float32, "norm"), grads.scratch.on(stream),
                                    grads.scratch.nbytes, _raw_stream(stream))
     _check(rc, "smfg_clip_grad_norm")
 

@@ -76,7 +76,9 @@ EmbedScratch embed_scratch(int64_t max_ids, int32_t dim) {
   };
   S.rec[0] = take(8 * max_ids);
   S.rec[1] = take(8 * max_ids);
-  S.hist = take(max_ids > kSmallSort ? 2 * kSortBins * S.tiles : 0);
+  // as much for many ids as for the most that have smaller tiles: scratch for max_ids has room for calls of fewer
+  const int64_t small_tiles = ceil_div(max_ids, 2 * kSortThreads);
+  S.hist = take(max_ids > kSmallSort ? 2 * kSortBins * (S.turns == 2 || S.tiles > kSortColumns ? S.tiles : small_tiles < kSortColumns ? small_tiles : kSortColumns) : 0);
   S.starts = take(S.tiles > kSortColumns ? 4 * kSortBins * S.tiles : 0);
   S.totals = take(4 * kSortBins);
   S.part = take(4 * 2 * G.blocks * G.width);

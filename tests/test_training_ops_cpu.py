@@ -106,6 +106,16 @@ def test_scratch_sizes_are_host_only():
         assert L.smfg_layer_norm_grad_scratch_bytes(n, dim) == -1
 
 
+def test_scratch_has_room_for_calls_of_fewer_ids():
+    """Also where a smaller call sorts in other tiles, or in another way."""
+    size = smfg.lib().smfg_embedding_grad_scratch_bytes
+    for dim in (1, 64, 65, 128, 129, 4096):
+        most = 0
+        for n in sorted({b + d for b in (0, 256, 2048, 8192, 100_000, 1 << 19, 600_000, 1 << 20, 3_000_000) for d in range(-3, 4) if b + d >= 0}):
+            assert size(n, 1000, dim) >= most, (n, dim)
+            most = size(n, 1000, dim)
+
+
 def test_grad_struct_layout_matches_the_binding(tmp_path):
     fields = ["grad", "out", "numel", "dtype", "out_dtype", "d_rows", "row_elems"]
     src = tmp_path / "layout.c"
