@@ -372,6 +372,7 @@ constexpr int kBlockTokens = kGradWaves * kGradTokens;
 // of four for touched rows alone.
 constexpr int kTinyIds = 256;
 constexpr int kTinyThreads = 1024;
+static_assert(kTinyThreads / 64 * kGradTokens == kTinyIds, "a piece a wave");
 constexpr int kRunTile = 1024;     // a multiple of every block's tokens
 constexpr int kScanTiles = 1024;   // more run tiles than that are scanned by a launch of their own
 constexpr int grad_columns(int dim) { return dim <= 64 ? 1 : dim <= 128 ? 2 : 4; }
@@ -549,7 +550,8 @@ __device__ __forceinline__ void clear_rows(const EmbedGradArgs& A, int64_t n, ui
 }
 
 // The ids in sorted[1 ..], between two entries that stand for no row.  By the block: four threads a token compare its row with a quarter of the others each.
-__device__ __forceinline__ void sort_tiny(const EmbedGradArgs& A, int n, uint2* sorted, uint32_t* keys, uint32_t (*smaller)[kTinyIds]) {
+__device__ __forceinline__ void sort_tiny(const EmbedGradArgs& A, int n, uint2* sorted, uint4* quads, uint32_t (*smaller)[kTinyIds]) {
+  uint32_t* keys = reinterpret_cast<uint32_t*>(quads);
   const uint32_t none = static_cast<uint32_t>(A.num_rows);
   const int i = threadIdx.x % kTinyIds, quarter = threadIdx.x / kTinyIds;
   if (quarter == 0) {
@@ -560,11 +562,12 @@ __device__ __forceinline__ void sort_tiny(const EmbedGradArgs& A, int n, uint2* 
   __syncthreads();
   const uint32_t key = keys[i];
   uint32_t count = 0;
-#pragma unroll 8
-  for (int q = 0; q < kTinyIds / 4; ++q) {
-    const int j = quarter * (kTinyIds / 4) + q;
-    const uint32_t k = keys[j];
-    count += (k < key) | ((k == key) & (j < i)) ? 1u : 0u;
+  const auto belongs_before = [&](uint32_t k, int j) { return (k < key) | ((k == key) & (j < i)) ? 1u : 0u; };
+#pragma unroll
+  for (int q = 0; q < kTinyIds / 16; ++q) {
+    const int at = quarter * (kTinyIds / 16) + q;
+    const uint4 k = quads[at];
+    count += belongs_before(k.x, 4 * at) + belongs_before(k.y, 4 * at + 1) + belongs_before(k.z, 4 * at + 2) + belongs_before(k.w, 4 * at + 3);
   }
   smaller[quarter][i] = count;
   __syncthreads();
@@ -596,7 +599,8 @@ __global__ void __launch_bounds__(TINY ? kTinyThreads : kGradThreads) k_embed_su
   uint32_t rank = 0, all = 0;
   if constexpr (TINY) {
     __shared__ uint2 sorted[kTinyIds + 2];
-    __shared__ uint32_t keys[kTinyIds], smaller[4][kTinyIds];
+    __shared__ uint4 keys[kTinyIds / 4];
+    __shared__ uint32_t smaller[4][kTinyIds];
     sort_tiny(A, static_cast<int>(n), sorted, keys, smaller);
     mine = lane <= kGradTokens + 1 ? sorted[wave * kGradTokens + lane] : make_uint2(none, 0);
   } else {
