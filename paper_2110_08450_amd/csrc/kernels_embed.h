@@ -464,14 +464,21 @@ __device__ __forceinline__ uint32_t share_of_runs(const EmbedGradArgs& A, uint32
   return x;
 }
 
-// V columns of a row of the gradient from their sum and, where it is added to, what they hold; those that the vector before has as well are
-// left to it.
+// V columns of a row of the gradient from their sum and, where it is added to, what they hold.  Columns that the vector before has as well are
+// left to it where the row is added to, as that may be another block's; else both write the same (480 K x 100 halfs 47 -> 41 us).
 template <typename TG, int V>
 __device__ __forceinline__ TG* grad_at(const EmbedGradArgs& A, int64_t row, const Columns<V>& c) {
   return static_cast<TG*>(A.grad) + row * A.grad_stride + c.start;
 }
 template <typename TG, int V>
-__device__ __forceinline__ void write_grad(const EmbedGradArgs& A, int64_t row, const Columns<V>& c, const float (&sum)[V], Elems<TG, V> e) {
+__device__ __forceinline__ void write_row(const EmbedGradArgs& A, int64_t row, const Columns<V>& c, const float (&sum)[V]) {
+  Elems<TG, V> e;
+#pragma unroll
+  for (int j = 0; j < V; ++j) e.v[j] = from_float<TG>(A.scale * sum[j]);
+  if (c.dup < V) *reinterpret_cast<Elems<TG, V>*>(grad_at<TG, V>(A, row, c)) = e;
+}
+template <typename TG, int V>
+__device__ __forceinline__ void add_to_row(const EmbedGradArgs& A, int64_t row, const Columns<V>& c, const float (&sum)[V], Elems<TG, V> e) {
   TG* g = grad_at<TG, V>(A, row, c);
 #pragma unroll
   for (int j = 0; j < V; ++j) e.v[j] = from_float<TG>(as_float(e.v[j]) + A.scale * sum[j]);
@@ -485,9 +492,8 @@ __device__ __forceinline__ void write_grad(const EmbedGradArgs& A, int64_t row, 
 }
 template <typename TG, int V>
 __device__ __forceinline__ void write_grad(const EmbedGradArgs& A, int64_t row, const Columns<V>& c, const float (&sum)[V]) {
-  Elems<TG, V> e = {};
-  if (A.accumulate) e = *reinterpret_cast<const Elems<TG, V>*>(grad_at<TG, V>(A, row, c));
-  write_grad<TG, V>(A, row, c, sum, e);
+  if (A.accumulate) add_to_row<TG, V>(A, row, c, sum, *reinterpret_cast<const Elems<TG, V>*>(grad_at<TG, V>(A, row, c)));
+  else write_row<TG, V>(A, row, c, sum);
 }
 
 // First sorted place whose row is at least `key`, in [lo, hi].
@@ -673,8 +679,8 @@ __global__ void __launch_bounds__(TINY ? kTinyThreads : kGradThreads) k_embed_su
         for (int j = 0; j < V; ++j) heads[wave][j * 64 + lane] = sum[j];
       } else {
         const int64_t row = A.row_ids ? static_cast<int64_t>(rank++) : static_cast<int64_t>(here);
-        if constexpr (ADD) write_grad<TG, V>(A, row, c, sum, held[u % kAhead]);
-        else write_grad<TG, V>(A, row, c, sum, {});
+        if constexpr (ADD) add_to_row<TG, V>(A, row, c, sum, held[u % kAhead]);
+        else write_row<TG, V>(A, row, c, sum);
       }
     }
     head = false;
