@@ -99,7 +99,7 @@ struct SortArgs {
 };
 
 // The sort leaves most of the chip idle and waits for memory, so part of the gradient is cleared beside each of its launches, where most rows
-// are untouched (see early_clear): 16 K tokens of 1024 columns into 50 K rows of floats 72.6 -> 69.0 us, 300 K of 64 into 2 M 172 -> 149.  A block has
+// are untouched (see early_clear): 16 K tokens of 1024 columns into 50 K rows of floats 72.6 -> 69.0 us, 300 K of 64 into 2 M 172 -> 149 (the sums took longer then).  A block has
 // every gridDim - own_blocks-th
 // vector, or row where rows are apart.
 __device__ __forceinline__ void clear_beside(const SortArgs& A) {
@@ -362,8 +362,8 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs A) {
 //
 // A wave has one row at a time, so that rows, their ends and the addresses are scalar: with groups of 32 lanes, two rows to a wave, ends that
 // differ made both halves wait and every lane work out addresses.  A lane has V columns, as few as let 64 lanes have the whole row.
-// 480 K x 100 halfs into touched rows 46 us for 216 MB in lines of 128 bytes (4.7 TB/s, the rate of a copy); pieces of 8 and 32 tokens make that
-// call 107 and 105 us instead of 102, few ids often 108 and 76 instead of 84, 4096 ids of 1024 columns 20 and 26 instead of 22.
+// 480 K x 100 halfs into touched rows 41 us for 216 MB in lines of 128 bytes (5.2 TB/s, more than a copy); pieces of 8 and 32 tokens made that
+// call 107 and 105 us where 16 made it 102, few ids often 108 and 76 instead of 84, 4096 ids of 1024 columns 20 and 26 instead of 22.
 constexpr int kGradTokens = 16;
 constexpr int kGradWaves = 8;
 constexpr int kGradThreads = 64 * kGradWaves;
