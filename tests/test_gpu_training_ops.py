@@ -121,6 +121,7 @@ GRADS = [(1, 0, 1, 1, F32, F32, "uniform", 0), (5, 3, 9, 3, F16, F32, "uniform",
          (0, 700, 40, 16, F32, F32, "uniform", 0), (150_000, 0, 4096, 16, F32, F32, "mixed", 0), (260_000, 1, 100, 33, F16, F32, "same", 0),
          (8192, 0, 16_777_217, 8, F32, F32, "uniform", 0), (4100, 3000, 130_000, 12, F16, F32, "backwards", 0),
          (1_300_000, 5000, 700_000, 4, F32, F32, "mixed", 0), (1_050_000, 0, 3, 2, F16, F32, "uniform", 0),
+         (0, 700, 5000, 16, F32, F32, "uniform", 0), (0, 9000, 20_000, 5, F16, F32, "uniform", 2), (2049, 0, 600, 130, F16, F32, "mixed", 1),
          (600, 3, 5000, 3, F16, F16, "uniform", 1), (700, 0, 1500, 5, BF16, BF16, "mixed", 0), (256, 0, 64, 200, F16, F32, "same", 0),
          (257, 0, 64, 64, F32, F32, "mixed", 0), (40_000, 0, 90_000, 33, F16, F16, "mixed", 7)]
 
