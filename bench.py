@@ -35,15 +35,29 @@ LAUNCH_CONFIG = {"tiny": (4, 1, 2), "mid": (16, 2, 3), "large": (8, 2, 3), "pape
 TRAFFIC_JSON = os.path.join(ROOT, "profiles", "traffic.json")
 
 
+def library_files():
+    """The sources that k_gather's part of the library is made of: smfg.hip and all it includes of this repository.  The training
+    operators are a source of their own, whose changes leave a counter figure of the gather as good as it was."""
+    import re
+    csrc, include = os.path.join(ROOT, "paper_2110_08450_amd", "csrc"), os.path.join(ROOT, "include")
+    found, ahead = set(), [os.path.join(csrc, "smfg.hip")]
+    while ahead:
+        f = ahead.pop()
+        if f in found:
+            continue
+        found.add(f)
+        for name in re.findall(r'^\s*#\s*include\s*"([^"]+)"', open(f, "r", encoding="utf-8").read(), flags=re.M):
+            ahead += [p for p in (os.path.join(d, name) for d in (csrc, include)) if os.path.exists(p)][:1]
+    return sorted(found, key=os.path.basename)
+
+
 def source_hash():
-    """sha256 over the library's sources (kernels, host side, header) without their comments and
+    """sha256 over those sources (kernels, host side, header) without their comments and
     blank space: names the code a stored counter figure was measured on."""
     import hashlib
     import re
     h = hashlib.sha256()
-    csrc = os.path.join(ROOT, "paper_2110_08450_amd", "csrc")
-    files = sorted(os.path.join(csrc, f) for f in os.listdir(csrc)) + [os.path.join(ROOT, "include", "smfg.h")]
-    for f in files:
+    for f in library_files():
         text = open(f, "r", encoding="utf-8").read()
         text = re.sub(r"/\*.*?\*/", " ", text, flags=re.S)   # no string literal of these files holds a comment mark
         text = re.sub(r"//[^\n]*", " ", text)
