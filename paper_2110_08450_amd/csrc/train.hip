@@ -36,15 +36,41 @@ void with_type(int32_t type, F f) {
   else if (type == SMFG_DTYPE_F16) f(_Float16{});
   else f(__bf16{});
 }
+// The launches of a call, one behind the other.  Behind one that failed there are no more: they would work on scratch that it should have
+// written, places of the output among it.
+class Launches {
+  template <typename T>
+  struct Just {
+    using type = T;
+  };
+
+ public:
+  explicit Launches(void* stream) : stream_(static_cast<hipStream_t>(stream)) {}
+  template <typename... P>
+  void operator()(void (*kernel)(P...), dim3 blocks, int threads, const typename Just<P>::type&... args) {
+    if (error_ != hipSuccess) return;
+    void* list[] = {const_cast<void*>(static_cast<const void*>(&args))...};
+    error_ = hipLaunchKernel(reinterpret_cast<const void*>(kernel), blocks, dim3(static_cast<unsigned>(threads)), list, 0, stream_);
+  }
+  int result() const {
+    if (error_ != hipSuccess) (void)hipGetLastError();  // told here, and not once more by who asks next
+    return hip_err(error_);
+  }
+
+ private:
+  hipStream_t stream_;
+  hipError_t error_ = hipSuccess;
+};
+
 template <typename T>
 constexpr int kVec = 16 / static_cast<int>(sizeof(T));  // columns of a 16-byte vector
 
 // ---- embedding ----------------------------------------------------------------------------------
 
 template <typename TI, typename TO>
-void launch_embedding(const EmbedArgs& A, unsigned blocks, bool vectors, hipStream_t st) {
-  if (vectors) k_embedding<TI, TO, kVec<TO>><<<blocks, kThreads, 0, st>>>(A);
-  else k_embedding<TI, TO, 1><<<blocks, kThreads, 0, st>>>(A);
+void launch_embedding(const EmbedArgs& A, unsigned blocks, bool vectors, Launches& go) {
+  if (vectors) go(k_embedding<TI, TO, kVec<TO>>, blocks, kThreads, A);
+  else go(k_embedding<TI, TO, 1>, blocks, kThreads, A);
 }
 
 // Blocks of k_embed_sums for the tokens, tiles of 64 * V columns, and floats of a row of partial sums.
@@ -111,7 +137,7 @@ unsigned sort_blocks(SortArgs& A, int64_t own, const Clear& c, int part, int par
 
 // (row, token) of the call's ids, sorted by row.  num_rows itself, which stands for no row, is a key as well.
 const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* ids, int32_t id_bytes, const int64_t* num, int64_t max_ids,
-                         int64_t num_rows, const Clear& clear, hipStream_t st) {
+                         int64_t num_rows, const Clear& clear, Launches& go) {
   SortArgs A = {};
   A.ids = ids;
   A.id_bytes = id_bytes;
@@ -125,7 +151,7 @@ const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* id
   A.out = reinterpret_cast<uint2*>(scratch + S.rec[0]);
   if (max_ids <= kSmallSort) {
     const unsigned blocks = sort_blocks(A, ceil_div(max_ids, kSmallTokens), clear, 0, 1);
-    k_sort_small<<<blocks, kSmallThreads, 0, st>>>(A);
+    go(k_sort_small, blocks, kSmallThreads, A);
     return A.out;
   }
   int key_bits = 0;
@@ -135,19 +161,19 @@ const uint2* launch_sort(const EmbedScratch& S, uint8_t* scratch, const void* id
   for (int p = 0; p < passes; ++p, A.shift += A.bits) {
     A.out = reinterpret_cast<uint2*>(scratch + S.rec[p & 1]);
     unsigned blocks = sort_blocks(A, S.tiles, clear, 2 * p, 2 * passes);
-    if (S.turns == 2) k_sort_count<2><<<blocks, kSortThreads, 0, st>>>(A);
-    else k_sort_count<4><<<blocks, kSortThreads, 0, st>>>(A);
-    if (A.starts) k_sort_scan<<<static_cast<unsigned>(ceil_div(1 << A.bits, 2 * kScanPairs)), kSortThreads, 0, st>>>(A);
+    if (S.turns == 2) go(k_sort_count<2>, blocks, kSortThreads, A);
+    else go(k_sort_count<4>, blocks, kSortThreads, A);
+    if (A.starts) go(k_sort_scan, static_cast<unsigned>(ceil_div(1 << A.bits, 2 * kScanPairs)), kSortThreads, A);
     blocks = sort_blocks(A, S.tiles, clear, 2 * p + 1, 2 * passes);
-    if (S.turns == 2) k_sort_scatter<2><<<blocks, kSortThreads, 0, st>>>(A);
-    else k_sort_scatter<4><<<blocks, kSortThreads, 0, st>>>(A);
+    if (S.turns == 2) go(k_sort_scatter<2>, blocks, kSortThreads, A);
+    else go(k_sort_scatter<4>, blocks, kSortThreads, A);
     A.in = A.out;
   }
   return A.in;
 }
 
 template <typename TD, typename TG, int V>
-void launch_embed_sums(EmbedGradArgs A, const GradShape& G, bool clear, hipStream_t st) {
+void launch_embed_sums(EmbedGradArgs A, const GradShape& G, bool clear, Launches& go) {
   A.sum_blocks = G.blocks > 0 ? static_cast<uint32_t>(G.blocks) : 1u;  // without tokens there is one, which has no tile
   A.tiles = G.blocks > 0 ? static_cast<uint32_t>(G.tiles) : 0u;
   // a block clears about 32 KiB, of at most a row a thread
@@ -159,24 +185,24 @@ void launch_embed_sums(EmbedGradArgs A, const GradShape& G, bool clear, hipStrea
   if (blocks == 0) return;
   const unsigned b = static_cast<unsigned>(blocks);
   if (tiny) {
-    if (A.accumulate) k_embed_sums<TD, TG, V, true, true><<<b, kTinyThreads, 0, st>>>(A);
-    else k_embed_sums<TD, TG, V, true, false><<<b, kTinyThreads, 0, st>>>(A);
+    if (A.accumulate) go(k_embed_sums<TD, TG, V, true, true>, b, kTinyThreads, A);
+    else go(k_embed_sums<TD, TG, V, true, false>, b, kTinyThreads, A);
     return;
   }
-  if (A.accumulate) k_embed_sums<TD, TG, V, false, true><<<b, kGradThreads, 0, st>>>(A);
-  else k_embed_sums<TD, TG, V, false, false><<<b, kGradThreads, 0, st>>>(A);
+  if (A.accumulate) go(k_embed_sums<TD, TG, V, false, true>, b, kGradThreads, A);
+  else go(k_embed_sums<TD, TG, V, false, false>, b, kGradThreads, A);
   if (G.blocks < 2) return;
   const uint32_t joins = static_cast<uint32_t>(ceil_div(G.blocks, kJoinWaves));
   const unsigned longs = static_cast<unsigned>((G.blocks - 1) / kJoinShort);
-  k_embed_join<TG, V><<<dim3(joins + longs, static_cast<unsigned>(G.tiles)), kJoinThreads, 0, st>>>(A, joins);
+  go(k_embed_join<TG, V>, dim3(joins + longs, static_cast<unsigned>(G.tiles)), kJoinThreads, A, joins);
 }
 
 template <typename TD, typename TG>
-void launch_embed_grad(const EmbedGradArgs& A, const GradShape& G, bool clear, hipStream_t st) {
+void launch_embed_grad(const EmbedGradArgs& A, const GradShape& G, bool clear, Launches& go) {
   const int V = grad_columns(A.dim);
-  if (V == 1) launch_embed_sums<TD, TG, 1>(A, G, clear, st);
-  else if (V == 2) launch_embed_sums<TD, TG, 2>(A, G, clear, st);
-  else launch_embed_sums<TD, TG, 4>(A, G, clear, st);
+  if (V == 1) launch_embed_sums<TD, TG, 1>(A, G, clear, go);
+  else if (V == 2) launch_embed_sums<TD, TG, 2>(A, G, clear, go);
+  else launch_embed_sums<TD, TG, 4>(A, G, clear, go);
 }
 
 // Is the whole gradient cleared beside the sort, and the touched rows written over?  Else only the untouched ones are, beside the sums.  At most half
@@ -186,7 +212,7 @@ bool early_clear(int64_t max_ids, int64_t num_rows) { return num_rows >= 2 * max
 int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids, int64_t max_ids, const void* d_dy, int64_t dy_stride,
                    int32_t dy_dtype, int32_t dim, float scale, void* d_grad, int64_t num_rows, int64_t grad_stride, int32_t grad_dtype,
                    int32_t accumulate, bool rows_only, int32_t* d_row_ids, int64_t* d_num_unique, void* d_scratch, int64_t scratch_bytes,
-                   hipStream_t st) {
+                   void* hip_stream) {
   if (!d_num_ids || !d_grad || (max_ids > 0 && (!d_ids || !d_dy || !d_scratch))) return SMFG_ERR_NULL_PTR;
   if (rows_only && (!d_num_unique || (max_ids > 0 && !d_row_ids))) return SMFG_ERR_NULL_PTR;
   if (bad_dim(dim) || (id_bytes != 4 && id_bytes != 8) || max_ids < 0 || max_ids >= kMaxRows || num_rows < 1 || num_rows >= kMaxRows ||
@@ -195,6 +221,7 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
       misaligned(d_num_ids, 8) || misaligned(d_row_ids, 4) || misaligned(d_num_unique, 8) || misaligned(d_scratch, 256))
     return SMFG_ERR_INVALID_ARG;
   if (max_ids == 0 && !rows_only && accumulate) return SMFG_OK;
+  Launches go(hip_stream);
   const EmbedScratch S = embed_scratch(max_ids, dim);
   if (max_ids > 0 && scratch_bytes < S.bytes) return SMFG_ERR_CAPACITY;
   const GradShape G = grad_shape(max_ids, dim);
@@ -225,21 +252,21 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
   if (!tiny) {
     const bool early = clear && early_clear(max_ids, num_rows);
     const Clear c = {early ? d_grad : nullptr, num_rows, dim, grad_stride, type_bytes(grad_dtype)};
-    A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, c, st);
+    A.sorted = launch_sort(S, scratch, d_ids, id_bytes, d_num_ids, max_ids, num_rows, c, go);
     clear = clear && !early;
   }
   A.direct = max_ids <= kDirectRuns;
   if (rows_only && (max_ids == 0 || !A.direct)) {
-    if (max_ids > 0) k_embed_runs<<<static_cast<unsigned>(S.run_tiles), kThreads, 0, st>>>(A);
+    if (max_ids > 0) go(k_embed_runs, static_cast<unsigned>(S.run_tiles), kThreads, A);
     A.scanned = max_ids == 0 || S.run_tiles > kScanTiles;
-    if (A.scanned) k_embed_scan<<<1, kThreads, 0, st>>>(A);
+    if (A.scanned) go(k_embed_scan, 1, kThreads, A);
   }
   with_type(dy_dtype, [&](auto t) {
     using T = decltype(t);
-    if (grad_dtype == SMFG_DTYPE_F32) launch_embed_grad<T, float>(A, G, clear, st);
-    else launch_embed_grad<T, T>(A, G, clear, st);
+    if (grad_dtype == SMFG_DTYPE_F32) launch_embed_grad<T, float>(A, G, clear, go);
+    else launch_embed_grad<T, T>(A, G, clear, go);
   });
-  return hip_err(hipGetLastError());
+  return go.result();
 }
 
 // ---- layer norm ---------------------------------------------------------------------------------
@@ -274,11 +301,11 @@ constexpr unsigned kNormBlocks = 2048;
 template <typename T>
 struct LaunchNorm {
   const NormArgs& A;
-  hipStream_t st;
+  Launches& go;
   template <int V, int NV, int LANES>
   void operator()() const {
     const unsigned blocks = blocks_for(A.max_rows, norm_threads(LANES) / LANES, kNormBlocks);
-    k_layer_norm<T, V, NV, LANES><<<blocks, norm_threads(LANES), 0, st>>>(A);
+    go(k_layer_norm<T, V, NV, LANES>, blocks, norm_threads(LANES), A);
   }
 };
 
@@ -297,12 +324,12 @@ template <typename T>
 struct LaunchNormGrad {
   const NormGradArgs& A;
   int64_t& slices;
-  hipStream_t st;
+  Launches& go;
   template <int V, int NV, int LANES>
   void operator()() const {
     const int64_t blocks = ceil_div(A.max_rows, norm_threads(LANES) / LANES);
     if (blocks < slices) slices = blocks;
-    k_layer_norm_grad<T, V, NV, LANES><<<static_cast<unsigned>(slices), norm_threads(LANES), 0, st>>>(A);
+    go(k_layer_norm_grad<T, V, NV, LANES>, static_cast<unsigned>(slices), norm_threads(LANES), A);
   }
 };
 
@@ -369,7 +396,7 @@ int smfg_embedding(const void* d_table, int64_t num_rows, int64_t table_stride, 
       (table_dtype != SMFG_DTYPE_F32 && table_dtype != out_dtype) || misaligned(d_ids, static_cast<uintptr_t>(id_bytes)) || misaligned(d_num_ids, 8))
     return SMFG_ERR_INVALID_ARG;
   if (max_ids == 0) return SMFG_OK;
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  Launches go(hip_stream);
   const EmbedArgs A = {d_table, num_rows, table_stride, dim, id_bytes, d_ids, d_num_ids, max_ids, scale, d_out, out_stride};
   const int vector = static_cast<int>(16 / type_bytes(out_dtype));
   const bool vectors = dim >= vector;
@@ -378,10 +405,10 @@ int smfg_embedding(const void* d_table, int64_t num_rows, int64_t table_stride, 
   const unsigned b = static_cast<unsigned>(blocks);
   with_type(out_dtype, [&](auto o) {
     using O = decltype(o);
-    if (table_dtype == SMFG_DTYPE_F32) launch_embedding<float, O>(A, b, vectors, st);
-    else launch_embedding<O, O>(A, b, vectors, st);
+    if (table_dtype == SMFG_DTYPE_F32) launch_embedding<float, O>(A, b, vectors, go);
+    else launch_embedding<O, O>(A, b, vectors, go);
   });
-  return hip_err(hipGetLastError());
+  return go.result();
 }
 
 int64_t smfg_embedding_grad_scratch_bytes(int64_t max_ids, int64_t num_rows, int32_t dim) {
@@ -393,14 +420,14 @@ int smfg_embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_nu
                         int32_t dy_dtype, int32_t dim, float scale, void* d_grad, int64_t num_rows, int64_t grad_stride, int32_t grad_dtype,
                         int32_t accumulate, void* d_scratch, int64_t scratch_bytes, void* hip_stream) {
   return embedding_grad(d_ids, id_bytes, d_num_ids, max_ids, d_dy, dy_stride, dy_dtype, dim, scale, d_grad, num_rows, grad_stride, grad_dtype,
-                        accumulate, false, nullptr, nullptr, d_scratch, scratch_bytes, static_cast<hipStream_t>(hip_stream));
+                        accumulate, false, nullptr, nullptr, d_scratch, scratch_bytes, hip_stream);
 }
 
 int smfg_embedding_grad_rows(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids, int64_t max_ids, const void* d_dy, int64_t dy_stride,
                              int32_t dy_dtype, int32_t dim, float scale, int64_t num_rows, int32_t* d_row_ids, int64_t* d_num_unique, void* d_grad,
                              int64_t grad_stride, int32_t grad_dtype, void* d_scratch, int64_t scratch_bytes, void* hip_stream) {
   return embedding_grad(d_ids, id_bytes, d_num_ids, max_ids, d_dy, dy_stride, dy_dtype, dim, scale, d_grad, num_rows, grad_stride, grad_dtype, 0,
-                        true, d_row_ids, d_num_unique, d_scratch, scratch_bytes, static_cast<hipStream_t>(hip_stream));
+                        true, d_row_ids, d_num_unique, d_scratch, scratch_bytes, hip_stream);
 }
 
 int smfg_layer_norm(const void* d_x, int64_t x_stride, int32_t dtype, const int64_t* d_num_rows, int64_t max_rows, int32_t dim, const void* d_w,
@@ -412,13 +439,13 @@ int smfg_layer_norm(const void* d_x, int64_t x_stride, int32_t dtype, const int6
       misaligned(d_rstd, 4) || (d_x == d_y && x_stride != y_stride))
     return SMFG_ERR_INVALID_ARG;
   if (max_rows == 0) return SMFG_OK;
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  Launches go(hip_stream);
   const NormArgs A = {d_x, x_stride, d_num_rows, max_rows, dim, param_dtype == SMFG_DTYPE_F32, d_w, d_b, eps, d_y, y_stride, d_mean, d_rstd};
   with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    if (!with_row_shape<T, 2048>(dim, LaunchNorm<T>{A, st})) k_layer_norm_long<T, kVec<T>><<<static_cast<unsigned>(max_rows), kThreads, 0, st>>>(A);
+    if (!with_row_shape<T, 2048>(dim, LaunchNorm<T>{A, go})) go(k_layer_norm_long<T, kVec<T>>, static_cast<unsigned>(max_rows), kThreads, A);
   });
-  return hip_err(hipGetLastError());
+  return go.result();
 }
 
 int64_t smfg_layer_norm_grad_scratch_bytes(int64_t max_rows, int32_t dim) {
@@ -440,7 +467,7 @@ int smfg_layer_norm_grad(const void* d_dy, int64_t dy_stride, const void* d_x, i
     return SMFG_ERR_INVALID_ARG;
   int64_t slices = norm_slices(max_rows, dim);
   if (sums && scratch_bytes < up256(slices * 8 * dim)) return SMFG_ERR_CAPACITY;
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  Launches go(hip_stream);
   float* part = sums ? static_cast<float*>(d_scratch) : nullptr;
   const NormGradArgs A = {d_dy, dy_stride, d_x, x_stride, d_num_rows, max_rows, dim, param_dtype == SMFG_DTYPE_F32, d_w, d_mean, d_rstd, d_dx, dx_stride, part};
   if (!sums && (max_rows == 0 || !d_dx)) return SMFG_OK;
@@ -448,22 +475,22 @@ int smfg_layer_norm_grad(const void* d_dy, int64_t dy_stride, const void* d_x, i
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
       constexpr int V = kVec<T>;
-      if (with_row_shape<T, sizeof(T) == 4 ? 2048 : 1536>(dim, LaunchNormGrad<T>{A, slices, st})) return;
+      if (with_row_shape<T, sizeof(T) == 4 ? 2048 : 1536>(dim, LaunchNormGrad<T>{A, slices, go})) return;
       if (sums) {
         if (slices > kNormLongSlices) slices = kNormLongSlices;
-        k_norm_grad_columns<T, V><<<dim3(static_cast<unsigned>(ceil_div(ceil_div(dim, V), kThreads)), static_cast<unsigned>(slices)), kThreads, 0, st>>>(A);
+        go(k_norm_grad_columns<T, V>, dim3(static_cast<unsigned>(ceil_div(ceil_div(dim, V), kThreads)), static_cast<unsigned>(slices)), kThreads, A);
       }
-      if (d_dx) k_layer_norm_grad_long<T, V><<<static_cast<unsigned>(max_rows), kThreads, 0, st>>>(A);
+      if (d_dx) go(k_layer_norm_grad_long<T, V>, static_cast<unsigned>(max_rows), kThreads, A);
     });
   }
   if (sums) {
     const unsigned blocks = static_cast<unsigned>(ceil_div(2 * static_cast<int64_t>(dim), kNormJoinCols));
     with_type(param_dtype, [&](auto p) {
       using P = decltype(p);
-      k_norm_grad_join<P><<<blocks, kNormJoinThreads, 0, st>>>(part, static_cast<int32_t>(slices), dim, static_cast<P*>(d_dw), static_cast<P*>(d_db));
+      go(k_norm_grad_join<P>, blocks, kNormJoinThreads, part, static_cast<int32_t>(slices), dim, static_cast<P*>(d_dw), static_cast<P*>(d_db));
     });
   }
-  return hip_err(hipGetLastError());
+  return go.result();
 }
 
 int64_t smfg_clip_grad_norm_scratch_bytes(const smfg_grad_t* grads, int32_t num_grads) {
@@ -481,7 +508,7 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
   const ClipScratch S = clip_scratch(grads, num_grads);
   if (S.blocks > 0x7FFFFFFF) return SMFG_ERR_INVALID_ARG;
   if (scratch_bytes < S.bytes) return SMFG_ERR_CAPACITY;
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  Launches go(hip_stream);
   uint8_t* scratch = static_cast<uint8_t*>(d_scratch);
   float* factor = static_cast<float*>(d_scratch);
   double* part = reinterpret_cast<double*>(scratch + S.part);
@@ -501,7 +528,7 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
     const smfg_grad_t& g = grads[i];
     if (g.numel == 0) continue;
     if (A.here == kClipTensors) {
-      k_clip_table<<<1, 64, 0, st>>>(A);
+      go(k_clip_table, 1, 64, A);
       A.first += A.here;
       A.here = 0;
     }
@@ -509,17 +536,17 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
                      g.dtype | (g.out ? g.out_dtype : g.dtype) << 4};
     A.blocks += static_cast<uint32_t>(ceil_div(g.numel, S.chunk));
   }
-  if (table) k_clip_table<<<1, 64, 0, st>>>(A);
+  if (table) go(k_clip_table, 1, 64, A);
   if (A.blocks > 0) {
-    if (table) k_clip_squares<true><<<A.blocks, kThreads, 0, st>>>(A);
-    else k_clip_squares<false><<<A.blocks, kThreads, 0, st>>>(A);
+    if (table) go(k_clip_squares<true>, A.blocks, kThreads, A);
+    else go(k_clip_squares<false>, A.blocks, kThreads, A);
   }
-  if (A.blocks == 0 || A.blocks > kClipJoin) k_clip_norm<<<1, kClipNormThreads, 0, st>>>(A);
+  if (A.blocks == 0 || A.blocks > kClipJoin) go(k_clip_norm, 1, kClipNormThreads, A);
   if (A.blocks > 0) {
-    if (table) k_clip_scale<true><<<A.blocks, kThreads, 0, st>>>(A);
-    else k_clip_scale<false><<<A.blocks, kThreads, 0, st>>>(A);
+    if (table) go(k_clip_scale<true>, A.blocks, kThreads, A);
+    else go(k_clip_scale<false>, A.blocks, kThreads, A);
   }
-  return hip_err(hipGetLastError());
+  return go.result();
 }
 
 }  // extern "C"
