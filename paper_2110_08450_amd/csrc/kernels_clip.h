@@ -30,6 +30,7 @@ struct ClipArgs {
   int32_t tensors;      // of the table, or of t
   int32_t first, here;  // tensors of the table that t has, for k_clip_table
   uint32_t blocks;
+  uint32_t first_block;  // of the launch
   int64_t chunk;
   double* part;         // a block's sum of squares
   float* factor;        // scale * c
@@ -136,9 +137,10 @@ __device__ __forceinline__ double sum_of_squares(const T* src, uint32_t q, int64
 template <bool TABLE>
 __global__ void __launch_bounds__(kThreads) k_clip_squares(ClipArgs A) {
   __shared__ double lds[kThreads / 64];
-  const ClipTensor T = tensor_of_block<TABLE>(A, blockIdx.x);
+  const uint32_t block = A.first_block + blockIdx.x;
+  const ClipTensor T = tensor_of_block<TABLE>(A, block);
   const int64_t n = elements_of(T);
-  const uint32_t q = blockIdx.x - T.first_block;
+  const uint32_t q = block - T.first_block;
   double s;
   switch (T.type & 15) {
     case SMFG_DTYPE_F32: s = sum_of_squares(static_cast<const float*>(T.src), q, A.chunk, T.numel, n); break;
@@ -152,7 +154,7 @@ __global__ void __launch_bounds__(kThreads) k_clip_squares(ClipArgs A) {
   if (threadIdx.x == 0) {
 #pragma unroll
     for (int w = 1; w < kThreads / 64; ++w) s += lds[w];
-    A.part[blockIdx.x] = s;
+    A.part[block] = s;
   }
 }
 
@@ -206,7 +208,7 @@ __device__ __forceinline__ void scaled_copy(const TS* src, TD* dst, uint32_t q, 
 // The last elements first: they are what the sum of squares has left in the caches (1 % of 670 us).  400 M halfs to floats 480 us, 5.0 TB/s.
 template <bool TABLE>
 __global__ void __launch_bounds__(kThreads) k_clip_scale(ClipArgs A) {
-  const uint32_t block = A.blocks - 1 - blockIdx.x;
+  const uint32_t block = A.blocks - 1 - (A.first_block + blockIdx.x);
   const ClipTensor T = tensor_of_block<TABLE>(A, block);
   float f;
   if (A.blocks <= kClipJoin) {

@@ -27,6 +27,7 @@ struct EmbedArgs {
   float scale;
   void* out;
   int64_t out_stride;
+  uint32_t first_block;  // of the launch
 };
 
 // out[i, :] = scale * table[ids[i], :].  The output is one sequence of vectors, ceil(dim / V) a row, of which a block writes
@@ -38,7 +39,7 @@ template <typename TI, typename TO, int V>
 __global__ void __launch_bounds__(kThreads) k_embedding(EmbedArgs A) {
   const int64_t n = count_of(A.num, A.max_ids);
   const uint32_t per_row = static_cast<uint32_t>((A.dim + V - 1) / V);
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * (kEmbedTurns * kThreads);
+  const int64_t first = (static_cast<int64_t>(A.first_block) + blockIdx.x) * (kEmbedTurns * kThreads);
   const int64_t row0 = first / per_row;
   if (row0 >= n) return;
   const uint32_t off = static_cast<uint32_t>(first - row0 * per_row);
@@ -389,6 +390,7 @@ struct EmbedGradArgs {
   const void* dy;
   int64_t dy_stride;
   float scale;
+  uint32_t first_block;        // of the launch of k_embed_sums
   uint32_t sum_blocks, tiles;  // blocks of k_embed_sums that add up, and tiles of columns; the blocks behind all of them clear
   void* grad;
   int64_t grad_stride;
@@ -590,10 +592,10 @@ __global__ void __launch_bounds__(TINY ? kTinyThreads : kGradThreads) k_embed_su
   __shared__ float heads[kWaves][64 * V];
   __shared__ uint32_t goes_on[kWaves];  // the wave's tokens are all of one run, that began before them and goes on behind them
   __shared__ uint32_t lds[kWaves * 64];
-  const uint32_t tile = blockIdx.x / A.sum_blocks, block = blockIdx.x - tile * A.sum_blocks;
+  const uint32_t number = A.first_block + blockIdx.x, tile = number / A.sum_blocks, block = number - tile * A.sum_blocks;
   const int64_t n = count_of(A.num, A.max_ids);
   if (tile >= A.tiles) {
-    clear_rows<TG, TINY>(A, n, blockIdx.x - A.sum_blocks * A.tiles, lds);
+    clear_rows<TG, TINY>(A, n, number - A.sum_blocks * A.tiles, lds);
     return;
   }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -649,7 +651,7 @@ __global__ void __launch_bounds__(TINY ? kTinyThreads : kGradThreads) k_embed_su
       all += lds[kWaves + w];
     }
     rank = __builtin_amdgcn_readfirstlane(share);
-    if (blockIdx.x == 0 && threadIdx.x == 0 && (TINY || !A.scanned)) *A.num_unique = all;
+    if (number == 0 && threadIdx.x == 0 && (TINY || !A.scanned)) *A.num_unique = all;
     if (begins && tile == 0) A.row_ids[rank + __popcll(set & ((1ull << lane) - 1))] = static_cast<int32_t>(mine.x);
   }
   if (b0 >= n) return;

@@ -23,6 +23,7 @@ struct NormArgs {
   int64_t y_stride;
   float* mean;
   float* rstd;
+  uint32_t first_block;  // of the launch, where a row is a block's
 };
 
 // Threads of a block whose groups of LANES lanes have a row each.
@@ -108,7 +109,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_layer_norm(NormArgs A) 
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads) k_layer_norm_long(NormArgs A) {
   __shared__ float lds[2][kThreads / 64];
-  const int64_t row = blockIdx.x;
+  const int64_t row = static_cast<int64_t>(A.first_block) + blockIdx.x;
   if (row >= count_of(A.num, A.max_rows)) return;
   const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
   const int vectors = (A.dim + V - 1) / V;
@@ -163,6 +164,7 @@ struct NormGradArgs {
   void* dx;  // or null
   int64_t dx_stride;
   float* part;  // [slices][2][dim]: sums of dy h and of dy over the rows of a slice, or null
+  uint32_t first_block;  // of the launch, where a row is a block's
 };
 
 // As k_layer_norm, a block striding over rows: a lane's columns are the same in each of them, so the sums for dw and db stay in
@@ -305,7 +307,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_layer_norm_grad(NormGra
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads) k_layer_norm_grad_long(NormGradArgs A) {
   __shared__ float lds[2][kThreads / 64];
-  const int64_t row = blockIdx.x;
+  const int64_t row = static_cast<int64_t>(A.first_block) + blockIdx.x;
   if (row >= count_of(A.num, A.max_rows)) return;
   const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
   const T* dy = static_cast<const T*>(A.dy) + row * A.dy_stride;

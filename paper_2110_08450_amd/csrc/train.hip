@@ -39,6 +39,7 @@ void with_type(int32_t type, F f) {
 // The launches of a call, one behind the other.  Behind one that failed there are no more: they would work on scratch that it should have
 // written, places of the output among it.
 class Launches {
+  static constexpr int64_t kLaunchItems = int64_t(1) << 31;
   template <typename T>
   struct Just {
     using type = T;
@@ -51,6 +52,16 @@ class Launches {
     if (error_ != hipSuccess) return;
     void* list[] = {const_cast<void*>(static_cast<const void*>(&args))...};
     error_ = hipLaunchKernel(reinterpret_cast<const void*>(kernel), blocks, dim3(static_cast<unsigned>(threads)), list, 0, stream_);
+  }
+  // One block after the other of a number that a launch may not hold, as it has fewer than 2^32 work items: as many launches as it takes, each
+  // of which finds its first block in the arguments.
+  template <typename A>
+  void all(void (*kernel)(A), int64_t blocks, int threads, A args) {
+    const int64_t most = kLaunchItems / threads;
+    for (int64_t first = 0; first < blocks; first += most) {
+      args.first_block = static_cast<uint32_t>(first);
+      (*this)(kernel, static_cast<unsigned>(blocks - first < most ? blocks - first : most), threads, args);
+    }
   }
   int result() const {
     if (error_ != hipSuccess) (void)hipGetLastError();  // told here, and not once more by who asks next
@@ -68,9 +79,9 @@ constexpr int kVec = 16 / static_cast<int>(sizeof(T));  // columns of a 16-byte 
 // ---- embedding ----------------------------------------------------------------------------------
 
 template <typename TI, typename TO>
-void launch_embedding(const EmbedArgs& A, unsigned blocks, bool vectors, Launches& go) {
-  if (vectors) go(k_embedding<TI, TO, kVec<TO>>, blocks, kThreads, A);
-  else go(k_embedding<TI, TO, 1>, blocks, kThreads, A);
+void launch_embedding(const EmbedArgs& A, int64_t blocks, bool vectors, Launches& go) {
+  if (vectors) go.all(k_embedding<TI, TO, kVec<TO>>, blocks, kThreads, A);
+  else go.all(k_embedding<TI, TO, 1>, blocks, kThreads, A);
 }
 
 // Blocks of k_embed_sums for the tokens, tiles of 64 * V columns, and floats of a row of partial sums.
@@ -81,6 +92,12 @@ GradShape grad_shape(int64_t max_ids, int32_t dim) {
   const int V = grad_columns(dim);
   const int64_t vectors = ceil_div(dim, V);
   return {ceil_div(max_ids, kBlockTokens), ceil_div(vectors, 64), vectors * V};
+}
+
+// Blocks have numbers of 32 bits: fewer than 2^31 that add up (as many are for 2^45 values), and those that clear, at most num_rows, behind them.
+bool too_many_blocks(int64_t max_ids, int32_t dim) {
+  const GradShape G = grad_shape(max_ids, dim);
+  return G.blocks * G.tiles >= kMaxRows;
 }
 
 struct EmbedScratch {
@@ -183,14 +200,13 @@ void launch_embed_sums(EmbedGradArgs A, const GradShape& G, bool clear, Launches
   if (tiny) A.sum_blocks = 1;
   const int64_t blocks = static_cast<int64_t>(A.sum_blocks) * A.tiles + (clear ? ceil_div(A.num_rows, A.clear_rows) : 0);
   if (blocks == 0) return;
-  const unsigned b = static_cast<unsigned>(blocks);
   if (tiny) {
-    if (A.accumulate) go(k_embed_sums<TD, TG, V, true, true>, b, kTinyThreads, A);
-    else go(k_embed_sums<TD, TG, V, true, false>, b, kTinyThreads, A);
+    if (A.accumulate) go.all(k_embed_sums<TD, TG, V, true, true>, blocks, kTinyThreads, A);
+    else go.all(k_embed_sums<TD, TG, V, true, false>, blocks, kTinyThreads, A);
     return;
   }
-  if (A.accumulate) go(k_embed_sums<TD, TG, V, false, true>, b, kGradThreads, A);
-  else go(k_embed_sums<TD, TG, V, false, false>, b, kGradThreads, A);
+  if (A.accumulate) go.all(k_embed_sums<TD, TG, V, false, true>, blocks, kGradThreads, A);
+  else go.all(k_embed_sums<TD, TG, V, false, false>, blocks, kGradThreads, A);
   if (G.blocks < 2) return;
   const uint32_t joins = static_cast<uint32_t>(ceil_div(G.blocks, kJoinWaves));
   const unsigned longs = static_cast<unsigned>((G.blocks - 1) / kJoinShort);
@@ -220,6 +236,7 @@ int embedding_grad(const void* d_ids, int32_t id_bytes, const int64_t* d_num_ids
       (grad_dtype != SMFG_DTYPE_F32 && grad_dtype != dy_dtype) || misaligned(d_ids, static_cast<uintptr_t>(id_bytes)) ||
       misaligned(d_num_ids, 8) || misaligned(d_row_ids, 4) || misaligned(d_num_unique, 8) || misaligned(d_scratch, 256))
     return SMFG_ERR_INVALID_ARG;
+  if (too_many_blocks(max_ids, dim)) return SMFG_ERR_INVALID_ARG;
   if (max_ids == 0 && !rows_only && accumulate) return SMFG_OK;
   Launches go(hip_stream);
   const EmbedScratch S = embed_scratch(max_ids, dim);
@@ -397,22 +414,21 @@ int smfg_embedding(const void* d_table, int64_t num_rows, int64_t table_stride, 
     return SMFG_ERR_INVALID_ARG;
   if (max_ids == 0) return SMFG_OK;
   Launches go(hip_stream);
-  const EmbedArgs A = {d_table, num_rows, table_stride, dim, id_bytes, d_ids, d_num_ids, max_ids, scale, d_out, out_stride};
+  const EmbedArgs A = {d_table, num_rows, table_stride, dim, id_bytes, d_ids, d_num_ids, max_ids, scale, d_out, out_stride, 0};
   const int vector = static_cast<int>(16 / type_bytes(out_dtype));
   const bool vectors = dim >= vector;
   const int64_t blocks = ceil_div(max_ids * ceil_div(dim, vectors ? vector : 1), kEmbedTurns * kThreads);
-  if (blocks > 0x7FFFFFFF) return SMFG_ERR_INVALID_ARG;
-  const unsigned b = static_cast<unsigned>(blocks);
+  if (blocks >= kMaxRows) return SMFG_ERR_INVALID_ARG;
   with_type(out_dtype, [&](auto o) {
     using O = decltype(o);
-    if (table_dtype == SMFG_DTYPE_F32) launch_embedding<float, O>(A, b, vectors, go);
-    else launch_embedding<O, O>(A, b, vectors, go);
+    if (table_dtype == SMFG_DTYPE_F32) launch_embedding<float, O>(A, blocks, vectors, go);
+    else launch_embedding<O, O>(A, blocks, vectors, go);
   });
   return go.result();
 }
 
 int64_t smfg_embedding_grad_scratch_bytes(int64_t max_ids, int64_t num_rows, int32_t dim) {
-  if (bad_dim(dim) || max_ids < 0 || max_ids >= kMaxRows || num_rows < 1 || num_rows >= kMaxRows) return -1;
+  if (bad_dim(dim) || max_ids < 0 || max_ids >= kMaxRows || num_rows < 1 || num_rows >= kMaxRows || too_many_blocks(max_ids, dim)) return -1;
   return embed_scratch(max_ids, dim).bytes;
 }
 
@@ -440,10 +456,10 @@ int smfg_layer_norm(const void* d_x, int64_t x_stride, int32_t dtype, const int6
     return SMFG_ERR_INVALID_ARG;
   if (max_rows == 0) return SMFG_OK;
   Launches go(hip_stream);
-  const NormArgs A = {d_x, x_stride, d_num_rows, max_rows, dim, param_dtype == SMFG_DTYPE_F32, d_w, d_b, eps, d_y, y_stride, d_mean, d_rstd};
+  const NormArgs A = {d_x, x_stride, d_num_rows, max_rows, dim, param_dtype == SMFG_DTYPE_F32, d_w, d_b, eps, d_y, y_stride, d_mean, d_rstd, 0};
   with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    if (!with_row_shape<T, 2048>(dim, LaunchNorm<T>{A, go})) go(k_layer_norm_long<T, kVec<T>>, static_cast<unsigned>(max_rows), kThreads, A);
+    if (!with_row_shape<T, 2048>(dim, LaunchNorm<T>{A, go})) go.all(k_layer_norm_long<T, kVec<T>>, max_rows, kThreads, A);
   });
   return go.result();
 }
@@ -469,7 +485,7 @@ int smfg_layer_norm_grad(const void* d_dy, int64_t dy_stride, const void* d_x, i
   if (sums && scratch_bytes < up256(slices * 8 * dim)) return SMFG_ERR_CAPACITY;
   Launches go(hip_stream);
   float* part = sums ? static_cast<float*>(d_scratch) : nullptr;
-  const NormGradArgs A = {d_dy, dy_stride, d_x, x_stride, d_num_rows, max_rows, dim, param_dtype == SMFG_DTYPE_F32, d_w, d_mean, d_rstd, d_dx, dx_stride, part};
+  const NormGradArgs A = {d_dy, dy_stride, d_x, x_stride, d_num_rows, max_rows, dim, param_dtype == SMFG_DTYPE_F32, d_w, d_mean, d_rstd, d_dx, dx_stride, part, 0};
   if (!sums && (max_rows == 0 || !d_dx)) return SMFG_OK;
   if (max_rows > 0) {
     with_type(dtype, [&](auto t) {
@@ -480,7 +496,7 @@ int smfg_layer_norm_grad(const void* d_dy, int64_t dy_stride, const void* d_x, i
         if (slices > kNormLongSlices) slices = kNormLongSlices;
         go(k_norm_grad_columns<T, V>, dim3(static_cast<unsigned>(ceil_div(ceil_div(dim, V), kThreads)), static_cast<unsigned>(slices)), kThreads, A);
       }
-      if (d_dx) go(k_layer_norm_grad_long<T, V>, static_cast<unsigned>(max_rows), kThreads, A);
+      if (d_dx) go.all(k_layer_norm_grad_long<T, V>, max_rows, kThreads, A);
     });
   }
   if (sums) {
@@ -506,7 +522,7 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
   for (int i = 0; i < num_grads; ++i)
     if (grads[i].numel > 0 && !grads[i].grad) return SMFG_ERR_NULL_PTR;
   const ClipScratch S = clip_scratch(grads, num_grads);
-  if (S.blocks > 0x7FFFFFFF) return SMFG_ERR_INVALID_ARG;
+  if (S.blocks >= kMaxRows) return SMFG_ERR_INVALID_ARG;
   if (scratch_bytes < S.bytes) return SMFG_ERR_CAPACITY;
   Launches go(hip_stream);
   uint8_t* scratch = static_cast<uint8_t*>(d_scratch);
@@ -517,6 +533,7 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
   A.table = table ? reinterpret_cast<ClipTensor*>(scratch + S.table) : nullptr;
   A.tensors = S.tensors;
   A.first = A.here = 0;
+  A.first_block = 0;
   A.blocks = 0;
   A.chunk = S.chunk;
   A.part = part;
@@ -538,13 +555,13 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
   }
   if (table) go(k_clip_table, 1, 64, A);
   if (A.blocks > 0) {
-    if (table) go(k_clip_squares<true>, A.blocks, kThreads, A);
-    else go(k_clip_squares<false>, A.blocks, kThreads, A);
+    if (table) go.all(k_clip_squares<true>, A.blocks, kThreads, A);
+    else go.all(k_clip_squares<false>, A.blocks, kThreads, A);
   }
   if (A.blocks == 0 || A.blocks > kClipJoin) go(k_clip_norm, 1, kClipNormThreads, A);
   if (A.blocks > 0) {
-    if (table) go(k_clip_scale<true>, A.blocks, kThreads, A);
-    else go(k_clip_scale<false>, A.blocks, kThreads, A);
+    if (table) go.all(k_clip_scale<true>, A.blocks, kThreads, A);
+    else go.all(k_clip_scale<false>, A.blocks, kThreads, A);
   }
   return go.result();
 }
