@@ -61,16 +61,16 @@ __device__ __forceinline__ void load_params(const void* p, bool is_float, int c,
   }
 }
 
-// Sum over groups of LANES lanes, in every lane; LANES of a whole block go through `lds`, a float per wave.  Between two sums through the
+// Sum over groups of LANES lanes, in every lane; LANES of a whole block go through `lds`, a number per wave.  Between two sums through the
 // same array has to be one through another: its barrier tells that the first has been read.
-template <int LANES>
-__device__ __forceinline__ float group_sum(float x, float* lds) {
+template <int LANES, typename S>
+__device__ __forceinline__ S group_sum(S x, S* lds) {
 #pragma unroll
   for (int o = 1; o < (LANES < 64 ? LANES : 64); o <<= 1) x += __shfl_xor(x, o, 64);
   if constexpr (LANES > 64) {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
-    x = 0.f;
+    x = 0;
 #pragma unroll
     for (int w = 0; w < LANES / 64; ++w) x += lds[w];
   }

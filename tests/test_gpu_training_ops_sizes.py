@@ -4,7 +4,7 @@ import torch
 
 from paper_2110_08450_amd import binding as smfg
 
-from test_gpu_training_ops import BF16, DEV, F16, F32, count
+from test_gpu_training_ops import BF16, DEV, F16, F32, check, count, rounded
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +44,55 @@ def test_gradient_of_a_table_of_2_31_rows(n):
     g[at] = 0
     for piece in g.split(2 ** 28):
         assert int(torch.count_nonzero(piece)) == 0
+
+
+# ---- long rows ----------------------------------------------------------------------------------
+
+U = 2.0 ** -24
+LONG = [(20_480, F32, 100.1, 0.0), (65_536, F32, 100.1, 0.0), (2 ** 20, F32, 100.1, 0.0), (2 ** 20, F32, 1.1, 0.0), (2 ** 20 + 3, BF16, 100.1, 0.0),
+        (2 ** 20 + 5, F16, 1.1, 0.0), (65_539, F32, 1000.0, 1.0), (2 ** 20, F32, -100.1, 0.5), (65_536, F16, 30.0, 0.5), (20_000, BF16, -1.1, 0.1)]
+
+
+@pytest.mark.parametrize("dim,dtype,centre,spread", LONG)
+def test_layer_norm_of_long_rows_off_centre(dim, dtype, centre, spread):
+    """Whatever the row's length, a mean is off by its one rounding to float, dm; the centred values by it and theirs; the variance by dm^2 and two
+    roundings of each value; 1 / sqrt(variance + eps) by four more."""
+    n, eps = 5, 1e-5
+    x = (centre + spread * torch.randn((n, dim), device=DEV, generator=torch.Generator(device=DEV).manual_seed(dim))).to(dtype)
+    w, b = torch.full((dim,), 1.5, device=DEV), torch.linspace(-1, 1, dim, device=DEV)
+    y, mean, rstd = torch.empty_like(x), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    smfg.layer_norm(x, count(n), n, w, b, eps, y, mean, rstd)
+    xd = x.double()
+    m = xd.mean(1, keepdim=True)
+    d = xd - m
+    var = (d * d).mean(1, keepdim=True)
+    r = 1 / torch.sqrt(var + eps)
+    dm = 1.001 * U * m.abs()
+    share = 6 * U + dm * dm / (2 * (var + eps))
+    want = d * r * w.double() + b.double()
+    tol = 1.5 * r * dm * (1 + share) + (want - b.double()).abs() * (share + 4 * U) + U * (want.abs() + b.double().abs())
+    check(y, want, rounded(1.01 * tol, want, dtype))
+    check(mean, m[:, 0], dm[:, 0])
+    check(rstd, r[:, 0], (r * share)[:, 0] * 1.01)
+
+
+@pytest.mark.parametrize("dim,dtype,centre,spread", LONG)
+def test_layer_norm_grad_of_long_rows_off_centre(dim, dtype, centre, spread):
+    """The same of the input's gradient, where dy is far off centre: products and differences are rounded once each, the means once more, whatever
+    the row's length."""
+    n = 5
+    g = torch.Generator(device=DEV).manual_seed(dim)
+    dy = (centre + spread * torch.randn((n, dim), device=DEV, generator=g)).to(dtype)
+    x = (0.3 + torch.randn((n, dim), device=DEV, generator=g)).to(dtype)
+    w = 1 + 0.25 * torch.rand(dim, device=DEV, generator=g) if spread else torch.ones(dim, device=DEV)
+    var, mean = torch.var_mean(x.float(), 1, correction=0)
+    rstd = (var + 1e-5).rsqrt()
+    dx = torch.empty_like(x)
+    smfg.layer_norm_grad(dy, x, count(n), n, w, mean, rstd, dx, None, None, None)
+    m, r = mean.double()[:, None], rstd.double()[:, None]
+    h, gw = (x.double() - m) * r, dy.double() * w.double()
+    c1, c2, both = gw.mean(1, keepdim=True), (gw * h).mean(1, keepdim=True), (gw * h).abs().mean(1, keepdim=True)
+    want = r * (gw - c1 - h * c2)
+    tol = U * (gw.abs() + gw.abs().mean(1, keepdim=True) + c1.abs() + h.abs() * (4 * both + c2.abs()) + 3 * (h * c2).abs()
+               + 2 * (gw.abs() + c1.abs() + (h * c2).abs()))
+    check(dx, want, rounded(1.01 * (r * tol + U * want.abs()), want, dtype))
