@@ -367,7 +367,8 @@ int smfg_layer_norm_grad(const void *d_dy, int64_t dy_stride, const void *d_x, i
  * Global norm over any number of gradients, and clipping:
  *   N = sqrt(sum over all elements of (scale g)^2),  out = scale * min(1, max_norm / (N + 1e-6)) * g
  * scale undoes a loss scale or averages micro-batches; max_norm > 0, infinite: no clipping.  *d_norm = N (device float).  Squares
- * are added in double.  A NaN among the gradients makes N and all outputs NaN; an infinite one makes N infinite, so finite ones 0.
+ * are added in double.  A NaN among the gradients makes N and all outputs NaN, whatever max_norm is.  An infinite one makes N infinite, so
+ * finite ones 0; with an infinite max_norm nothing is clipped then either, and they are scaled alone.
  * Gradients that are clipped in place are not written again where scale and factor multiply to one.
  */
 typedef struct {

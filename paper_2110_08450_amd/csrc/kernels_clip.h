@@ -173,7 +173,7 @@ __device__ __forceinline__ float factor_of(const double* part, int64_t parts, fl
   for (int w = 0; w < THREADS / 64; ++w) s += lds[w];
   const double n = fabs(static_cast<double>(scale)) * sqrt(s), c = max_norm / (n + 1e-6);
   norm = static_cast<float>(n);
-  return static_cast<float>(scale * (__builtin_isinf(max_norm) || c >= 1.0 ? 1.0 : c));  // NaN stays NaN
+  return static_cast<float>(scale * (c >= 1.0 || (__builtin_isinf(max_norm) && n == n) ? 1.0 : c));  // of a NaN among the gradients NaN
 }
 
 // Up to kClipJoin blocks every one of k_clip_scale adds up all sums itself; of more a launch of one block does (nine tensors of 281 K floats in all, 142

@@ -96,3 +96,25 @@ def test_layer_norm_grad_of_long_rows_off_centre(dim, dtype, centre, spread):
     tol = U * (gw.abs() + gw.abs().mean(1, keepdim=True) + c1.abs() + h.abs() * (4 * both + c2.abs()) + 3 * (h * c2).abs()
                + 2 * (gw.abs() + c1.abs() + (h * c2).abs()))
     check(dx, want, rounded(1.01 * (r * tol + U * want.abs()), want, dtype))
+
+
+# ---- clipping -----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("scale", [1.0, 0.5])
+@pytest.mark.parametrize("tensors,numel", [(2, 10), (90, 3000), (3, 1_000_000)])
+def test_no_limit_lets_a_nan_through_and_clips_nothing_else(tensors, numel, scale):
+    """max_norm infinite: a NaN makes everything NaN, in place and into other buffers; an infinite norm leaves finite gradients what they are."""
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        for in_place in (True, False):
+            grads = [torch.full((numel,), 3.0, dtype=(F32, F16, BF16)[i % 3], device=DEV) for i in range(tensors)]
+            grads[tensors // 2][numel - 1] = bad
+            outs = [None if in_place else torch.full((numel,), 7.0, device=DEV) for _ in grads]
+            norm = torch.zeros(1, device=DEV)
+            smfg.clip_grad_norm(smfg.grad_list(grads, outs), float("inf"), norm, scale=scale)
+            got = torch.cat([(g if o is None else o).float() for g, o in zip(grads, outs)])
+            if bad != bad:
+                assert norm.isnan().all() and got.isnan().all()
+            else:
+                want = torch.full_like(got, 3.0 * scale)
+                want[tensors // 2 * numel + numel - 1] = bad
+                assert float(norm) == float("inf") and torch.equal(got, want)
