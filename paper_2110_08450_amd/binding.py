@@ -584,7 +584,7 @@ def grad_list(grads: Sequence[torch.Tensor], outs: Optional[Sequence[Optional[to
     nbytes = int(lib().smfg_clip_grad_norm_scratch_bytes(c, n))
     if device is None and n > 0:
         device = grads[0].device
-    return GradList(c, n, Scratch(nbytes, "smfg_clip_grad_norm_scratch_bytes", device), (list(grads), outs, rows))
+    return GradList(c, n, Scratch(nbytes, "smfg_clip_grad_norm_scratch_bytes", device), [list(ts) for ts in (grads, outs, rows) if ts is not None])
 
 
 def clip_grad_norm(grads: GradList, max_norm: float, norm: torch.Tensor, scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
