@@ -526,7 +526,6 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
   if (scratch_bytes < S.bytes) return SMFG_ERR_CAPACITY;
   Launches go(hip_stream);
   uint8_t* scratch = static_cast<uint8_t*>(d_scratch);
-  float* factor = static_cast<float*>(d_scratch);
   double* part = reinterpret_cast<double*>(scratch + S.part);
   const bool table = S.tensors > kClipTensors;
   ClipArgs A;
@@ -537,7 +536,7 @@ int smfg_clip_grad_norm(const smfg_grad_t* grads, int32_t num_grads, float scale
   A.blocks = 0;
   A.chunk = S.chunk;
   A.part = part;
-  A.factor = factor;
+  A.factor = static_cast<ClipFactor*>(d_scratch);
   A.norm = d_norm;
   A.scale = scale;
   A.max_norm = max_norm;

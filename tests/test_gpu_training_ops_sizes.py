@@ -118,3 +118,21 @@ def test_no_limit_lets_a_nan_through_and_clips_nothing_else(tensors, numel, scal
                 want = torch.full_like(got, 3.0 * scale)
                 want[tensors // 2 * numel + numel - 1] = bad
                 assert float(norm) == float("inf") and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("numel,value,limit,scale", [(10, 1e38, 1e-6, 1.0), (3_000_000, 3e38, 1e-3, 0.25), (1000, -2e35, 1e-9, 4.0), (5, 1e30, 1e-20, 1.0),
+                                                     (70_000, 1e20, 1e-12, 1.0), (100, 3e38, 1e-38, 1.0), (9, 3.0, 1e-30, 1.0), (9, 1e-3, 1.0, 2.0 ** -110)])
+def test_clipping_of_norms_that_leave_a_float_no_digits_for_the_factor(numel, value, limit, scale):
+    """A clipped value has the factor's rounding, the product's and the output's, also where the factor itself is below a float's normal range."""
+    g = torch.full((numel,), value, device=DEV) * torch.linspace(0.5, 1, numel, device=DEV)
+    small = torch.tensor([1e-30, value * 1e-12], device=DEV)
+    b = (torch.ones(numel, device=DEV) * min(abs(value), 1e38)).to(BF16)
+    out = torch.zeros(numel, device=DEV)
+    total = torch.cat([g, small, b.float()]).double() * scale
+    n64 = float(torch.linalg.vector_norm(total))
+    factor = scale * min(1.0, limit / (n64 + 1e-6))
+    want = [t.double() * factor for t in (g, small, b)]
+    norm = torch.zeros(1, device=DEV)
+    smfg.clip_grad_norm(smfg.grad_list([g, small, b], [None, None, out]), limit, norm, scale=scale)
+    for got, w in zip((g, small, out), want):
+        check(got, w, rounded(4 * U * w.abs(), w, F32))
