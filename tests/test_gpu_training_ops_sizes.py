@@ -4,7 +4,7 @@ import torch
 
 from paper_2110_08450_amd import binding as smfg
 
-from test_gpu_training_ops import BF16, DEV, F16, F32, check, count, rounded
+from test_gpu_training_ops import BF16, DEV, F16, F32, check, count, norm_grad_of, norm_inputs, norm_of, rounded, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -136,3 +136,113 @@ def test_clipping_of_norms_that_leave_a_float_no_digits_for_the_factor(numel, va
     smfg.clip_grad_norm(smfg.grad_list([g, small, b], [None, None, out]), limit, norm, scale=scale)
     for got, w in zip((g, small, out), want):
         check(got, w, rounded(4 * U * w.abs(), w, F32))
+
+
+# ---- more rows than a launch has at once ---------------------------------------------------------
+#
+# k_layer_norm has at most 2048 blocks, k_layer_norm_grad 1024 slices, k_norm_grad_columns 64: every shape of a row's lanes with several rows to
+# each of them, the count ending between two blocks' turns.
+MANY = [(70_001, 3, F32, F32, 1), (140_007, 31, F16, F32, 2), (200_000, 32, F16, F16, 0), (70_003, 57, BF16, F32, 0), (70_000, 64, F16, F32, 3), (70_000, 100, F16, F32, 0),
+        (40_001, 64, F32, F32, 0), (20_005, 250, BF16, BF16, 1), (20_000, 200, F32, F32, 0), (20_000, 1024, F16, F32, 0), (9001, 512, F32, F32, 5), (5000, 2048, F16, F16, 0),
+        (5003, 1500, F32, F32, 0), (5000, 4096, BF16, F32, 0), (4500, 6143, F16, F32, 0), (5000, 8192, F16, F16, 0), (4400, 7001, F32, F32, 1), (4300, 12_288, BF16, F32, 0),
+        (4200, 16_384, F16, F32, 0), (4200, 8192, F32, F32, 0), (3000, 8193, F32, F32, 1), (2500, 20_001, F16, F32, 0), (300, 16_385, BF16, BF16, 2)]
+
+
+@pytest.mark.parametrize("cap,dim,dtype,ptype,pad", MANY)
+def test_layer_norm_of_many_rows(cap, dim, dtype, ptype, pad):
+    n = cap - cap // 37 - 1
+    x, w, b = norm_inputs(n, cap, dim, dtype, ptype, pad)
+    y, wide = strided((cap, dim), dtype, pad, 5)
+    before = wide.clone()
+    mean, rstd = torch.full((cap,), 7.0, device=DEV), torch.full((cap,), 7.0, device=DEV)
+    smfg.layer_norm(x, count(n), cap, w, b, 1e-5, y, mean, rstd)
+    for at in range(0, n, 1000):
+        rows = slice(at, min(n, at + 1000))
+        want, m, r, tol, tm, tr = norm_of(x[rows], w, b, 1e-5)
+        check(y[rows], want, rounded(tol, want, dtype))
+        check(mean[rows], m, rounded(tm, m, F32))
+        check(rstd[rows], r, rounded(tr, r, F32))
+    assert bool((mean[n:] == 7).all()) and bool((rstd[n:] == 7).all())
+    before[:n, :dim] = y[:n]
+    assert torch.equal(wide.view(torch.int16), before.view(torch.int16))
+    z = x.clone()
+    smfg.layer_norm(z, count(n), cap, w, b, 1e-5, z)
+    assert torch.equal(z[:n], y[:n]) and torch.equal(z[n:], x[n:])
+
+
+@pytest.mark.parametrize("cap,dim,dtype,ptype,pad", MANY)
+def test_layer_norm_grad_of_many_rows(cap, dim, dtype, ptype, pad):
+    """Statistics that make (x - mean) * rstd whole numbers, and whole dy: every sum over the rows is exact, so that no row is left out or counted twice.
+    dx into a buffer of its own, and in the place of dy and of x."""
+    n = cap - cap // 41 - 1
+    g = torch.Generator(device=DEV).manual_seed(dim)
+
+    def whole(*shape, most=2):
+        return torch.randint(-most, most + 1, shape, device=DEV, generator=g)
+
+    x, _ = strided((cap, dim), dtype, pad, 1)
+    dy, _ = strided((cap, dim), dtype, pad, 2)
+    x.copy_(whole(cap, dim))
+    dy.copy_(whole(cap, dim, most=1))
+    w = (1 + 0.2 * torch.randn(dim, device=DEV, generator=g)).to(ptype)
+    mean, rstd = whole(cap, most=1).float(), 2.0 ** whole(cap, most=1).abs().float()
+    x[n:], dy[n:], mean[n:] = float("nan"), float("nan"), float("nan")
+    ws = smfg.layer_norm_grad_workspace(cap, dim)
+    dx, wide = strided((cap, dim), dtype, pad, 7)
+    before = wide.clone()
+    dw, db = torch.full((dim,), 9.0, device=DEV).to(ptype), torch.full((dim,), 9.0, device=DEV).to(ptype)
+    smfg.layer_norm_grad(dy, x, count(n), cap, w, mean, rstd, dx, dw, db, ws)
+    sums = torch.zeros((2, dim), dtype=torch.float64, device=DEV)
+    for at in range(0, n, 1000):
+        rows = slice(at, min(n, at + 1000))
+        wx, sw, sb, tx, _, _ = norm_grad_of(dy[rows], x[rows], w, mean[rows], rstd[rows])
+        check(dx[rows], wx, rounded(tx, wx, dtype))
+        sums += torch.stack([sw, sb])
+    assert float(sums.abs().max()) * 8 < 2 ** 24 and cap * 12 < 2 ** 24  # also of magnitudes
+    assert torch.equal(dw, sums[0].to(ptype)) and torch.equal(db, sums[1].to(ptype))
+    before[:n, :dim] = dx[:n]
+    assert torch.equal(wide.view(torch.int16), before.view(torch.int16))
+    for which in (0, 1):
+        given = [dy.clone(), x.clone()]
+        a, b = torch.full_like(dw, 9), torch.full_like(db, 9)
+        smfg.layer_norm_grad(given[0], given[1], count(n), cap, w, mean, rstd, given[which], a, b, ws)
+        assert torch.equal(given[which][:n], dx[:n]) and bool(given[which][n:].isnan().all())
+        assert torch.equal(a, dw) and torch.equal(b, db)
+
+
+@pytest.mark.parametrize("n,spare,dim,dtype,ptype,pad", [(9, 1, 8194, F16, F32, 0), (7, 0, 10_000, BF16, BF16, 1), (5, 2, 12_289, F16, F16, 3), (4, 0, 12_288, BF16, F32, 0),
+                                                         (5, 0, 16_384, F16, F32, 0), (3, 1, 16_385, BF16, F32, 1), (3, 0, 30_007, F16, F16, 5), (2, 0, 70_000, BF16, F32, 0)])
+def test_layer_norm_and_gradient_of_long_half_rows(n, spare, dim, dtype, ptype, pad):
+    cap = n + spare
+    x, w, b = norm_inputs(n, cap, dim, dtype, ptype, pad)
+    y, mean, rstd = torch.full((cap, dim), 4.0, dtype=dtype, device=DEV), torch.zeros(cap, device=DEV), torch.zeros(cap, device=DEV)
+    smfg.layer_norm(x, count(n), cap, w, b, 1e-5, y, mean, rstd)
+    want, m, r, tol, tm, tr = norm_of(x[:n], w, b, 1e-5)
+    check(y[:n], want, rounded(tol, want, dtype))
+    check(mean[:n], m, rounded(tm, m, F32))
+    check(rstd[:n], r, rounded(tr, r, F32))
+    assert bool((y[n:] == 4).all())
+    dy, _ = strided((cap, dim), dtype, pad + 1, 6)
+    dx, dw, db = torch.full_like(y, 4), torch.empty_like(w), torch.empty_like(w)
+    smfg.layer_norm_grad(dy, x, count(n), cap, w, mean, rstd, dx, dw, db, smfg.layer_norm_grad_workspace(cap, dim))
+    wx, ww, wb, tx, tw, tb = norm_grad_of(dy[:n], x[:n], w, mean[:n], rstd[:n])
+    check(dx[:n], wx, rounded(tx, wx, dtype))
+    check(dw, ww, rounded(tw, ww, ptype))
+    check(db, wb, rounded(tb, wb, ptype))
+    assert bool((dx[n:] == 4).all())
+    z = x.clone()  # dx in the place of x, without the sums
+    smfg.layer_norm_grad(dy, z, count(n), cap, w, mean, rstd, z, None, None, None)
+    assert torch.equal(z[:n], dx[:n]) and torch.equal(z[n:], x[n:])
+
+
+@pytest.mark.parametrize("n,rows,dim,dtype,pad", [(600, 5000, 3, F16, 5), (8000, 16_001, 1, F32, 3), (20_000, 50_000, 3, BF16, 2), (20_000, 50_001, 1, F32, 1),
+                                                  (9000, 70_000, 7, F16, 1), (300_000, 600_001, 1, F16, 1)])
+def test_gradient_of_narrow_rows_apart(n, rows, dim, dtype, pad):
+    """Rows shorter than a vector in a wider buffer, cleared beside the sort: what is between them stays."""
+    ids = torch.randint(-1, rows, (n,), device=DEV, generator=torch.Generator(device=DEV).manual_seed(n))
+    dy = torch.ones((n, dim), dtype=dtype, device=DEV)
+    g, wide = strided((rows, dim), dtype, pad, 7)
+    before = wide.clone()
+    smfg.embedding_grad(ids, count(n), n, dy, g, smfg.embedding_grad_workspace(n, rows, dim))
+    before[:, :dim] = torch.bincount(ids[ids >= 0], minlength=rows)[:, None].to(dtype)
+    assert torch.equal(wide.view(torch.int16), before.view(torch.int16))
