@@ -321,8 +321,9 @@ int smfg_embedding(const void *d_table, int64_t num_rows, int64_t table_stride, 
                    int64_t out_stride, int32_t out_dtype, void *hip_stream);
 
 /*
- * Its gradient: G[v, :] = scale * sum of dy[i, :] over i < *d_num_ids with ids[i] = v, in the order of i; ids outside
- * [0, num_rows) have none.  d_dy: max_ids x dim.  The gradient is of float or of dy's type.
+ * Its gradient: G[v, :] = scale * sum of dy[i, :] over i < *d_num_ids with ids[i] = v; ids outside [0, num_rows) have none.
+ * The sum is made of partial sums over pieces of the sorted ids: a fixed order for given ids and max_ids, but not that of i, and not
+ * that of the same tokens among other ids.  d_dy: max_ids x dim.  The gradient is of float or of dy's type.
  *   smfg_embedding_grad       the whole table's, num_rows x dim: rows that no id names are zeros; with accumulate != 0 it
  *                             is added to what d_grad holds, and those rows are not touched
  *   smfg_embedding_grad_rows  the touched rows alone: their number *d_num_unique, their ids ascending in d_row_ids [max_ids] and

@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kThreads) k_embedding(EmbedArgs A) {
 
 // ---- ids sorted by row -------------------------------------------------------------------------
 //
-// (row, token), stable: equal ids stay in the order of their tokens, so that a row's sum has one order, whatever the schedule.
+// (row, token), stable: equal ids stay in the order of their tokens, so that the parts of a row's sum are the same whatever the schedule.
 //
 // Up to kSmallSort ids: every token counts the ids that belong before its own, in one launch.  More: digits of at most kSortBits
 // bits from the lowest on, a launch that counts the digits of every tile and one that scatters.  Up to kSortColumns tiles the block
@@ -99,10 +99,9 @@ struct SortArgs {
   int64_t clear_rows, clear_width, clear_stride;
 };
 
-// The sort leaves most of the chip idle and waits for memory, so part of the gradient is cleared beside each of its launches, where most rows
-// are untouched (see early_clear): 16 K tokens of 1024 columns into 50 K rows of floats 72.6 -> 69.0 us, 300 K of 64 into 2 M 172 -> 149 (the sums took longer then).  A block has
-// every gridDim - own_blocks-th
-// vector, or row where rows are apart.
+// The sort leaves most of the chip idle and waits for memory, so part of the gradient is cleared beside each of its launches where most rows are
+// untouched (see early_clear): 16 K tokens of 1024 columns into 50 K rows of floats 72.6 -> 69.0 us, 300 K of 64 into 2 M 172 -> 149 (with sums that
+// took longer than now).  Of n blocks that clear, each has every n-th piece of blockDim vectors, or every n-th row where rows are apart.
 __device__ __forceinline__ void clear_beside(const SortArgs& A) {
   typedef Elems<uint16_t, 8> Vector;
   const uint32_t block = blockIdx.x - A.own_blocks, blocks = gridDim.x - A.own_blocks;
