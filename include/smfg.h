@@ -365,6 +365,60 @@ int smfg_layer_norm_grad(const void *d_dy, int64_t dy_stride, const void *d_x, i
                          void *d_scratch, int64_t scratch_bytes, void *hip_stream);
 
 /*
+ * Root-mean-square norm of rows i < *d_num_rows, with the addition of a residual before it and an output in 8 bits with scales:
+ *   t_i = x_i + residual_i, rounded to dtype (t = x without a residual),  r_i = 1 / sqrt(mean of t_i^2 + eps),  y[i, j] = t[i, j] r_i w[j]
+ * The norm is of the rounded sum, which is the one that the gradient reads.
+ *   d_x, d_residual, d_total  of dtype; d_residual NULL: none; d_total: the sum t, or NULL (always without a residual).  d_total may be d_x or
+ *             d_residual with the same stride.
+ *   d_w       [dim] of param_dtype, which is float or dtype, or NULL (ones).  eps >= 0.
+ *   d_y       of y_dtype: dtype (y may be x or the residual then, with the same stride), or
+ *               SMFG_DTYPE_I8    y = s q, q a whole number in [-127, 127], s = (largest |y|) / 127
+ *               SMFG_DTYPE_E4M3  y = s q, q a float of 8 bits (4 of exponent, 3 of mantissa, no infinities), s = (largest |y|) / 448
+ *             for every `group` consecutive columns of a row (32, 64 or 128; 0: the whole row), q rounded to nearest even.  A largest value below
+ *             2^-120 counts as 0: s = 0, q = 0.  With an infinity or a NaN among the values s is NaN and q = 0.
+ *   d_scales  float, s of group k of row i at i * scales_stride + k; NULL if y is of dtype
+ *   d_rstd    float [max_rows], r for the gradient, or NULL
+ * Squares are added in float (in double in rows of over 16384 halfs or 8192 floats).
+ */
+#define SMFG_DTYPE_I8 3   /* outputs of smfg_rms_norm alone */
+#define SMFG_DTYPE_E4M3 4 /* the same */
+int smfg_rms_norm(const void *d_x, int64_t x_stride, int32_t dtype, const void *d_residual, int64_t residual_stride, void *d_total,
+                  int64_t total_stride, const int64_t *d_num_rows, int64_t max_rows, int32_t dim, const void *d_w, int32_t param_dtype,
+                  float eps, void *d_y, int64_t y_stride, int32_t y_dtype, float *d_scales, int64_t scales_stride, int32_t group,
+                  float *d_rstd, void *hip_stream);
+/*
+ * Its gradient, with n = t r and g = dy w:
+ *   dx = r (g - n mean(g n)) + dtotal,  dw[j] = sum over rows of dy n
+ *   d_t       the sum (x without a residual).  d_dtotal: the gradient that reaches the sum from elsewhere, or NULL.  dx is the gradient of x and of
+ *             the residual alike.
+ *   d_dy, d_t, d_dtotal, d_dx  of dtype; dx may be any of the others with the same stride; NULL: not wanted.  d_dw: [dim] of param_dtype, or NULL.
+ */
+int64_t smfg_rms_norm_grad_scratch_bytes(int64_t max_rows, int32_t dim);
+int smfg_rms_norm_grad(const void *d_dy, int64_t dy_stride, const void *d_t, int64_t t_stride, int32_t dtype, const void *d_dtotal,
+                       int64_t dtotal_stride, const int64_t *d_num_rows, int64_t max_rows, int32_t dim, const void *d_w, int32_t param_dtype,
+                       const float *d_rstd, void *d_dx, int64_t dx_stride, void *d_dw, void *d_scratch, int64_t scratch_bytes,
+                       void *hip_stream);
+
+/*
+ * Softmax cross entropy over rows i < *d_num_rows of logits, and their gradient in the same pass:
+ *   loss_i = log(sum over j of exp(x[i, j])) - x[i, y_i],  dx[i, j] = c (softmax(x_i)[j] - [j = y_i])
+ * A row whose label is outside [0, classes) does not count: its loss is 0, its gradient zeros, whatever its logits are.
+ *   d_logits, d_dlogits  of dtype, max_rows x classes; classes in [1, SMFG_MAX_DIM]; dlogits may be logits with the same stride; NULL: not wanted
+ *   d_labels  int32 or int64 (label_bytes 4 or 8) [max_rows]
+ *   reduction SMFG_LOSS_MEAN: *d_loss is the mean of the counted rows' losses (0 of none), c = scale / their number;
+ *             SMFG_LOSS_SUM: their sum, c = scale.  scale (a loss scale, the share of a micro-batch) does not act on the loss.
+ *   d_row_loss  float [max_rows], or NULL
+ * A logit of -infinity has probability 0, and an infinite loss where it is the label's.  A counted row with a NaN, with +infinity or with -infinity alone
+ * has a loss and a gradient of NaN.  Exponentials below 2^-126 of the row's largest are zeros.  Losses are added in double.
+ */
+#define SMFG_LOSS_MEAN 0
+#define SMFG_LOSS_SUM 1
+int64_t smfg_cross_entropy_scratch_bytes(int64_t max_rows, int32_t classes);
+int smfg_cross_entropy(const void *d_logits, int64_t logits_stride, int32_t dtype, const void *d_labels, int32_t label_bytes,
+                       const int64_t *d_num_rows, int64_t max_rows, int32_t classes, int32_t reduction, float scale, float *d_loss,
+                       float *d_row_loss, void *d_dlogits, int64_t dlogits_stride, void *d_scratch, int64_t scratch_bytes, void *hip_stream);
+
+/*
  * Global norm over any number of gradients, and clipping:
  *   N = sqrt(sum over all elements of (scale g)^2),  out = scale * min(1, max_norm / (N + 1e-6)) * g
  * scale undoes a loss scale or averages micro-batches; max_norm > 0, infinite: no clipping.  *d_norm = N (device float).  Squares
@@ -383,6 +437,52 @@ typedef struct {
 int64_t smfg_clip_grad_norm_scratch_bytes(const smfg_grad_t *grads, int32_t num_grads);
 int smfg_clip_grad_norm(const smfg_grad_t *grads /* host */, int32_t num_grads, float scale, float max_norm, float *d_norm,
                         void *d_scratch, int64_t scratch_bytes, void *hip_stream);
+
+/*
+ * One step of AdamW over any number of tensors, in place:
+ *   g' = f g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *   p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),  f = scale min(1, max_norm / (norm + 1e-6))
+ * With d_norm (the norm of smfg_clip_grad_norm, called with an infinite max_norm and no outputs) gradients are clipped here, and not written; where
+ * *d_norm is not finite the step is not taken: nothing is written.  Without it f = scale.
+ * A tensor is of rows of row_elems elements (0: a single row of numel).  With d_row_ids the gradient's row i is that of row d_row_ids[i] of a table of
+ * num_rows rows (param, m, v and copy), whose other rows are left as they are: the touched rows that smfg_embedding_grad_rows tells.  These ids are
+ * distinct; one outside [0, num_rows) is left out.
+ * m and v are of float (state_bits 32), or of 8 bits: every SMFG_STATE_BLOCK consecutive elements of a row (the last of a row may be fewer) share two floats,
+ * A in m_scale and B in v_scale, of ceil(row_elems / SMFG_STATE_BLOCK) a row, and
+ *   m = A (k / 127) |k / 127| with k int8,  v = (B (k / 255)^2)^2 with k uint8
+ * are what is next to the value in k, A and B being the largest |m| and sqrt(v) of the elements; v > 0 is kept as k >= 1.  A below 2^-100 counts as 0.
+ * An infinity or a NaN in m or v makes the kept state of its block NaN.  Zeroed memory is the state of zeros, of either kind.  The step itself uses m
+ * and v before they are rounded.
+ */
+#define SMFG_STATE_BLOCK 128
+typedef struct {
+  void *param;           /* device, of param_dtype */
+  const void *grad;      /* device, numel elements of grad_dtype: float, or param_dtype, or any if the parameters are of float */
+  void *m, *v;           /* device, as many elements as param */
+  float *m_scale, *v_scale; /* device, for states of 8 bits */
+  void *copy;            /* device, of copy_dtype (half or bfloat16): the new parameters, rounded, if these are of float; or NULL */
+  int64_t numel;         /* of grad; >= 0 */
+  int32_t param_dtype, grad_dtype, copy_dtype, state_bits;
+  float weight_decay;    /* >= 0 */
+  int64_t row_elems;     /* numel is a multiple */
+  const int64_t *d_rows; /* device: only the first *d_rows rows of grad count; NULL: all do */
+  const int32_t *d_row_ids; /* device, a row of the table for each row of grad; NULL: the same */
+  int64_t num_rows;      /* of the table, with d_row_ids */
+} smfg_param_t;
+typedef struct {
+  double lr, beta1, beta2, eps; /* beta1, beta2 in [0, 1), eps >= 0 */
+  double scale, max_norm;       /* max_norm > 0 */
+  int64_t step;                 /* t = step + *d_step, 1 in the first step */
+  const int64_t *d_step;        /* device, or NULL (0): for graphs, in which step is what it was when they were captured */
+  const float *d_lr;            /* device, multiplies lr, or NULL (1): the same */
+  const float *d_norm;          /* device, or NULL */
+} smfg_adamw_t;
+int64_t smfg_adamw_scratch_bytes(const smfg_param_t *params, int32_t num_params);
+int smfg_adamw(const smfg_param_t *params /* host */, int32_t num_params, const smfg_adamw_t *hyper /* host */, void *d_scratch,
+               int64_t scratch_bytes, void *hip_stream);
+/* What states of 8 bits stand for, as numel values of out_dtype: m's (second 0) or v's (second 1). */
+int smfg_adamw_values(const void *d_codes, const float *d_scales, int64_t numel, int64_t row_elems, int32_t second, void *d_out,
+                      int32_t out_dtype, void *hip_stream);
 
 /* Copies counts[0 .. 2L+2) to the host after synchronising the stream; returns SMFG_OK or, if the
  * status word is non-zero, its (positive) SMFG_ST_* value. */

@@ -37,7 +37,8 @@ EXPORTS = [
     "smfg_gather_rows", "smfg_gather_many", "smfg_mean_aggregate", "smfg_sage_layer", "smfg_sage_pack_weights",
     "smfg_sage_packed_bytes", "smfg_embedding", "smfg_embedding_grad_scratch_bytes", "smfg_embedding_grad", "smfg_embedding_grad_rows",
     "smfg_layer_norm", "smfg_layer_norm_grad_scratch_bytes", "smfg_layer_norm_grad", "smfg_clip_grad_norm_scratch_bytes",
-    "smfg_clip_grad_norm", "smfg_read_counts", "smfg_strerror", "smfg_profile_begin", "smfg_profile_end",
+    "smfg_clip_grad_norm", "smfg_rms_norm", "smfg_rms_norm_grad_scratch_bytes", "smfg_rms_norm_grad", "smfg_cross_entropy_scratch_bytes",
+    "smfg_cross_entropy", "smfg_adamw_scratch_bytes", "smfg_adamw", "smfg_adamw_values", "smfg_read_counts", "smfg_strerror", "smfg_profile_begin", "smfg_profile_end",
 ]
 STAGES = ["clear", "seeds", "sample_insert", "flag_rows", "scan_tiles", "assemble", "gather",
           "mean_aggregate", "sage_layer", "partition", "dedup_buckets"]
@@ -74,6 +75,43 @@ class _Grad(ctypes.Structure):
     ]
 
 
+class _Param(ctypes.Structure):
+    _fields_ = [
+        ("param", ctypes.c_void_p),
+        ("grad", ctypes.c_void_p),
+        ("m", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("m_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("copy", ctypes.c_void_p),
+        ("numel", ctypes.c_int64),
+        ("param_dtype", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+        ("copy_dtype", ctypes.c_int32),
+        ("state_bits", ctypes.c_int32),
+        ("weight_decay", ctypes.c_float),
+        ("row_elems", ctypes.c_int64),
+        ("d_rows", ctypes.c_void_p),
+        ("d_row_ids", ctypes.c_void_p),
+        ("num_rows", ctypes.c_int64),
+    ]
+
+
+class _AdamW(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("scale", ctypes.c_double),
+        ("max_norm", ctypes.c_double),
+        ("step", ctypes.c_int64),
+        ("d_step", ctypes.c_void_p),
+        ("d_lr", ctypes.c_void_p),
+        ("d_norm", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -107,7 +145,8 @@ def lib() -> ctypes.CDLL:
         L.smfg_sage_packed_bytes.argtypes = [i32, i32]
         L.smfg_sage_pack_weights.argtypes = [vp, i32, i32, vp, vp]
         f32, sizes = ctypes.c_float, ("smfg_workspace_bytes", "smfg_sage_packed_bytes", "smfg_embedding_grad_scratch_bytes",
-                                      "smfg_layer_norm_grad_scratch_bytes", "smfg_clip_grad_norm_scratch_bytes")
+                                      "smfg_layer_norm_grad_scratch_bytes", "smfg_clip_grad_norm_scratch_bytes", "smfg_rms_norm_grad_scratch_bytes",
+                                      "smfg_cross_entropy_scratch_bytes", "smfg_adamw_scratch_bytes")
         L.smfg_embedding.argtypes = [vp, i64, i64, i32, vp, i32, vp, i64, i32, f32, vp, i64, i32, vp]
         L.smfg_embedding_grad_scratch_bytes.argtypes = [i64, i64, i32]
         L.smfg_embedding_grad.argtypes = [vp, i32, vp, i64, vp, i64, i32, i32, f32, vp, i64, i64, i32, i32, vp, i64, vp]
@@ -117,6 +156,14 @@ def lib() -> ctypes.CDLL:
         L.smfg_layer_norm_grad.argtypes = [vp, i64, vp, i64, i32, vp, i64, i32, vp, i32, vp, vp, vp, i64, vp, vp, vp, i64, vp]
         L.smfg_clip_grad_norm_scratch_bytes.argtypes = [ctypes.POINTER(_Grad), i32]
         L.smfg_clip_grad_norm.argtypes = [ctypes.POINTER(_Grad), i32, f32, f32, vp, vp, i64, vp]
+        L.smfg_rms_norm.argtypes = [vp, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp, i32, f32, vp, i64, i32, vp, i64, i32, vp, vp]
+        L.smfg_rms_norm_grad_scratch_bytes.argtypes = [i64, i32]
+        L.smfg_rms_norm_grad.argtypes = [vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp, i32, vp, vp, i64, vp, vp, i64, vp]
+        L.smfg_cross_entropy_scratch_bytes.argtypes = [i64, i32]
+        L.smfg_cross_entropy.argtypes = [vp, i64, i32, vp, i32, vp, i64, i32, i32, f32, vp, vp, vp, i64, vp, i64, vp]
+        L.smfg_adamw_scratch_bytes.argtypes = [ctypes.POINTER(_Param), i32]
+        L.smfg_adamw.argtypes = [ctypes.POINTER(_Param), i32, ctypes.POINTER(_AdamW), vp, i64, vp]
+        L.smfg_adamw_values.argtypes = [vp, vp, i64, i64, i32, vp, i32, vp]
         L.smfg_read_counts.argtypes = [ctypes.POINTER(_Output), i32, ctypes.POINTER(i64), vp]
         L.smfg_profile_begin.argtypes = [i32, i32]
         L.smfg_profile_end.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i64)]
@@ -593,6 +640,184 @@ def clip_grad_norm(grads: GradList, max_norm: float, norm: torch.Tensor, scale: 
     rc = lib().smfg_clip_grad_norm(grads.c, grads.n, scale, max_norm, _vector(norm, 1, torch.float32, "norm"), grads.scratch.on(stream),
                                    grads.scratch.nbytes, _raw_stream(stream))
     _check(rc, "smfg_clip_grad_norm")
+
+
+BYTE_DTYPES = {torch.int8: 3, torch.float8_e4m3fn: 4}
+
+
+def rms_norm(x: torch.Tensor, num_rows: torch.Tensor, max_rows: int, weight: Optional[torch.Tensor], eps: float, y: torch.Tensor,
+             residual: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, group: int = 0,
+             rstd: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """total[i] = x[i] + residual[i] (x[i] without a residual), y[i] = total[i] / sqrt(mean(total[i]^2) + eps) * weight for i < num_rows (device
+    int64).  y of x's type, or int8 or float8_e4m3fn: then y stands for y * scales, scales (float32 [max_rows x groups]) one for each `group` columns
+    (32, 64, 128; 0: a row).  weight float32 or of x's type, or None.  total may be None, x or residual; y may be x or residual.  rstd (float32
+    [max_rows]) is what rms_norm_grad needs."""
+    assert x.dim() == 2 and y.dim() == 2 and x.shape[1] == y.shape[1]
+    dim = int(x.shape[1])
+    a, as_, at = _matrix(x, max_rows, "x")
+    r = t = s = None
+    rs = ts = ss = 0
+    if residual is not None:
+        assert residual.dim() == 2 and residual.shape[1] == dim and residual.dtype == x.dtype
+        r, rs, _ = _matrix(residual, max_rows, "residual")
+    if total is not None:
+        assert total.dim() == 2 and total.shape[1] == dim and total.dtype == x.dtype
+        t, ts, _ = _matrix(total, max_rows, "total")
+    if y.dtype in BYTE_DTYPES:
+        assert y.is_cuda and y.shape[0] >= max_rows and (y.stride(1) == 1 or dim == 1)
+        o, os_, ot = y.data_ptr(), y.stride(0) if y.shape[0] > 1 else max(y.stride(0), dim), BYTE_DTYPES[y.dtype]
+        assert scales is not None and scales.dim() == 2 and scales.dtype == torch.float32 and scales.shape[1] == (-(-dim // group) if group > 0 else 1)
+        s, ss, _ = _matrix(scales, max_rows, "scales")
+    else:
+        assert y.dtype == x.dtype and scales is None
+        o, os_, ot = _matrix(y, max_rows, "y")
+    pd = weight.dtype if weight is not None else torch.float32
+    assert pd in DTYPES
+    rc = lib().smfg_rms_norm(a, as_, at, r, rs, t, ts, _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, dim, _vector(weight, dim, pd, "weight"),
+                             DTYPES[pd], eps, o, os_, ot, s, ss, group, _vector(rstd, max_rows, torch.float32, "rstd"), _raw_stream(stream))
+    _check(rc, "smfg_rms_norm")
+
+
+def rms_norm_grad_workspace(max_rows: int, dim: int, device=None) -> Scratch:
+    """Scratch of rms_norm_grad for up to max_rows rows."""
+    return Scratch(int(lib().smfg_rms_norm_grad_scratch_bytes(max_rows, dim)), "smfg_rms_norm_grad_scratch_bytes", device)
+
+
+def rms_norm_grad(grad_y: torch.Tensor, total: torch.Tensor, num_rows: torch.Tensor, max_rows: int, weight: Optional[torch.Tensor], rstd: torch.Tensor,
+                  grad_x: Optional[torch.Tensor], grad_weight: Optional[torch.Tensor], ws: Optional[Scratch], grad_total: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Gradients of rms_norm's input (and of its residual, which is the same) and weight; None where one is not wanted (without the latter, ws may be
+    None).  total is the sum that was normed, or x; grad_total the gradient that reaches the sum from elsewhere, which is added.  grad_x is of x's type
+    and may be grad_y, total or grad_total; grad_weight is of weight's type."""
+    assert total.dim() == 2 and grad_y.dim() == 2 and grad_y.shape[1] == total.shape[1] and grad_y.dtype == total.dtype
+    dim = int(total.shape[1])
+    d, ds, _ = _matrix(grad_y, max_rows, "grad_y")
+    a, as_, at = _matrix(total, max_rows, "total")
+    gx = gt = None
+    gs = gts = 0
+    if grad_x is not None:
+        assert grad_x.dim() == 2 and grad_x.shape[1] == dim and grad_x.dtype == total.dtype
+        gx, gs, _ = _matrix(grad_x, max_rows, "grad_x")
+    if grad_total is not None:
+        assert grad_total.dim() == 2 and grad_total.shape[1] == dim and grad_total.dtype == total.dtype
+        gt, gts, _ = _matrix(grad_total, max_rows, "grad_total")
+    pd = next((t.dtype for t in (weight, grad_weight) if t is not None), torch.float32)
+    assert pd in DTYPES
+    rc = lib().smfg_rms_norm_grad(d, ds, a, as_, at, gt, gts, _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, dim,
+                                  _vector(weight, dim, pd, "weight"), DTYPES[pd], _vector(rstd, max_rows, torch.float32, "rstd"), gx, gs,
+                                  _vector(grad_weight, dim, pd, "grad_weight"), ws.on(stream) if ws is not None else None,
+                                  ws.nbytes if ws is not None else 0, _raw_stream(stream))
+    _check(rc, "smfg_rms_norm_grad")
+
+
+REDUCTIONS = {"mean": 0, "sum": 1}
+
+
+def cross_entropy_workspace(max_rows: int, classes: int, device=None) -> Scratch:
+    """Scratch of cross_entropy for up to max_rows rows."""
+    return Scratch(int(lib().smfg_cross_entropy_scratch_bytes(max_rows, classes)), "smfg_cross_entropy_scratch_bytes", device)
+
+
+def cross_entropy(logits: torch.Tensor, labels: torch.Tensor, num_rows: torch.Tensor, max_rows: int, loss: torch.Tensor, ws: Scratch,
+                  grad_logits: Optional[torch.Tensor] = None, row_loss: Optional[torch.Tensor] = None, scale: float = 1.0, reduction: str = "mean",
+                  stream: Optional[torch.cuda.Stream] = None) -> None:
+    """loss (float32, one element) = mean or sum over rows i < num_rows (device int64) of log(sum(exp(logits[i]))) - logits[i, labels[i]]; grad_logits
+    (of logits' type; may be logits) = its gradient times scale; row_loss (float32 [max_rows]) the rows' own.  A row whose label (int32 or int64) is
+    no class does not count: loss 0, gradient zeros."""
+    assert logits.dim() == 2 and labels.dtype in (torch.int32, torch.int64)
+    x, xs, xt = _matrix(logits, max_rows, "logits")
+    g, gs = None, 0
+    if grad_logits is not None:
+        assert grad_logits.dim() == 2 and grad_logits.shape[1] == logits.shape[1] and grad_logits.dtype == logits.dtype
+        g, gs, _ = _matrix(grad_logits, max_rows, "grad_logits")
+    rc = lib().smfg_cross_entropy(x, xs, xt, _vector(labels, max_rows, labels.dtype, "labels"), labels.element_size(),
+                                  _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, logits.shape[1], REDUCTIONS[reduction], scale,
+                                  _vector(loss, 1, torch.float32, "loss"), _vector(row_loss, max_rows, torch.float32, "row_loss"), g, gs,
+                                  ws.on(stream), ws.nbytes, _raw_stream(stream))
+    _check(rc, "smfg_cross_entropy")
+
+
+STATE_BLOCK = 128
+
+
+class AdamWList:
+    """Tensors to be stepped together, their states and scratch; keeps the tensors alive."""
+
+    def __init__(self, c, n: int, scratch: Scratch, tensors):
+        self.c, self.n, self.scratch, self.tensors = c, n, scratch, tensors
+        self.hyper = _AdamW()
+
+
+def adamw_list(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
+               m_scales: Optional[Sequence[Optional[torch.Tensor]]] = None, v_scales: Optional[Sequence[Optional[torch.Tensor]]] = None,
+               copies: Optional[Sequence[Optional[torch.Tensor]]] = None, rows: Optional[Sequence[Optional[torch.Tensor]]] = None,
+               row_ids: Optional[Sequence[Optional[torch.Tensor]]] = None, weight_decay=0.0, device=None) -> AdamWList:
+    """The buffers of adamw: contiguous parameters, their gradients and states.  m[i], v[i] float32, or int8 and uint8 with m_scales[i], v_scales[i]
+    (float32, one for each STATE_BLOCK elements: of the whole tensor if they have one dimension, of each row if they have two).  copies[i] (float16 or bfloat16):
+    where float32 parameters are written to as well, rounded.  row_ids[i] (int32): the rows of params[i] that grads[i] has rows of, rows[i] (device int64) how many
+    of them count (None: all), as embedding_grad_rows tells both.  weight_decay: one for all, or one each.  What the buffers hold is read by each step anew."""
+    n = len(params)
+    lists = [params, grads, m, v] + [t if t is not None else [None] * n for t in (m_scales, v_scales, copies, rows, row_ids)]
+    decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+    assert all(len(t) == n for t in lists) and len(decay) == n
+    c = (_Param * max(1, n))()
+    for e, p, g, a, b, sa, sb, copy, count, ids, wd in zip(c, *lists, decay):
+        assert p.dtype in DTYPES and g.dtype in DTYPES and all(t.is_contiguous() and t.is_cuda for t in (p, g, a, b))
+        assert a.numel() == p.numel() == b.numel()
+        e.param, e.grad, e.m, e.v = p.data_ptr(), g.data_ptr(), a.data_ptr(), b.data_ptr()
+        e.numel, e.param_dtype, e.grad_dtype, e.weight_decay = g.numel(), DTYPES[p.dtype], DTYPES[g.dtype], wd
+        by_row = ids is not None or count is not None
+        if a.dtype == torch.float32:
+            assert b.dtype == torch.float32 and sa is None and sb is None
+            e.state_bits = 32
+        else:
+            assert a.dtype == torch.int8 and b.dtype == torch.uint8 and sa is not None and sb is not None and sa.shape == sb.shape
+            by_row = by_row or sa.dim() == 2
+            want = (p.shape[0] if by_row else 1) * -(-(p.numel() // max(1, p.shape[0]) if by_row else p.numel()) // STATE_BLOCK)
+            assert all(t.dtype == torch.float32 and t.is_contiguous() and t.is_cuda and t.numel() == want for t in (sa, sb))
+            e.state_bits, e.m_scale, e.v_scale = 8, sa.data_ptr(), sb.data_ptr()
+        if copy is not None:
+            assert copy.dtype in DTYPES and copy.is_contiguous() and copy.is_cuda and copy.numel() == p.numel()
+            e.copy, e.copy_dtype = copy.data_ptr(), DTYPES[copy.dtype]
+        if by_row:
+            e.row_elems = max(1, p.numel() // max(1, p.shape[0]))
+        if count is not None:
+            e.d_rows = _vector(count, 1, torch.int64, "rows")
+        if ids is not None:
+            assert g.numel() == g.shape[0] * e.row_elems
+            e.d_row_ids, e.num_rows = _vector(ids, g.shape[0], torch.int32, "row_ids"), p.shape[0]
+        else:
+            assert g.numel() == p.numel()
+    nbytes = int(lib().smfg_adamw_scratch_bytes(c, n))
+    if device is None and n > 0:
+        device = params[0].device
+    return AdamWList(c, n, Scratch(nbytes, "smfg_adamw_scratch_bytes", device), [list(t) for t in lists])
+
+
+def adamw(params: AdamWList, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, scale: float = 1.0, max_norm: float = float("inf"),
+          norm: Optional[torch.Tensor] = None, device_step: Optional[torch.Tensor] = None, device_lr: Optional[torch.Tensor] = None,
+          stream: Optional[torch.cuda.Stream] = None) -> None:
+    """One step of AdamW, step + device_step (device int64) the first being 1, with lr * device_lr (device float32).  Gradients are multiplied by
+    scale, and by min(1, max_norm / (norm + 1e-6)) where norm (device float32) is given; if that is not finite the step is not taken."""
+    h = params.hyper
+    h.lr, h.beta1, h.beta2, h.eps, h.scale, h.max_norm, h.step = lr, betas[0], betas[1], eps, scale, max_norm, step
+    h.d_step = _vector(device_step, 1, torch.int64, "device_step")
+    h.d_lr = _vector(device_lr, 1, torch.float32, "device_lr")
+    h.d_norm = _vector(norm, 1, torch.float32, "norm")
+    rc = lib().smfg_adamw(params.c, params.n, h, params.scratch.on(stream), params.scratch.nbytes, _raw_stream(stream))
+    _check(rc, "smfg_adamw")
+
+
+def adamw_values(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """out (of any type) = what a state of 8 bits stands for: the first moment's (int8) or the second's (uint8); scales as in adamw_list."""
+    assert codes.dtype in (torch.int8, torch.uint8) and out.dtype in DTYPES and codes.numel() == out.numel()
+    assert all(t.is_contiguous() and t.is_cuda for t in (codes, scales, out)) and scales.dtype == torch.float32
+    rows = codes.shape[0] if scales.dim() == 2 else 1
+    cols = codes.numel() // max(1, rows)
+    assert scales.numel() == rows * -(-cols // STATE_BLOCK)
+    rc = lib().smfg_adamw_values(codes.data_ptr(), scales.data_ptr(), codes.numel(), cols if scales.dim() == 2 else 0, int(codes.dtype == torch.uint8),
+                                 out.data_ptr(), DTYPES[out.dtype], _raw_stream(stream))
+    _check(rc, "smfg_adamw_values")
 
 
 def read_counts(out: Output, stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> List[int]:

@@ -7,7 +7,7 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SRC = os.path.join(_HERE, "csrc", "smfg.hip")
-SOURCES = [SRC, os.path.join(_HERE, "csrc", "train.hip")]
+SOURCES = [SRC] + [os.path.join(_HERE, "csrc", f) for f in ("train.hip", "rms_norm.hip", "loss.hip", "adamw.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(_HERE, "libsmfg.so")
 

@@ -378,10 +378,8 @@ __global__ void __launch_bounds__(kThreads) k_norm_grad_columns(NormGradArgs A) 
 constexpr int kNormJoinCols = 16;
 constexpr int kNormJoinThreads = 1024;
 constexpr int kNormJoinRows = kNormJoinThreads / kNormJoinCols;
-template <typename P>
-__global__ void __launch_bounds__(kNormJoinThreads) k_norm_grad_join(const float* __restrict__ part, int32_t slices, int32_t dim, P* dw, P* db) {
-  __shared__ float lds[kNormJoinThreads];
-  const int64_t width = 2 * static_cast<int64_t>(dim), i = static_cast<int64_t>(blockIdx.x) * kNormJoinCols + threadIdx.x % kNormJoinCols;
+// The sum of column i over the slices' sums, in the first kNormJoinCols threads of the block.
+__device__ __forceinline__ float join_slices(const float* __restrict__ part, int32_t slices, int64_t width, int64_t i, float* lds) {
   const float* p = part + (i < width ? i : width - 1);
   float s = 0.f;
 #pragma unroll 8
@@ -396,10 +394,19 @@ __global__ void __launch_bounds__(kNormJoinThreads) k_norm_grad_join(const float
   __syncthreads();
   if (threadIdx.x < 128) lds[threadIdx.x] = s;
   __syncthreads();
-  if (threadIdx.x >= kNormJoinCols || i >= width) return;
   s = 0.f;
+  if (threadIdx.x < kNormJoinCols) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q) s += lds[q * kNormJoinCols + threadIdx.x];
+    for (int q = 0; q < 8; ++q) s += lds[q * kNormJoinCols + threadIdx.x];
+  }
+  return s;
+}
+template <typename P>
+__global__ void __launch_bounds__(kNormJoinThreads) k_norm_grad_join(const float* __restrict__ part, int32_t slices, int32_t dim, P* dw, P* db) {
+  __shared__ float lds[kNormJoinThreads];
+  const int64_t width = 2 * static_cast<int64_t>(dim), i = static_cast<int64_t>(blockIdx.x) * kNormJoinCols + threadIdx.x % kNormJoinCols;
+  const float s = join_slices(part, slices, width, i, lds);
+  if (threadIdx.x >= kNormJoinCols || i >= width) return;
   P* out = i < dim ? dw : db;
   if (out) out[i < dim ? i : i - dim] = from_float<P>(s);
 }

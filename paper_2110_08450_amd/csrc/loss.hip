@@ -1,0 +1,98 @@
+// libsmfg: softmax cross entropy and its gradient (include/smfg.h), host side.  Kernels: kernels_loss.h.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "smfg.h"
+
+#include "kernels_loss.h"
+#include "train_common.h"
+
+namespace {
+
+using namespace smfg_dev;
+
+constexpr unsigned kLossBlocks = 2048, kLongLossBlocks = 512;
+
+// The blocks' sums, then the counts of labels.
+struct LossScratch {
+  int64_t counts, bytes;
+};
+LossScratch loss_scratch(int64_t max_rows) {
+  LossScratch S;
+  S.counts = up256(kLossBlocks * static_cast<int64_t>(sizeof(LossPart)));
+  S.bytes = S.counts + up256(8 * ceil_div(max_rows, kCountRows));
+  return S;
+}
+
+template <typename T>
+struct LaunchLoss {
+  LossArgs& A;
+  Launches& go;
+  template <int V, int NV, int LANES>
+  void operator()() const {
+    constexpr int threads = loss_threads(LANES);
+    A.parts = static_cast<int32_t>(blocks_for(A.max_rows, threads / LANES, LANES == 1024 ? kLongLossBlocks : kLossBlocks));
+    go(k_cross_entropy<T, V, NV, LANES>, static_cast<unsigned>(A.parts), threads, A);
+  }
+};
+
+// As with_row_shape; beyond 1536 vectors a row is that of 1024 lanes.
+template <typename T, typename F>
+bool with_loss_shape(int32_t classes, F f) {
+  constexpr int V = kVec<T>;
+  if (with_row_shape<T, 1536>(classes, f)) return true;
+  const int64_t vectors = ceil_div(classes, V);
+  if (vectors <= 2048) f.template operator()<V, 2, 1024>();
+  else if (vectors <= 3072) f.template operator()<V, 3, 1024>();
+  else if (vectors <= 4096) f.template operator()<V, 4, 1024>();
+  else if (vectors <= 5120) f.template operator()<V, 5, 1024>();
+  else if (vectors <= 6144) f.template operator()<V, 6, 1024>();
+  else if (vectors <= 7168) f.template operator()<V, 7, 1024>();
+  else return false;
+  return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t smfg_cross_entropy_scratch_bytes(int64_t max_rows, int32_t classes) {
+  if (bad_dim(classes) || max_rows < 0 || max_rows >= kMaxRows) return -1;
+  return loss_scratch(max_rows).bytes;
+}
+
+int smfg_cross_entropy(const void* d_logits, int64_t logits_stride, int32_t dtype, const void* d_labels, int32_t label_bytes, const int64_t* d_num_rows,
+                       int64_t max_rows, int32_t classes, int32_t reduction, float scale, float* d_loss, float* d_row_loss, void* d_dlogits,
+                       int64_t dlogits_stride, void* d_scratch, int64_t scratch_bytes, void* hip_stream) {
+  if (!d_num_rows || !d_loss || !d_scratch || (max_rows > 0 && (!d_logits || !d_labels))) return SMFG_ERR_NULL_PTR;
+  if (bad_dim(classes) || max_rows < 0 || max_rows >= kMaxRows || bad_matrix(d_logits, dtype, logits_stride, classes) ||
+      (label_bytes != 4 && label_bytes != 8) || misaligned(d_labels, static_cast<uintptr_t>(label_bytes)) ||
+      (reduction != SMFG_LOSS_MEAN && reduction != SMFG_LOSS_SUM) || !std::isfinite(scale) || misaligned(d_num_rows, 8) || misaligned(d_loss, 4) ||
+      misaligned(d_row_loss, 4) || misaligned(d_scratch, 256) ||
+      (d_dlogits && (bad_matrix(d_dlogits, dtype, dlogits_stride, classes) || (d_dlogits == d_logits && dlogits_stride != logits_stride))))
+    return SMFG_ERR_INVALID_ARG;
+  const LossScratch S = loss_scratch(max_rows);
+  if (scratch_bytes < S.bytes) return SMFG_ERR_CAPACITY;
+  Launches go(hip_stream);
+  uint8_t* scratch = static_cast<uint8_t*>(d_scratch);
+  LossArgs A = {d_logits, logits_stride, d_labels, label_bytes, classes, d_num_rows, max_rows, reduction == SMFG_LOSS_MEAN, scale, d_dlogits, dlogits_stride,
+                d_row_loss, d_loss, reinterpret_cast<LossPart*>(scratch), 0, reinterpret_cast<int64_t*>(scratch + S.counts), 0};
+  if (max_rows > 0) {
+    if (A.mean && d_dlogits && max_rows > kCountRows) {
+      A.num_counts = static_cast<int32_t>(ceil_div(max_rows, kCountRows));
+      go(k_loss_count, static_cast<unsigned>(A.num_counts), 1024, A);
+    }
+    with_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      if (with_loss_shape<T>(classes, LaunchLoss<T>{A, go})) return;
+      A.parts = static_cast<int32_t>(blocks_for(max_rows, 1, kLongLossBlocks));
+      go(k_cross_entropy_long<T, kVec<T>>, static_cast<unsigned>(A.parts), kLongLossThreads, A);
+    });
+  }
+  go(k_loss_join, 1, kThreads, A);
+  return go.result();
+}
+
+}  // extern "C"
