@@ -198,7 +198,13 @@ __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs 
       Elems<T, V> o;
 #pragma unroll
       for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(v[k][j]);
-      *reinterpret_cast<Elems<T, V>*>(dx + col.start) = o;
+      if (!ragged || col.dup == 0) {
+        *reinterpret_cast<Elems<T, V>*>(dx + col.start) = o;
+      } else {  // columns that two vectors share have other roundings in each, as the lanes' maxima differ: the first writes them
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (j >= col.dup) dx[col.start + j] = o.v[j];
+      }
     }
   }
   leave_part<kBlock>(A, sum, rows);
