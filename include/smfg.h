@@ -478,9 +478,7 @@ typedef struct {
   const float *d_lr;            /* device, multiplies lr, or NULL (1): the same */
   const float *d_norm;          /* device, or NULL */
 } smfg_adamw_t;
-int64_t smfg_adamw_scratch_bytes(const smfg_param_t *params, int32_t num_params);
-int smfg_adamw(const smfg_param_t *params /* host */, int32_t num_params, const smfg_adamw_t *hyper /* host */, void *d_scratch,
-               int64_t scratch_bytes, void *hip_stream);
+int smfg_adamw(const smfg_param_t *params /* host */, int32_t num_params, const smfg_adamw_t *hyper /* host */, void *hip_stream);
 /* What states of 8 bits stand for, as numel values of out_dtype: m's (second 0) or v's (second 1). */
 int smfg_adamw_values(const void *d_codes, const float *d_scales, int64_t numel, int64_t row_elems, int32_t second, void *d_out,
                       int32_t out_dtype, void *hip_stream);

@@ -38,7 +38,7 @@ EXPORTS = [
     "smfg_sage_packed_bytes", "smfg_embedding", "smfg_embedding_grad_scratch_bytes", "smfg_embedding_grad", "smfg_embedding_grad_rows",
     "smfg_layer_norm", "smfg_layer_norm_grad_scratch_bytes", "smfg_layer_norm_grad", "smfg_clip_grad_norm_scratch_bytes",
     "smfg_clip_grad_norm", "smfg_rms_norm", "smfg_rms_norm_grad_scratch_bytes", "smfg_rms_norm_grad", "smfg_cross_entropy_scratch_bytes",
-    "smfg_cross_entropy", "smfg_adamw_scratch_bytes", "smfg_adamw", "smfg_adamw_values", "smfg_read_counts", "smfg_strerror", "smfg_profile_begin", "smfg_profile_end",
+    "smfg_cross_entropy", "smfg_adamw", "smfg_adamw_values", "smfg_read_counts", "smfg_strerror", "smfg_profile_begin", "smfg_profile_end",
 ]
 STAGES = ["clear", "seeds", "sample_insert", "flag_rows", "scan_tiles", "assemble", "gather",
           "mean_aggregate", "sage_layer", "partition", "dedup_buckets"]
@@ -146,7 +146,7 @@ def lib() -> ctypes.CDLL:
         L.smfg_sage_pack_weights.argtypes = [vp, i32, i32, vp, vp]
         f32, sizes = ctypes.c_float, ("smfg_workspace_bytes", "smfg_sage_packed_bytes", "smfg_embedding_grad_scratch_bytes",
                                       "smfg_layer_norm_grad_scratch_bytes", "smfg_clip_grad_norm_scratch_bytes", "smfg_rms_norm_grad_scratch_bytes",
-                                      "smfg_cross_entropy_scratch_bytes", "smfg_adamw_scratch_bytes")
+                                      "smfg_cross_entropy_scratch_bytes")
         L.smfg_embedding.argtypes = [vp, i64, i64, i32, vp, i32, vp, i64, i32, f32, vp, i64, i32, vp]
         L.smfg_embedding_grad_scratch_bytes.argtypes = [i64, i64, i32]
         L.smfg_embedding_grad.argtypes = [vp, i32, vp, i64, vp, i64, i32, i32, f32, vp, i64, i64, i32, i32, vp, i64, vp]
@@ -161,8 +161,7 @@ def lib() -> ctypes.CDLL:
         L.smfg_rms_norm_grad.argtypes = [vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp, i32, vp, vp, i64, vp, vp, i64, vp]
         L.smfg_cross_entropy_scratch_bytes.argtypes = [i64, i32]
         L.smfg_cross_entropy.argtypes = [vp, i64, i32, vp, i32, vp, i64, i32, i32, f32, vp, vp, vp, i64, vp, i64, vp]
-        L.smfg_adamw_scratch_bytes.argtypes = [ctypes.POINTER(_Param), i32]
-        L.smfg_adamw.argtypes = [ctypes.POINTER(_Param), i32, ctypes.POINTER(_AdamW), vp, i64, vp]
+        L.smfg_adamw.argtypes = [ctypes.POINTER(_Param), i32, ctypes.POINTER(_AdamW), vp]
         L.smfg_adamw_values.argtypes = [vp, vp, i64, i64, i32, vp, i32, vp]
         L.smfg_read_counts.argtypes = [ctypes.POINTER(_Output), i32, ctypes.POINTER(i64), vp]
         L.smfg_profile_begin.argtypes = [i32, i32]
@@ -741,17 +740,16 @@ STATE_BLOCK = 128
 
 
 class AdamWList:
-    """Tensors to be stepped together, their states and scratch; keeps the tensors alive."""
+    """Tensors to be stepped together with their states; keeps the tensors alive."""
 
-    def __init__(self, c, n: int, scratch: Scratch, tensors):
-        self.c, self.n, self.scratch, self.tensors = c, n, scratch, tensors
-        self.hyper = _AdamW()
+    def __init__(self, c, n: int, tensors):
+        self.c, self.n, self.tensors = c, n, tensors
 
 
 def adamw_list(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
                m_scales: Optional[Sequence[Optional[torch.Tensor]]] = None, v_scales: Optional[Sequence[Optional[torch.Tensor]]] = None,
                copies: Optional[Sequence[Optional[torch.Tensor]]] = None, rows: Optional[Sequence[Optional[torch.Tensor]]] = None,
-               row_ids: Optional[Sequence[Optional[torch.Tensor]]] = None, weight_decay=0.0, device=None) -> AdamWList:
+               row_ids: Optional[Sequence[Optional[torch.Tensor]]] = None, weight_decay=0.0) -> AdamWList:
     """The buffers of adamw: contiguous parameters, their gradients and states.  m[i], v[i] float32, or int8 and uint8 with m_scales[i], v_scales[i]
     (float32, one for each STATE_BLOCK elements: of the whole tensor if they have one dimension, of each row if they have two).  copies[i] (float16 or bfloat16):
     where float32 parameters are written to as well, rounded.  row_ids[i] (int32): the rows of params[i] that grads[i] has rows of, rows[i] (device int64) how many
@@ -790,10 +788,7 @@ def adamw_list(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
             e.d_row_ids, e.num_rows = _vector(ids, g.shape[0], torch.int32, "row_ids"), p.shape[0]
         else:
             assert g.numel() == p.numel()
-    nbytes = int(lib().smfg_adamw_scratch_bytes(c, n))
-    if device is None and n > 0:
-        device = params[0].device
-    return AdamWList(c, n, Scratch(nbytes, "smfg_adamw_scratch_bytes", device), [list(t) for t in lists])
+    return AdamWList(c, n, [list(t) for t in lists])
 
 
 def adamw(params: AdamWList, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, scale: float = 1.0, max_norm: float = float("inf"),
@@ -801,12 +796,9 @@ def adamw(params: AdamWList, step: int, lr: float, betas=(0.9, 0.999), eps: floa
           stream: Optional[torch.cuda.Stream] = None) -> None:
     """One step of AdamW, step + device_step (device int64) the first being 1, with lr * device_lr (device float32).  Gradients are multiplied by
     scale, and by min(1, max_norm / (norm + 1e-6)) where norm (device float32) is given; if that is not finite the step is not taken."""
-    h = params.hyper
-    h.lr, h.beta1, h.beta2, h.eps, h.scale, h.max_norm, h.step = lr, betas[0], betas[1], eps, scale, max_norm, step
-    h.d_step = _vector(device_step, 1, torch.int64, "device_step")
-    h.d_lr = _vector(device_lr, 1, torch.float32, "device_lr")
-    h.d_norm = _vector(norm, 1, torch.float32, "norm")
-    rc = lib().smfg_adamw(params.c, params.n, h, params.scratch.on(stream), params.scratch.nbytes, _raw_stream(stream))
+    h = _AdamW(lr, betas[0], betas[1], eps, scale, max_norm, step, _vector(device_step, 1, torch.int64, "device_step"),
+               _vector(device_lr, 1, torch.float32, "device_lr"), _vector(norm, 1, torch.float32, "norm"))
+    rc = lib().smfg_adamw(params.c, params.n, h, _raw_stream(stream))
     _check(rc, "smfg_adamw")
 
 

@@ -38,27 +38,32 @@ bool has_null(const smfg_param_t& p) {
   return p.numel > 0 && (!p.param || !p.grad || !p.m || !p.v || (p.state_bits == 8 && (!p.m_scale || !p.v_scale)));
 }
 
-int64_t units_of(const smfg_param_t& p) {
-  const int64_t cols = p.row_elems > 0 ? p.row_elems : p.numel;
-  return cols == 0 ? 0 : p.numel / cols * ceil_div(cols, kStateBlock);
-}
+inline int64_t cols_of(const smfg_param_t& p) { return p.row_elems > 0 ? p.row_elems : p.numel; }
 
-// Scratch: the table of more tensors than the arguments hold.  A block has so many units that there are 4096 blocks, but 16 (2 Ki elements) at least and 512 at most.
+// What a block of threads has as one: vectors of states of floats, blocks of states of 8 bits.
+inline int64_t items_of(const smfg_param_t& p) {
+  const int64_t cols = cols_of(p);
+  if (cols == 0) return 0;
+  return p.numel / cols * (p.state_bits == 8 ? ceil_div(cols, kStateBlock) : cols >= kAdamFloats ? ceil_div(cols, kAdamFloats) : cols);
+}
+// Blocks of threads, and how many times kStateBlock elements each has.  States of floats: a vector a thread (400 M of them 2040 us; two 2100, 16 2150, 64 2250),
+// as short-lived blocks keep the memory busiest.  Of 8 bits: what leaves 2048 blocks, but 16 at least and 64 at most (1204; 16 1700, 32 1229), as they have
+// more to work out before they begin.  More, up to 512, where there would be over 2^20 blocks.
 struct AdamShape {
-  int64_t blocks, bytes;
-  uint32_t units;
-  int32_t tensors;
+  int64_t blocks[2];  // for states of floats, of 8 bits
+  uint32_t units[2];
 };
+inline int64_t blocks_of(const smfg_param_t& p, const AdamShape& S) {
+  return ceil_div(items_of(p), p.state_bits == 8 ? S.units[1] : S.units[0] * (kStateBlock / kAdamFloats));
+}
 AdamShape adam_shape(const smfg_param_t* p, int32_t n) {
-  AdamShape S = {0, 0, 16, 0};
-  double all = 0;
-  for (int i = 0; i < n; ++i) all += static_cast<double>(units_of(p[i]));
-  while (S.units < 512 && all > 4096.0 * 2 * S.units) S.units *= 2;
-  for (int i = 0; i < n; ++i) {
-    S.tensors += p[i].numel > 0;
-    S.blocks += ceil_div(units_of(p[i]), S.units);
-  }
-  S.bytes = S.tensors > kAdamTensors ? up256(static_cast<int64_t>(sizeof(AdamTensor)) * S.tensors) : 0;
+  AdamShape S = {{0, 0}, {8, 16}};
+  double all[2] = {0, 0};
+  for (int i = 0; i < n; ++i) all[p[i].state_bits == 8] += static_cast<double>(p[i].numel) / kStateBlock;
+  while (S.units[1] < 64 && all[1] > 2048.0 * 2 * S.units[1]) S.units[1] *= 2;
+  for (int k = 0; k < 2; ++k)
+    while (S.units[k] < 512 && all[k] > 1048576.0 * S.units[k]) S.units[k] *= 2;
+  for (int i = 0; i < n; ++i) S.blocks[p[i].state_bits == 8] += blocks_of(p[i], S);
   return S;
 }
 
@@ -66,32 +71,20 @@ AdamShape adam_shape(const smfg_param_t* p, int32_t n) {
 
 extern "C" {
 
-int64_t smfg_adamw_scratch_bytes(const smfg_param_t* params, int32_t num_params) {
-  if (num_params < 0 || (num_params > 0 && !params) || bad_params(params, num_params)) return -1;
-  return adam_shape(params, num_params).bytes;
-}
-
-int smfg_adamw(const smfg_param_t* params, int32_t num_params, const smfg_adamw_t* hyper, void* d_scratch, int64_t scratch_bytes, void* hip_stream) {
+int smfg_adamw(const smfg_param_t* params, int32_t num_params, const smfg_adamw_t* hyper, void* hip_stream) {
   if ((num_params > 0 && !params) || !hyper) return SMFG_ERR_NULL_PTR;
   const smfg_adamw_t& h = *hyper;
   if (num_params < 0 || bad_params(params, num_params) || !std::isfinite(h.lr) || !(h.beta1 >= 0.0 && h.beta1 < 1.0) || !(h.beta2 >= 0.0 && h.beta2 < 1.0) ||
       !(h.eps >= 0.0) || !std::isfinite(h.eps) || !std::isfinite(h.scale) || !(h.max_norm > 0.0) || h.step < (h.d_step ? 0 : 1) || h.step >= (int64_t(1) << 48) ||
-      misaligned(h.d_step, 8) || misaligned(h.d_lr, 4) || misaligned(h.d_norm, 4) || misaligned(d_scratch, 256))
+      misaligned(h.d_step, 8) || misaligned(h.d_lr, 4) || misaligned(h.d_norm, 4))
     return SMFG_ERR_INVALID_ARG;
   for (int i = 0; i < num_params; ++i)
     if (has_null(params[i])) return SMFG_ERR_NULL_PTR;
   const AdamShape S = adam_shape(params, num_params);
-  if (S.blocks >= kMaxRows) return SMFG_ERR_INVALID_ARG;
-  if (S.bytes > 0 && !d_scratch) return SMFG_ERR_NULL_PTR;
-  if (scratch_bytes < S.bytes) return SMFG_ERR_CAPACITY;
+  if (S.blocks[0] >= kMaxRows || S.blocks[1] >= kMaxRows) return SMFG_ERR_INVALID_ARG;
   Launches go(hip_stream);
-  const bool table = S.tensors > kAdamTensors;
   AdamArgs A;
-  A.table = table ? static_cast<AdamTensor*>(d_scratch) : nullptr;
-  A.tensors = S.tensors;
-  A.first = A.here = 0;
   A.first_block = 0;
-  A.units = S.units;
   A.lr = static_cast<float>(h.lr);
   A.b1 = static_cast<float>(h.beta1);
   A.one_b1 = static_cast<float>(1.0 - h.beta1);
@@ -100,31 +93,36 @@ int smfg_adamw(const smfg_param_t* params, int32_t num_params, const smfg_adamw_
   A.eps = static_cast<float>(h.eps);
   A.log_b1 = std::log(h.beta1);
   A.log_b2 = std::log(h.beta2);
+  const double t = static_cast<double>(h.step < 1 ? 1 : h.step);
+  A.step_size = static_cast<float>(h.lr / -std::expm1(t * A.log_b1));
+  A.root = static_cast<float>(1.0 / std::sqrt(-std::expm1(t * A.log_b2)));
   A.scale = h.scale;
   A.max_norm = h.max_norm;
   A.step = h.step;
   A.d_step = h.d_step;
   A.d_lr = h.d_lr;
   A.norm = h.d_norm;
-  uint32_t blocks = 0;
-  for (int i = 0; i < num_params; ++i) {
-    const smfg_param_t& p = params[i];
-    if (p.numel == 0) continue;
-    if (A.here == kAdamTensors) {
-      go(k_adamw_table, 1, 64, A);
-      A.first += A.here;
-      A.here = 0;
+  for (int bytes = 0; bytes < 2; ++bytes) {
+    int64_t blocks = 0;
+    A.tensors = 0;
+    A.units = S.units[bytes];
+    const auto launch = [&] {
+      if (bytes) go.all(k_adamw<true>, blocks, kThreads, A);
+      else go.all(k_adamw<false>, blocks, kThreads, A);
+      A.tensors = 0;
+      blocks = 0;
+    };
+    for (int i = 0; i < num_params; ++i) {
+      const smfg_param_t& p = params[i];
+      if (p.numel == 0 || (p.state_bits == 8) != (bytes == 1)) continue;
+      if (A.tensors == kAdamTensors) launch();
+      const int64_t cols = cols_of(p);
+      A.t[A.tensors++] = {p.param, p.grad, p.m, p.v, p.m_scale, p.v_scale, p.copy, p.d_rows, p.d_row_ids, p.numel / cols, cols,
+                          static_cast<int32_t>(p.d_row_ids ? p.num_rows : 0), static_cast<uint32_t>(blocks),
+                          p.param_dtype | p.grad_dtype << 4 | (p.copy ? p.copy_dtype : 0) << 8, p.weight_decay};
+      blocks += blocks_of(p, S);
     }
-    const int64_t cols = p.row_elems > 0 ? p.row_elems : p.numel;
-    A.t[A.here++] = {p.param, p.grad, p.m, p.v, p.m_scale, p.v_scale, p.copy, p.d_rows, p.d_row_ids, p.numel / cols, cols,
-                     static_cast<int32_t>(p.d_row_ids ? p.num_rows : 0), blocks,
-                     p.param_dtype | p.grad_dtype << 4 | (p.copy ? p.copy_dtype : 0) << 8 | (p.state_bits == 8) << 12, p.weight_decay};
-    blocks += static_cast<uint32_t>(ceil_div(units_of(p), S.units));
-  }
-  if (table) go(k_adamw_table, 1, 64, A);
-  if (blocks > 0) {
-    if (table) go.all(k_adamw<true>, blocks, kThreads, A);
-    else go.all(k_adamw<false>, blocks, kThreads, A);
+    launch();
   }
   return go.result();
 }
@@ -138,7 +136,7 @@ int smfg_adamw_values(const void* d_codes, const float* d_scales, int64_t numel,
     return SMFG_ERR_INVALID_ARG;
   if (numel == 0) return SMFG_OK;
   Launches go(hip_stream);
-  const int64_t cols = row_elems > 0 ? row_elems : numel, blocks = numel / cols * ceil_div(cols, kValueColumns);
+  const int64_t cols = row_elems > 0 ? row_elems : numel, blocks = ceil_div(numel, kValueSpan);
   if (blocks >= (int64_t(1) << 32)) return SMFG_ERR_INVALID_ARG;
   const AdamValuesArgs A = {static_cast<const uint8_t*>(d_codes), d_scales, numel / cols, cols, second, d_out, 0};
   with_type(out_dtype, [&](auto t) { go.all(k_adamw_values<decltype(t)>, blocks, kThreads, A); });

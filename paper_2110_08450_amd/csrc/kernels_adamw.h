@@ -17,7 +17,8 @@ namespace smfg_dev {
 
 constexpr int kStateBlock = 128;
 
-// Tensors are rows of `cols` elements (most of them one row), rows are units of kStateBlock columns.  A lane has V consecutive columns of a unit.
+// Tensors are rows of `cols` elements (most of them one row), which blocks of threads have by items of V or kStateBlock columns.  Those with states of floats
+// and those with states of 8 bits have kernels of their own.
 struct AdamTensor {
   void* p;
   const void* g;
@@ -31,18 +32,17 @@ struct AdamTensor {
   int64_t rows, cols;  // of g
   int32_t table_rows;  // of p, with ids
   uint32_t first_block;
-  int32_t type;  // of p | of g << 4 | of copy << 8 | state of 8 bits << 12
+  int32_t type;  // of p | of g << 4 | of copy << 8
   float decay;
 };
 constexpr int kAdamTensors = 36;
 struct AdamArgs {
   AdamTensor t[kAdamTensors];
-  AdamTensor* table;
   int32_t tensors;
-  int32_t first, here;
-  uint32_t first_block;
-  uint32_t units;  // of a block
+  uint32_t first_block;  // of the launch
+  uint32_t units;  // a block of threads has this many times kStateBlock elements
   float lr, one_b1, b1, one_b2, b2, eps;
+  float step_size, root;  // without a step on the device: lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
   double log_b1, log_b2, scale, max_norm;
   int64_t step;
   const int64_t* d_step;
@@ -51,27 +51,11 @@ struct AdamArgs {
 };
 static_assert(sizeof(AdamTensor) == 104 && sizeof(AdamArgs) <= 4096, "kernel arguments are limited to 4 KB");
 
-static __global__ void __launch_bounds__(64) k_adamw_table(AdamArgs A) {
-  for (int i = threadIdx.x; i < A.here; i += 64) A.table[A.first + i] = A.t[i];
-}
-
 // The last tensor that begins at the block or before it.
-template <bool TABLE>
 __device__ __forceinline__ AdamTensor adam_tensor(const AdamArgs& A, uint32_t block) {
+  static_assert(kAdamTensors <= 64, "one ballot");
   const int lane = threadIdx.x & 63;
-  if constexpr (!TABLE) {
-    static_assert(kAdamTensors <= 64, "one ballot");
-    return A.t[__popcll(__ballot(lane < A.tensors && block >= A.t[lane < A.tensors ? lane : 0].first_block)) - 1];
-  } else {
-    int lo = 0, hi = A.tensors;  // it is in [lo, hi)
-    while (hi - lo > 1) {
-      const int step = (hi - lo + 63) / 64, at = lo + lane * step;
-      const int begun = __popcll(__ballot(at < hi && block >= A.table[at < hi ? at : lo].first_block));
-      lo += (begun - 1) * step;
-      hi = lo + step < hi ? lo + step : hi;
-    }
-    return A.table[lo];
-  }
+  return A.t[__popcll(__ballot(lane < A.tensors && block >= A.t[lane < A.tensors ? lane : 0].first_block)) - 1];
 }
 
 // The numbers of a step that are the same for all elements.
@@ -82,12 +66,17 @@ struct AdamStep {
 };
 __device__ __forceinline__ AdamStep adam_step(const AdamArgs& A) {
   AdamStep S;
-  int64_t t = A.step + (A.d_step ? *A.d_step : 0);
-  if (t < 1) t = 1;
-  S.lr = A.d_lr ? A.lr * *A.d_lr : A.lr;
-  // 1 - b^t of a float b would have lost its digits
-  S.step = S.lr / -expm1f(static_cast<float>(static_cast<double>(t) * A.log_b1));
-  S.root = 1.f / sqrtf(-expm1f(static_cast<float>(static_cast<double>(t) * A.log_b2)));
+  const float rate = A.d_lr ? *A.d_lr : 1.f;
+  S.lr = A.lr * rate;
+  S.step = A.step_size * rate;
+  S.root = A.root;
+  if (A.d_step) {
+    const int64_t t = A.step + *A.d_step;
+    const double d = static_cast<double>(t < 1 ? 1 : t);
+    // 1 - b^t of a float b would have lost its digits
+    S.step = S.lr / -expm1f(static_cast<float>(d * A.log_b1));
+    S.root = 1.f / sqrtf(-expm1f(static_cast<float>(d * A.log_b2)));
+  }
   S.eps = A.eps;
   S.b1 = A.b1;
   S.one_b1 = A.one_b1;
@@ -103,22 +92,29 @@ __device__ __forceinline__ AdamStep adam_step(const AdamArgs& A) {
   S.f = static_cast<float>(f);
   return S;
 }
-__device__ __forceinline__ void adam_update(const AdamStep& S, float decay, float g, float& p, float& m, float& v) {
+// The update of an element, and the root of its second moment.  States of 8 bits keep the hardware busy with roots: theirs are its own, off by one in the last digit
+// (a v below 2^-126 counts as 0), and the quotient is a product with its reciprocal; floats, which the memory bounds, have the exact ones.
+template <bool FAST>
+__device__ __forceinline__ float adam_update(const AdamStep& S, float decay, float g, float& p, float& m, float& v) {
   g *= S.f;
   if (S.power != 0) g = __builtin_ldexpf(g, S.power);
   m = S.b1 * m + S.one_b1 * g;
   v = S.b2 * v + S.one_b2 * g * g;
-  p = p - decay * p - S.step * m / (sqrtf(v) * S.root + S.eps);
+  const float root = FAST ? __builtin_amdgcn_sqrtf(v) : sqrtf(v), den = root * S.root + S.eps;
+  p = p - decay * p - (FAST ? S.step * m * __builtin_amdgcn_rcpf(den) : S.step * m / den);
+  return root;
 }
 
+// m = A (k / 127) |k / 127|, sqrt(v) = B (k / 255)^2: squares of whole numbers are exact.
 __device__ __forceinline__ float state_m(float scale, uint8_t k) {
-  const float x = static_cast<float>(static_cast<int8_t>(k)) * (1.f / 127.f);
-  return scale * x * fabsf(x);
+  const float x = static_cast<float>(static_cast<int8_t>(k));
+  return x * fabsf(x) * scale;
 }
 __device__ __forceinline__ float state_root(float scale, uint8_t k) {
-  const float x = static_cast<float>(k) * (1.f / 255.f);
-  return scale * x * x;
+  const float x = static_cast<float>(k);
+  return x * x * scale;
 }
+constexpr float kStateM = 127.f * 127.f, kStateV = 255.f * 255.f;
 
 // What a block of elements has in common: the scale that is kept, and what its elements are multiplied by before their root.  Below 2^-100 all are zeros;
 // an infinity or a NaN makes the block NaN.
@@ -128,127 +124,196 @@ struct StateScale {
 __device__ __forceinline__ StateScale state_scale(uint32_t top, float most) {
   if (top < 0x0d800000u) return {0.f, 0.f};
   if (top >= 0x7f800000u) return {__uint_as_float(0x7fc00000u), 0.f};
-  return {__uint_as_float(top), most * most / __uint_as_float(top)};
+  return {__uint_as_float(top), most / __uint_as_float(top)};
 }
 
-template <typename TP, typename TG, int V, bool BYTES>
-__device__ __forceinline__ void adam_block(const AdamArgs& A, const AdamTensor& T, const AdamStep& S, uint32_t q) {
-  // lanes of a unit: as many as a short row has vectors, so that none idles in short rows
-  const int per_row = static_cast<int>(T.cols < kStateBlock ? (T.cols + V - 1) / V : kStateBlock / V);
-  int lanes = 1;
-  while (lanes < per_row) lanes <<= 1;
-  const int64_t row_units = (T.cols + kStateBlock - 1) / kStateBlock;
-  int64_t rows = T.rows;
-  if (T.num) {
-    const int64_t r = *T.num;
-    rows = r < 0 ? 0 : r < rows ? r : rows;
+// The row and the place in it of item i of a block whose first item has the place `at` in row `first_row`, of rows of `per_row` items.
+struct AdamPlace {
+  int64_t row, at;
+};
+__device__ __forceinline__ AdamPlace place_of(int64_t rows, int64_t per_row, int64_t first_row, int64_t at, int i) {
+  if (rows == 1) return {0, at + i};
+  // rows of a tensor with several have at most 2^23 items
+  const uint32_t b = static_cast<uint32_t>(at) + static_cast<uint32_t>(i), r = b / static_cast<uint32_t>(per_row);
+  return {first_row + r, b - r * static_cast<uint32_t>(per_row)};
+}
+__device__ __forceinline__ int64_t rows_of(const AdamTensor& T) {
+  if (!T.num) return T.rows;
+  const int64_t r = *T.num;
+  return r < 0 ? 0 : r < T.rows ? r : T.rows;
+}
+// Items of a block, of `all`.
+__device__ __forceinline__ int items_of(int64_t all, int64_t first, uint32_t most) {
+  const int64_t left = all - first;
+  return left <= 0 ? 0 : left < most ? static_cast<int>(left) : static_cast<int>(most);
+}
+// V values at any element's address.  Nothing of a step is read or written twice, so that it leaves the caches to others: 400 M floats with half gradients and
+// copies (28 bytes each) 2430 us without the hints, 2219 with those of the stores, 2152 with both.
+template <typename T, int V>
+using Raw = T __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+template <typename T, int V>
+__device__ __forceinline__ Elems<T, V> load_once(const T* src) {
+  if constexpr (V == 1) {
+    return *reinterpret_cast<const Elems<T, V>*>(src);
+  } else {
+    const Raw<T, V> x = __builtin_nontemporal_load(reinterpret_cast<const Raw<T, V>*>(src));
+    return __builtin_bit_cast(Elems<T , V>, x);
   }
-  const int64_t units = rows * row_units, first = static_cast<int64_t>(q) * A.units;
-  const int64_t end = first + A.units < units ? first + A.units : units;
-  const int at_once = kThreads / lanes, lane = static_cast<int>(threadIdx.x) & (lanes - 1);
-  const float decay = S.lr * T.decay;
-  for (int64_t base = first; base < end; base += at_once) {
-    const int64_t u = base + static_cast<int>(threadIdx.x) / lanes;
-    if (u >= end) continue;  // all lanes of the unit
-    const int64_t row = T.rows == 1 ? 0 : u / row_units;
-    int64_t to = row;
-    if (T.ids) {
-      to = T.ids[row];
-      if (to < 0 || to >= T.table_rows) continue;
-    }
-    const int64_t b = u - row * row_units;
-    const int64_t c = b * kStateBlock + lane * V;
-    // the last vector of a row ends with it; the columns that it shares with the one before are left to that
-    const int64_t start = c + V <= T.cols ? c : T.cols - V;
-    const int dup = c >= T.cols || lane >= per_row ? V : static_cast<int>(c - start);
-    const int64_t ig = row * T.cols + start, ip = to * T.cols + start, is = to * row_units + b;
-    const Elems<TG, V> eg = *reinterpret_cast<const Elems<TG, V>*>(static_cast<const TG*>(T.g) + ig);
-    const Elems<TP, V> ep = *reinterpret_cast<const Elems<TP, V>*>(static_cast<const TP*>(T.p) + ip);
-    float p[V], m[V], v[V];
-    if constexpr (BYTES) {
-      const Elems<uint8_t, V> em = *reinterpret_cast<const Elems<uint8_t, V>*>(static_cast<const uint8_t*>(T.m) + ip);
-      const Elems<uint8_t, V> ev = *reinterpret_cast<const Elems<uint8_t, V>*>(static_cast<const uint8_t*>(T.v) + ip);
-      const float sm = T.m_scale[is], sv = T.v_scale[is];
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        m[j] = state_m(sm, em.v[j]);
-        v[j] = state_root(sv, ev.v[j]);
-        v[j] *= v[j];
-      }
+}
+// V values, of which the first `dup` are left alone.
+template <typename T, int V>
+__device__ __forceinline__ void store_own(T* dst, const Elems<T, V>& e, int dup) {
+  if (dup == 0) {
+    if constexpr (V == 1) {
+      *reinterpret_cast<Elems<T, V>*>(dst) = e;
     } else {
-      const Elems<float, V> em = *reinterpret_cast<const Elems<float, V>*>(static_cast<const float*>(T.m) + ip);
-      const Elems<float, V> ev = *reinterpret_cast<const Elems<float, V>*>(static_cast<const float*>(T.v) + ip);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        m[j] = em.v[j];
-        v[j] = ev.v[j];
-      }
+      __builtin_nontemporal_store(__builtin_bit_cast(Raw<T , V>, e), reinterpret_cast<Raw<T, V>*>(dst));
     }
+  } else if (dup < V) {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (j >= dup) dst[j] = e.v[j];
+  }
+}
+template <typename TP, int V>
+__device__ __forceinline__ void store_params(const AdamTensor& T, int64_t at, const float (&p)[V], int dup) {
+  Elems<TP, V> e;
+#pragma unroll
+  for (int j = 0; j < V; ++j) e.v[j] = from_float<TP>(p[j]);
+  store_own(static_cast<TP*>(T.p) + at, e, dup);
+  if (!T.copy) return;
+  if ((T.type >> 8 & 15) == SMFG_DTYPE_F16) {
+    Elems<_Float16, V> o;
+#pragma unroll
+    for (int j = 0; j < V; ++j) o.v[j] = from_float<_Float16>(p[j]);
+    store_own(static_cast<_Float16*>(T.copy) + at, o, dup);
+  } else {
+    Elems<__bf16, V> o;
+#pragma unroll
+    for (int j = 0; j < V; ++j) o.v[j] = from_float<__bf16>(p[j]);
+    store_own(static_cast<__bf16*>(T.copy) + at, o, dup);
+  }
+}
+
+// States of floats: an item is a vector of V columns.
+constexpr int kAdamFloats = 4;  // columns of a vector
+template <typename TP, typename TG, int V>
+__device__ __forceinline__ void adam_floats(const AdamArgs& A, const AdamTensor& T, const AdamStep& S, uint32_t q) {
+  const int64_t per_row = (T.cols + V - 1) / V;
+  const uint32_t most = A.units * (kStateBlock / kAdamFloats);
+  const int64_t first = static_cast<int64_t>(q) * most;
+  const int count = items_of(rows_of(T) * per_row, first, most);
+  const int64_t first_row = T.rows == 1 ? 0 : first / per_row, first_at = first - first_row * per_row;
+  const float decay = S.lr * T.decay;
+  for (int i = static_cast<int>(threadIdx.x); i < count; i += kThreads) {
+    const AdamPlace a = place_of(T.rows, per_row, first_row, first_at, i);
+    // the last vector of a row ends with it; the columns that it shares with the one before are left to that
+    const int64_t c = a.at * V, start = c + V <= T.cols ? c : T.cols - V, ig = a.row * T.cols + start;
+    int64_t ip = ig;
+    if (T.ids) {
+      const int32_t id = T.ids[a.row];
+      if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(T.table_rows)) continue;
+      ip = id * T.cols + start;
+    }
+    const int dup = static_cast<int>(c - start);
+    const Elems<TG, V> eg = load_once<TG, V>(static_cast<const TG*>(T.g) + ig);
+    const Elems<TP, V> ep = load_once<TP, V>(static_cast<const TP*>(T.p) + ip);
+    Elems<float, V> em = load_once<float, V>(static_cast<const float*>(T.m) + ip), ev = load_once<float, V>(static_cast<const float*>(T.v) + ip);
+    float p[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       p[j] = as_float(ep.v[j]);
-      adam_update(S, decay, as_float(eg.v[j]), p[j], m[j], v[j]);
+      adam_update<false>(S, decay, as_float(eg.v[j]), p[j], em.v[j], ev.v[j]);
     }
-    const auto store = [&](auto* dst, const auto& e) {
-      if (dup == 0) {
-        *reinterpret_cast<__remove_cvref(decltype(e))*>(dst) = e;
-      } else {
+    store_params<TP, V>(T, ip, p, dup);
+    store_own(static_cast<float*>(T.m) + ip, em, dup);
+    store_own(static_cast<float*>(T.v) + ip, ev, dup);
+  }
+}
+
+// States of 8 bits: an item is a block of kStateBlock columns, whose largest values its lanes tell each other.
+// Rows are read through the caches: those of few bytes share their lines with their neighbours (200 K rows of 100 halfs 404 us instead of 431).
+template <typename T, int V, bool ROWS>
+__device__ __forceinline__ Elems<T, V> load_bytes(const T* src) {
+  if constexpr (ROWS) return *reinterpret_cast<const Elems<T, V>*>(src);
+  else return load_once<T, V>(src);
+}
+template <typename TP, typename TG, int V, bool ROWS>
+__device__ __forceinline__ void adam_bytes(const AdamArgs& A, const AdamTensor& T, const AdamStep& S, uint32_t q) {
+  // lanes of a block: as many as a short row has vectors, so that none idles in short rows
+  const int vectors = static_cast<int>(T.cols < kStateBlock ? (T.cols + V - 1) / V : kStateBlock / V);
+  int lanes = 1;
+  while (lanes < vectors) lanes <<= 1;
+  const int64_t per_row = (T.cols + kStateBlock - 1) / kStateBlock, first = static_cast<int64_t>(q) * A.units;
+  const int count = items_of(rows_of(T) * per_row, first, A.units);
+  const int64_t first_row = T.rows == 1 ? 0 : first / per_row, first_at = first - first_row * per_row;
+  const int lane = static_cast<int>(threadIdx.x) & (lanes - 1), mine = static_cast<int>(threadIdx.x) / lanes, at_once = kThreads / lanes;
+  const float decay = S.lr * T.decay;
+  constexpr int kTurns = 2;
+  for (int base = 0; base < count; base += kTurns * at_once) {
+    int64_t ig[kTurns], ip[kTurns], is[kTurns];
+    int dup[kTurns];
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (j >= dup) dst[j] = e.v[j];
+    for (int k = 0; k < kTurns; ++k) {
+      const int i = base + k * at_once + mine;
+      const AdamPlace a = place_of(T.rows, per_row, first_row, first_at, i < count ? i : 0);
+      const int64_t c = a.at * kStateBlock + lane * V, start = c + V <= T.cols ? c : T.cols - V;
+      dup[k] = i >= count || c >= T.cols || lane >= vectors ? V : static_cast<int>(c - start);
+      int64_t to = a.row;
+      if (T.ids) {
+        const int32_t id = T.ids[a.row];
+        const bool inside = static_cast<uint32_t>(id) < static_cast<uint32_t>(T.table_rows);
+        if (!inside) dup[k] = V;
+        to = inside ? id : 0;
       }
-    };
-    Elems<TP, V> op;
-#pragma unroll
-    for (int j = 0; j < V; ++j) op.v[j] = from_float<TP>(p[j]);
-    store(static_cast<TP*>(T.p) + ip, op);
-    if (T.copy) {
-      if ((T.type >> 8 & 15) == SMFG_DTYPE_F16) {
-        Elems<_Float16, V> o;
-#pragma unroll
-        for (int j = 0; j < V; ++j) o.v[j] = from_float<_Float16>(p[j]);
-        store(static_cast<_Float16*>(T.copy) + ip, o);
-      } else {
-        Elems<__bf16, V> o;
-#pragma unroll
-        for (int j = 0; j < V; ++j) o.v[j] = from_float<__bf16>(p[j]);
-        store(static_cast<__bf16*>(T.copy) + ip, o);
-      }
+      ig[k] = a.row * T.cols + start;
+      ip[k] = to * T.cols + start;
+      is[k] = to * per_row + a.at;
     }
-    if constexpr (BYTES) {
+    Elems<TG, V> eg[kTurns];
+    Elems<TP, V> ep[kTurns];
+    Elems<uint8_t, V> em[kTurns], ev[kTurns];
+    float sm[kTurns], sv[kTurns];
+#pragma unroll
+    for (int k = 0; k < kTurns; ++k) {
+      eg[k] = load_once<TG, V>(static_cast<const TG*>(T.g) + ig[k]);
+      ep[k] = load_bytes<TP, V, ROWS>(static_cast<const TP*>(T.p) + ip[k]);
+      em[k] = load_bytes<uint8_t, V, ROWS>(static_cast<const uint8_t*>(T.m) + ip[k]);
+      ev[k] = load_bytes<uint8_t, V, ROWS>(static_cast<const uint8_t*>(T.v) + ip[k]);
+      sm[k] = T.m_scale[is[k]];
+      sv[k] = T.v_scale[is[k]];
+    }
+#pragma unroll
+    for (int k = 0; k < kTurns; ++k) {
+      float p[V], m[V], root[V];
+      const float xm = sm[k] * (1.f / kStateM), xv = sv[k] * (1.f / kStateV);
       uint32_t top_m = 0, top_v = 0;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        v[j] = sqrtf(v[j]);
-        if (j < dup) continue;
+        p[j] = as_float(ep[k].v[j]);
+        m[j] = state_m(xm, em[k].v[j]);
+        const float r = state_root(xv, ev[k].v[j]);
+        float v = r * r;
+        root[j] = adam_update<true>(S, decay, as_float(eg[k].v[j]), p[j], m[j], v);
+        if (j < dup[k]) continue;
         top_m = max_u(top_m, magnitude(m[j]));
-        top_v = max_u(top_v, magnitude(v[j]));
+        top_v = max_u(top_v, __float_as_uint(root[j]));
       }
-      const StateScale sm = state_scale(wave_max(top_m, lanes), 127.f), sv = state_scale(wave_max(top_v, lanes), 255.f);
-      Elems<uint8_t, V> om, ov;
+      store_params<TP, V>(T, ip[k], p, dup[k]);
+      const StateScale am = state_scale(lanes_max(top_m, lanes), kStateM), av = state_scale(lanes_max(top_v, lanes), kStateV);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float km = sm.inverse == 0.f ? 0.f : __builtin_rintf(sqrtf(fabsf(m[j]) * sm.inverse));
-        float kv = sv.inverse == 0.f ? 0.f : __builtin_rintf(sqrtf(v[j] * sv.inverse));
-        if (kv < 1.f && v[j] > 0.f && sv.inverse != 0.f) kv = 1.f;
-        om.v[j] = static_cast<uint8_t>(static_cast<int>(copysignf(km, m[j])));
-        ov.v[j] = static_cast<uint8_t>(static_cast<int>(kv));
+        const float km = am.inverse == 0.f ? 0.f : __builtin_rintf(__builtin_amdgcn_sqrtf(fabsf(m[j]) * am.inverse));
+        const float kv = __builtin_rintf(__builtin_amdgcn_sqrtf(root[j] * av.inverse)), least = root[j] > 0.f ? 1.f : 0.f;
+        em[k].v[j] = static_cast<uint8_t>(static_cast<int>(copysignf(km, m[j])));
+        ev[k].v[j] = static_cast<uint8_t>(static_cast<int>(av.inverse == 0.f ? 0.f : fmaxf(kv, least)));
       }
-      store(static_cast<uint8_t*>(T.m) + ip, om);
-      store(static_cast<uint8_t*>(T.v) + ip, ov);
-      if (lane == 0) {
-        T.m_scale[is] = sm.kept;
-        T.v_scale[is] = sv.kept;
+      store_own(static_cast<uint8_t*>(T.m) + ip[k], em[k], dup[k]);
+      store_own(static_cast<uint8_t*>(T.v) + ip[k], ev[k], dup[k]);
+      if (lane == 0 && dup[k] < V) {
+        T.m_scale[is[k]] = am.kept;
+        T.v_scale[is[k]] = av.kept;
       }
-    } else {
-      Elems<float, V> om, ov;
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        om.v[j] = m[j];
-        ov.v[j] = v[j];
-      }
-      store(static_cast<float*>(T.m) + ip, om);
-      store(static_cast<float*>(T.v) + ip, ov);
     }
   }
 }
@@ -256,34 +321,33 @@ __device__ __forceinline__ void adam_block(const AdamArgs& A, const AdamTensor& 
 // Vectors of the widest type are 16 bytes; rows of fewer columns than a vector go element by element.
 template <typename TP, typename TG, bool BYTES>
 __device__ __forceinline__ void adam_any(const AdamArgs& A, const AdamTensor& T, const AdamStep& S, uint32_t q) {
-  constexpr int V = BYTES && sizeof(TP) == 2 && sizeof(TG) == 2 ? 8 : 4;
-  if (T.cols >= V) adam_block<TP, TG, V, BYTES>(A, T, S, q);
-  else adam_block<TP, TG, 1, BYTES>(A, T, S, q);
+  if constexpr (BYTES) {
+    constexpr int V = sizeof(TP) == 2 && sizeof(TG) == 2 ? 8 : 4;
+    if (T.cols < V) adam_bytes<TP, TG, 1, true>(A, T, S, q);
+    else if (T.rows > 1) adam_bytes<TP, TG, V, true>(A, T, S, q);
+    else adam_bytes<TP, TG, V, false>(A, T, S, q);
+  } else {
+    if (T.cols >= kAdamFloats) adam_floats<TP, TG, kAdamFloats>(A, T, S, q);
+    else adam_floats<TP, TG, 1>(A, T, S, q);
+  }
 }
 
-template <bool TABLE>
+template <bool BYTES>
 __global__ void __launch_bounds__(kThreads) k_adamw(AdamArgs A) {
   if (A.norm && !(fabsf(*A.norm) < __builtin_inff())) return;  // no step with a gradient that is not finite
   const uint32_t block = A.first_block + blockIdx.x;
-  const AdamTensor T = adam_tensor<TABLE>(A, block);
+  const AdamTensor T = adam_tensor(A, block);
   const uint32_t q = block - T.first_block;
   const AdamStep S = adam_step(A);
-  constexpr int F32 = SMFG_DTYPE_F32, F16 = SMFG_DTYPE_F16, BF16 = SMFG_DTYPE_BF16, BYTES = 1 << 12;
-  switch (T.type & (BYTES | 255)) {
-    case F32 | F32 << 4: adam_any<float, float, false>(A, T, S, q); break;
-    case F32 | F16 << 4: adam_any<float, _Float16, false>(A, T, S, q); break;
-    case F32 | BF16 << 4: adam_any<float, __bf16, false>(A, T, S, q); break;
-    case F16 | F16 << 4: adam_any<_Float16, _Float16, false>(A, T, S, q); break;
-    case F16 | F32 << 4: adam_any<_Float16, float, false>(A, T, S, q); break;
-    case BF16 | BF16 << 4: adam_any<__bf16, __bf16, false>(A, T, S, q); break;
-    case BF16 | F32 << 4: adam_any<__bf16, float, false>(A, T, S, q); break;
-    case F32 | F32 << 4 | BYTES: adam_any<float, float, true>(A, T, S, q); break;
-    case F32 | F16 << 4 | BYTES: adam_any<float, _Float16, true>(A, T, S, q); break;
-    case F32 | BF16 << 4 | BYTES: adam_any<float, __bf16, true>(A, T, S, q); break;
-    case F16 | F16 << 4 | BYTES: adam_any<_Float16, _Float16, true>(A, T, S, q); break;
-    case F16 | F32 << 4 | BYTES: adam_any<_Float16, float, true>(A, T, S, q); break;
-    case BF16 | BF16 << 4 | BYTES: adam_any<__bf16, __bf16, true>(A, T, S, q); break;
-    case BF16 | F32 << 4 | BYTES: adam_any<__bf16, float, true>(A, T, S, q); break;
+  constexpr int F32 = SMFG_DTYPE_F32, F16 = SMFG_DTYPE_F16, BF16 = SMFG_DTYPE_BF16;
+  switch (T.type & 255) {
+    case F32 | F32 << 4: adam_any<float, float, BYTES>(A, T, S, q); break;
+    case F32 | F16 << 4: adam_any<float, _Float16, BYTES>(A, T, S, q); break;
+    case F32 | BF16 << 4: adam_any<float, __bf16, BYTES>(A, T, S, q); break;
+    case F16 | F16 << 4: adam_any<_Float16, _Float16, BYTES>(A, T, S, q); break;
+    case F16 | F32 << 4: adam_any<_Float16, float, BYTES>(A, T, S, q); break;
+    case BF16 | BF16 << 4: adam_any<__bf16, __bf16, BYTES>(A, T, S, q); break;
+    default: adam_any<__bf16, float, BYTES>(A, T, S, q); break;
   }
 }
 
@@ -296,18 +360,57 @@ struct AdamValuesArgs {
   void* out;
   uint32_t first_block;
 };
-constexpr int kValueColumns = 2048;  // of a row, by a block
+// All values as one sequence, a vector of them a thread and turn; a block of kValueSpan begins anywhere in a row, the rest by 32-bit arithmetic.
+constexpr int kValueSpan = 8192;
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_adamw_values(AdamValuesArgs A) {
-  const int64_t block = static_cast<int64_t>(A.first_block) + blockIdx.x, pieces = (A.cols + kValueColumns - 1) / kValueColumns;
-  const int64_t row = A.rows == 1 ? 0 : block / pieces, row_units = (A.cols + kStateBlock - 1) / kStateBlock;
-  for (int k = 0; k < kValueColumns / kThreads; ++k) {
-    const int64_t c = (block - row * pieces) * kValueColumns + k * kThreads + static_cast<int>(threadIdx.x);
-    if (c >= A.cols) break;
-    const float s = A.scales[row * row_units + c / kStateBlock];
-    const uint8_t code = A.codes[row * A.cols + c];
-    const float root = state_root(s, code);
-    static_cast<T*>(A.out)[row * A.cols + c] = from_float<T>(A.second ? root * root : state_m(s, code));
+  constexpr int V = 8, kTurns = kValueSpan / kThreads / V;
+  const int64_t block = static_cast<int64_t>(A.first_block) + blockIdx.x, first = block * kValueSpan, all = A.rows * A.cols;
+  const int64_t row_units = (A.cols + kStateBlock - 1) / kStateBlock;
+  const int64_t first_row = A.rows == 1 ? 0 : first / A.cols, first_col = first - first_row * A.cols;
+  const float most = A.second ? kStateV : kStateM;
+  const auto value = [&](float scale, uint8_t k) {
+    const float root = state_root(scale, k);
+    return A.second ? root * root : state_m(scale, k);
+  };
+  Elems<uint8_t, V> e[kTurns];
+  float scale[kTurns];
+  int64_t row[kTurns], col[kTurns];
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int64_t i = first + (t * kThreads + static_cast<int>(threadIdx.x)) * V;
+    row[t] = first_row;
+    col[t] = i - first + first_col;
+    if (A.rows > 1) {  // first_col < cols <= 2^23
+      const uint32_t r = static_cast<uint32_t>(col[t]) / static_cast<uint32_t>(A.cols);
+      row[t] += r;
+      col[t] -= r * A.cols;
+    }
+    if (i + V > all) continue;
+    e[t] = *reinterpret_cast<const Elems<uint8_t, V>*>(A.codes + i);
+    scale[t] = A.scales[row[t] * row_units + col[t] / kStateBlock];
+  }
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int64_t i = first + (t * kThreads + static_cast<int>(threadIdx.x)) * V;
+    T* out = static_cast<T*>(A.out) + i;
+    const int64_t left = A.cols - col[t], here = kStateBlock - col[t] % kStateBlock;
+    if (i + V <= all && left >= V && here >= V) {
+      const float s = scale[t] / most;
+      Elems<T, V> o;
+#pragma unroll
+      for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(value(s, e[t].v[j]));
+      *reinterpret_cast<Elems<T, V>*>(out) = o;
+    } else {  // across rows or blocks, or at the end
+      int64_t r = row[t], c = col[t];
+      for (int j = 0; j < V && i + j < all; ++j) {
+        out[j] = from_float<T>(value(A.scales[r * row_units + c / kStateBlock] / most, A.codes[i + j]));
+        if (++c == A.cols) {
+          c = 0;
+          ++r;
+        }
+      }
+    }
   }
 }
 

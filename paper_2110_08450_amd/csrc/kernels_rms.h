@@ -38,14 +38,23 @@ struct RmsArgs {
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 __device__ __forceinline__ uint32_t max_u(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// Largest magnitude over groups of `lanes` lanes of a wave (a power of two).
-__device__ __forceinline__ uint32_t wave_max(uint32_t x, int lanes) {
-  for (int o = 1; o < lanes; o <<= 1) x = max_u(x, static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), o, 64)));
+// Largest of groups of `lanes` lanes (1 to 32, a power of two), within the 16 of a row by register moves between lanes.
+template <int CONTROL>
+__device__ __forceinline__ uint32_t max_with(uint32_t x) {
+  return max_u(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), CONTROL, 15, 15, true)));
+}
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x, int lanes) {
+  if (lanes > 1) x = max_with<0xb1>(x);   // the neighbour
+  if (lanes > 2) x = max_with<0x4e>(x);   // the other pair of four
+  if (lanes > 4) x = max_with<0x141>(x);  // the other four of eight, mirrored
+  if (lanes > 8) x = max_with<0x140>(x);  // the other eight of sixteen, mirrored
+  if (lanes > 16) x = max_u(x, static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), 16, 64)));
   return x;
 }
 template <int LANES>
 __device__ __forceinline__ uint32_t group_max(uint32_t x, uint32_t* lds) {
-  x = wave_max(x, LANES < 64 ? LANES : 64);
+  x = lanes_max(x, LANES < 32 ? LANES : 32);
+  if constexpr (LANES >= 64) x = max_u(x, static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), 32, 64)));
   if constexpr (LANES > 64) {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
@@ -190,7 +199,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_rms_norm(RmsArgs A) {
         for (int k = 1; k < NV; ++k) top[k] = top[0];
       } else {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) top[k] = wave_max(top[k], lanes < LANES ? lanes : LANES);
+        for (int k = 0; k < NV; ++k) top[k] = lanes_max(top[k], lanes < LANES ? lanes : LANES);
       }
 #pragma unroll
       for (int k = 0; k < NV; ++k)
@@ -278,7 +287,7 @@ __global__ void __launch_bounds__(kThreads) k_rms_norm_long(RmsArgs A) {
     float v[V];
     outputs(c, v);
     if constexpr (BYTES) {
-      if (A.group != 0) scale = byte_scale(wave_max(top_of(c, v), A.group / V), A.e4m3 != 0);
+      if (A.group != 0) scale = byte_scale(lanes_max(top_of(c, v), A.group / V), A.e4m3 != 0);
       store_bytes<V>(A, row, c, i, v, scale, A.group == 0 ? 1 << 30 : A.group / V);
     } else {
       T* y = static_cast<T*>(A.y) + row * A.y_stride;

@@ -62,7 +62,7 @@ def test_nothing_to_do_is_not_refused():
     assert call("smfg_rms_norm", BYTES, max_rows=0, x=None, y=None, scales=None) == smfg.OK
     assert call("smfg_rms_norm_grad", RGRAD, max_rows=0, t=None, dy=None, rstd=None, dw=None, scratch=None) == smfg.OK
     assert call("smfg_rms_norm_grad", RGRAD, dx=None, dw=None, scratch=None) == smfg.OK
-    assert smfg.lib().smfg_adamw((smfg._Param * 1)(), 0, hyper(), None, 0, None) == smfg.OK
+    assert smfg.lib().smfg_adamw((smfg._Param * 1)(), 0, hyper(), None) == smfg.OK
     assert adamw(numel=0, param=None, grad=None, m=None, v=None) == smfg.OK
     assert smfg.lib().smfg_adamw_values(None, None, 0, 0, 0, None, F32, None) == smfg.OK
 
@@ -81,8 +81,8 @@ def param(**change):
     return (smfg._Param * 1)(p)
 
 
-def adamw(h=None, n=1, scratch=P, nbytes=1 << 40, **change):
-    return smfg.lib().smfg_adamw(param(**change), n, h if h is not None else hyper(), scratch, nbytes, None)
+def adamw(h=None, n=1, **change):
+    return smfg.lib().smfg_adamw(param(**change), n, h if h is not None else hyper(), None)
 
 
 @pytest.mark.parametrize("change", [
@@ -94,7 +94,6 @@ def adamw(h=None, n=1, scratch=P, nbytes=1 << 40, **change):
     dict(state_bits=8, m_scale=P + 2, v_scale=P), dict(state_bits=8, m_scale=P, v_scale=P + 1), dict(numel=1 << 33, row_elems=2)])
 def test_adamw_refuses_tensors(change):
     assert adamw(**change) == ARG
-    assert smfg.lib().smfg_adamw_scratch_bytes(param(**change), 1) == -1
 
 
 def test_adamw_refusals():
@@ -102,21 +101,15 @@ def test_adamw_refusals():
     for k in ("param", "grad", "m", "v"):
         assert adamw(**{k: None}) == NULL
     assert adamw(state_bits=8, m_scale=P) == NULL and adamw(state_bits=8, v_scale=P) == NULL
-    assert L.smfg_adamw(None, 1, hyper(), P, 1 << 40, None) == NULL and L.smfg_adamw(param(), 1, None, P, 1 << 40, None) == NULL
-    assert L.smfg_adamw(param(), -1, hyper(), P, 1 << 40, None) == ARG
+    assert L.smfg_adamw(None, 1, hyper(), None) == NULL and L.smfg_adamw(param(), 1, None, None) == NULL
+    assert L.smfg_adamw(param(), -1, hyper(), None) == ARG
     inf, nan = float("inf"), float("nan")
     for bad in (dict(lr=nan), dict(lr=inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta1=nan), dict(beta2=1.0), dict(beta2=-1e-9), dict(eps=-1e-9), dict(eps=inf),
                 dict(eps=nan), dict(scale=inf), dict(scale=nan), dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=nan), dict(step=0), dict(step=-1),
                 dict(step=1 << 48), dict(step=-1, d_step=P), dict(d_step=P + 4), dict(d_lr=P + 2), dict(d_norm=P + 1)):
         assert adamw(hyper(**bad)) == ARG, bad
-    assert adamw(scratch=P + 16) == ARG
-    many = (smfg._Param * 300)(*[param()[0] for _ in range(300)])
-    need = L.smfg_adamw_scratch_bytes(many, 300)
-    assert need > 0 and L.smfg_adamw_scratch_bytes(param(), 1) == 0 and L.smfg_adamw_scratch_bytes(None, 0) == 0
-    assert L.smfg_adamw(many, 300, hyper(), P, need - 1, None) == ROOM and L.smfg_adamw(many, 300, hyper(), None, need, None) == NULL
-    assert L.smfg_adamw_scratch_bytes(None, 1) == -1 and L.smfg_adamw_scratch_bytes(param(), -1) == -1
     huge = (smfg._Param * 70_000)(*[param(numel=(1 << 48) - 1, grad_dtype=F32)[0]] * 70_000)
-    assert L.smfg_adamw(huge, 70_000, hyper(), P, 1 << 40, None) == ARG  # more blocks than have numbers
+    assert L.smfg_adamw(huge, 70_000, hyper(), None) == ARG  # more blocks than have numbers
 
 
 VALUES = dict(codes=P, scales=P, numel=4096, row_elems=0, second=0, out=P, otype=F32, stream=None)
@@ -171,12 +164,12 @@ def tensor(*shape, dtype=torch.float32):
 def test_lists_of_tensors_are_checked():
     """Sizes and types that the binding alone can see."""
     p, g, m, v = [tensor(300) for _ in range(4)]
-    smfg.adamw_list([p], [g], [m], [v], device="cpu")
+    smfg.adamw_list([p], [g], [m], [v])
     k, u, s = tensor(300, dtype=torch.int8), tensor(300, dtype=torch.uint8), tensor(3)
-    smfg.adamw_list([p], [g], [k], [u], [s], [s.clone()], device="cpu")
+    smfg.adamw_list([p], [g], [k], [u], [s], [s.clone()])
     table, states = tensor(4, 200), (tensor(4, 200, dtype=torch.int8), tensor(4, 200, dtype=torch.uint8), tensor(4, 2))
     made = smfg.adamw_list([table], [tensor(3, 200)], [states[0]], [states[1]], [states[2]], [states[2].clone()], rows=[tensor(1, dtype=torch.int64)],
-                           row_ids=[tensor(3, dtype=torch.int32)], device="cpu")
+                           row_ids=[tensor(3, dtype=torch.int32)])
     assert made.c[0].row_elems == 200 and made.c[0].num_rows == 4 and made.c[0].numel == 600
     for bad in (dict(g=[tensor(299)]), dict(m=[tensor(301)]), dict(v=[tensor(5)]), dict(m=[k], v=[u]), dict(m=[k], v=[u], m_scales=[tensor(2)], v_scales=[tensor(2)]),
                 dict(m=[k], v=[k], m_scales=[s], v_scales=[s]), dict(m=[k], v=[u], m_scales=[s], v_scales=[tensor(4)]), dict(copies=[tensor(10, dtype=torch.float16)]),
@@ -184,10 +177,10 @@ def test_lists_of_tensors_are_checked():
         args = dict(p=[p], g=[g], m=[m], v=[v])
         args.update(bad)
         with pytest.raises(AssertionError):
-            smfg.adamw_list(args.pop("p"), args.pop("g"), args.pop("m"), args.pop("v"), device="cpu", **args)
+            smfg.adamw_list(args.pop("p"), args.pop("g"), args.pop("m"), args.pop("v"), **args)
     with pytest.raises(AssertionError):
-        smfg.adamw_list([p, p], [g, g], [m, tensor(300)], [v, tensor(300)], device="cpu")  # two steps of one tensor at once
+        smfg.adamw_list([p, p], [g, g], [m, tensor(300)], [v, tensor(300)])  # two steps of one tensor at once
     with pytest.raises(AssertionError):
-        smfg.adamw_list([table], [tensor(3, 100)], [tensor(4, 200)], [tensor(4, 200)], row_ids=[tensor(3, dtype=torch.int32)], device="cpu")
+        smfg.adamw_list([table], [tensor(3, 100)], [tensor(4, 200)], [tensor(4, 200)], row_ids=[tensor(3, dtype=torch.int32)])
     with pytest.raises(AssertionError):
-        smfg.adamw_list([table], [tensor(3, 200)], [tensor(4, 200)], [tensor(4, 200)], row_ids=[tensor(2, dtype=torch.int32)], device="cpu")
+        smfg.adamw_list([table], [tensor(3, 200)], [tensor(4, 200)], [tensor(4, 200)], row_ids=[tensor(2, dtype=torch.int32)])
