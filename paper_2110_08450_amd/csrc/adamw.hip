@@ -54,13 +54,13 @@ struct AdamShape {
   uint32_t units[2];
 };
 inline int64_t blocks_of(const smfg_param_t& p, const AdamShape& S) {
-  return ceil_div(items_of(p), p.state_bits == 8 ? S.units[1] : S.units[0] * (kStateBlock / kAdamFloats));
+  const size_t pb = static_cast<size_t>(type_bytes(p.param_dtype)), gb = static_cast<size_t>(type_bytes(p.grad_dtype));
+  return ceil_div(items_of(p), p.state_bits == 8 ? S.units[1] * adam_bytes_wide(pb, gb, cols_of(p)) : S.units[0] * (kStateBlock / kAdamFloats));
 }
 AdamShape adam_shape(const smfg_param_t* p, int32_t n) {
   AdamShape S = {{0, 0}, {8, 16}};
   double all[2] = {0, 0};
   for (int i = 0; i < n; ++i) all[p[i].state_bits == 8] += static_cast<double>(p[i].numel) / kStateBlock;
-  while (S.units[1] < 64 && all[1] > 2048.0 * 2 * S.units[1]) S.units[1] *= 2;
   for (int k = 0; k < 2; ++k)
     while (S.units[k] < 512 && all[k] > 1048576.0 * S.units[k]) S.units[k] *= 2;
   for (int i = 0; i < n; ++i) S.blocks[p[i].state_bits == 8] += blocks_of(p[i], S);
@@ -87,9 +87,10 @@ int smfg_adamw(const smfg_param_t* params, int32_t num_params, const smfg_adamw_
   A.first_block = 0;
   A.lr = static_cast<float>(h.lr);
   A.b1 = static_cast<float>(h.beta1);
-  A.one_b1 = static_cast<float>(1.0 - h.beta1);
   A.b2 = static_cast<float>(h.beta2);
-  A.one_b2 = static_cast<float>(1.0 - h.beta2);
+  A.root_b2 = static_cast<float>(std::sqrt(h.beta2));
+  A.one_b1 = 1.0 - h.beta1;
+  A.root_one_b2 = std::sqrt(1.0 - h.beta2);
   A.eps = static_cast<float>(h.eps);
   A.log_b1 = std::log(h.beta1);
   A.log_b2 = std::log(h.beta2);

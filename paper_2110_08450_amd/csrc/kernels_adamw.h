@@ -41,9 +41,9 @@ struct AdamArgs {
   int32_t tensors;
   uint32_t first_block;  // of the launch
   uint32_t units;  // a block of threads has this many times kStateBlock elements
-  float lr, one_b1, b1, one_b2, b2, eps;
+  float lr, b1, b2, root_b2, eps;
   float step_size, root;  // without a step on the device: lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
-  double log_b1, log_b2, scale, max_norm;
+  double one_b1, root_one_b2, log_b1, log_b2, scale, max_norm;
   int64_t step;
   const int64_t* d_step;
   const float* d_lr;
@@ -58,11 +58,11 @@ __device__ __forceinline__ AdamTensor adam_tensor(const AdamArgs& A, uint32_t bl
   return A.t[__popcll(__ballot(lane < A.tensors && block >= A.t[lane < A.tensors ? lane : 0].first_block)) - 1];
 }
 
-// The numbers of a step that are the same for all elements.
+// The numbers of a step that are the same for all elements.  The gradient's factor f is in those of the moments: m = b1 m + g1 g, v = b2 v + (g2 g)^2 with
+// g1 = (1 - b1) f and g2 = sqrt(1 - b2) f.  Where f is below 2^-100, g is multiplied by 2^power first, as a float has few digits left there.
 struct AdamStep {
-  float f;  // of the gradient
   int power;
-  float lr, step, root, eps, b1, one_b1, b2, one_b2;
+  float lr, step, root, eps, b1, b2, root_b2, g1, g2;
 };
 __device__ __forceinline__ AdamStep adam_step(const AdamArgs& A) {
   AdamStep S;
@@ -79,29 +79,36 @@ __device__ __forceinline__ AdamStep adam_step(const AdamArgs& A) {
   }
   S.eps = A.eps;
   S.b1 = A.b1;
-  S.one_b1 = A.one_b1;
   S.b2 = A.b2;
-  S.one_b2 = A.one_b2;
+  S.root_b2 = A.root_b2;
   double f = A.scale;
   if (A.norm) {
     const double c = A.max_norm / (static_cast<double>(*A.norm) + 1e-6);
     if (c < 1.0) f *= c;
   }
   S.power = 0;
-  if (fabs(f) < 0x1p-100 && f != 0.0) f = frexp(f, &S.power);  // a float has few digits left there
-  S.f = static_cast<float>(f);
+  if (fabs(f) < 0x1p-100 && f != 0.0) f = frexp(f, &S.power);
+  S.power = __builtin_amdgcn_readfirstlane(S.power);  // the same for all lanes
+  S.g1 = static_cast<float>(A.one_b1 * f);
+  S.g2 = static_cast<float>(A.root_one_b2 * f);
   return S;
 }
-// The update of an element, and the root of its second moment.  States of 8 bits keep the hardware busy with roots: theirs are its own, off by one in the last digit
+// A vector's gradients, times the factor's power.
+template <typename TG, int V>
+__device__ __forceinline__ void adam_gradient(const AdamStep& S, const Elems<TG, V>& e, float (&g)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) g[j] = as_float(e.v[j]);
+  if (S.power != 0) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) g[j] = __builtin_ldexpf(g[j], S.power);
+  }
+}
+// The parameter from the moments, and the root of the second.  States of 8 bits keep the hardware busy with roots: theirs are its own, off by one in the last digit
 // (a v below 2^-126 counts as 0), and the quotient is a product with its reciprocal; floats, which the memory bounds, have the exact ones.
 template <bool FAST>
-__device__ __forceinline__ float adam_update(const AdamStep& S, float decay, float g, float& p, float& m, float& v) {
-  g *= S.f;
-  if (S.power != 0) g = __builtin_ldexpf(g, S.power);
-  m = S.b1 * m + S.one_b1 * g;
-  v = S.b2 * v + S.one_b2 * g * g;
+__device__ __forceinline__ float adam_update(const AdamStep& S, float keep, float& p, float m, float v) {
   const float root = FAST ? __builtin_amdgcn_sqrtf(v) : sqrtf(v), den = root * S.root + S.eps;
-  p = p - decay * p - (FAST ? S.step * m * __builtin_amdgcn_rcpf(den) : S.step * m / den);
+  p = FAST ? p * keep - S.step * m * __builtin_amdgcn_rcpf(den) : p * keep - S.step * m / den;
   return root;
 }
 
@@ -204,7 +211,7 @@ __device__ __forceinline__ void adam_floats(const AdamArgs& A, const AdamTensor&
   const int64_t first = static_cast<int64_t>(q) * most;
   const int count = items_of(rows_of(T) * per_row, first, most);
   const int64_t first_row = T.rows == 1 ? 0 : first / per_row, first_at = first - first_row * per_row;
-  const float decay = S.lr * T.decay;
+  const float keep = 1.f - S.lr * T.decay;
   for (int i = static_cast<int>(threadIdx.x); i < count; i += kThreads) {
     const AdamPlace a = place_of(T.rows, per_row, first_row, first_at, i);
     // the last vector of a row ends with it; the columns that it shares with the one before are left to that
@@ -219,11 +226,14 @@ __device__ __forceinline__ void adam_floats(const AdamArgs& A, const AdamTensor&
     const Elems<TG, V> eg = load_once<TG, V>(static_cast<const TG*>(T.g) + ig);
     const Elems<TP, V> ep = load_once<TP, V>(static_cast<const TP*>(T.p) + ip);
     Elems<float, V> em = load_once<float, V>(static_cast<const float*>(T.m) + ip), ev = load_once<float, V>(static_cast<const float*>(T.v) + ip);
-    float p[V];
+    float p[V], g[V];
+    adam_gradient(S, eg, g);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       p[j] = as_float(ep.v[j]);
-      adam_update<false>(S, decay, as_float(eg.v[j]), p[j], em.v[j], ev.v[j]);
+      em.v[j] = S.b1 * em.v[j] + S.g1 * g[j];
+      ev.v[j] = S.b2 * ev.v[j] + (S.g2 * g[j]) * (S.g2 * g[j]);
+      adam_update<false>(S, keep, p[j], em.v[j], ev.v[j]);
     }
     store_params<TP, V>(T, ip, p, dup);
     store_own(static_cast<float*>(T.m) + ip, em, dup);
@@ -231,6 +241,11 @@ __device__ __forceinline__ void adam_floats(const AdamArgs& A, const AdamTensor&
   }
 }
 
+// Columns of a vector where states are of 8 bits, so that the widest of its types is 16 bytes, and how many times A.units a block has of them then.
+__host__ __device__ constexpr int adam_bytes_vector(size_t param, size_t grad) { return param == 2 && grad == 2 ? 8 : 4; }
+__host__ __device__ constexpr uint32_t adam_bytes_wide(size_t param, size_t grad, int64_t cols) {
+  return adam_bytes_vector(param, grad) == 8 && cols >= 8 ? 2 : 1;
+}
 // States of 8 bits: an item is a block of kStateBlock columns, whose largest values its lanes tell each other.
 // Rows are read through the caches: those of few bytes share their lines with their neighbours (200 K rows of 100 halfs 404 us instead of 431).
 template <typename T, int V, bool ROWS>
@@ -244,76 +259,84 @@ __device__ __forceinline__ void adam_bytes(const AdamArgs& A, const AdamTensor& 
   const int vectors = static_cast<int>(T.cols < kStateBlock ? (T.cols + V - 1) / V : kStateBlock / V);
   int lanes = 1;
   while (lanes < vectors) lanes <<= 1;
-  const int64_t per_row = (T.cols + kStateBlock - 1) / kStateBlock, first = static_cast<int64_t>(q) * A.units;
-  const int count = items_of(rows_of(T) * per_row, first, A.units);
+  const uint32_t most = A.units * adam_bytes_wide(sizeof(TP), sizeof(TG), T.cols);
+  const int64_t per_row = (T.cols + kStateBlock - 1) / kStateBlock, first = static_cast<int64_t>(q) * most;
+  const int count = items_of(rows_of(T) * per_row, first, most);
   const int64_t first_row = T.rows == 1 ? 0 : first / per_row, first_at = first - first_row * per_row;
+  const bool ragged = T.cols % V != 0;
   const int lane = static_cast<int>(threadIdx.x) & (lanes - 1), mine = static_cast<int>(threadIdx.x) / lanes, at_once = kThreads / lanes;
-  const float decay = S.lr * T.decay;
-  constexpr int kTurns = 2;
-  for (int base = 0; base < count; base += kTurns * at_once) {
-    int64_t ig[kTurns], ip[kTurns], is[kTurns];
-    int dup[kTurns];
-#pragma unroll
-    for (int k = 0; k < kTurns; ++k) {
-      const int i = base + k * at_once + mine;
-      const AdamPlace a = place_of(T.rows, per_row, first_row, first_at, i < count ? i : 0);
-      const int64_t c = a.at * kStateBlock + lane * V, start = c + V <= T.cols ? c : T.cols - V;
-      dup[k] = i >= count || c >= T.cols || lane >= vectors ? V : static_cast<int>(c - start);
-      int64_t to = a.row;
-      if (T.ids) {
-        const int32_t id = T.ids[a.row];
-        const bool inside = static_cast<uint32_t>(id) < static_cast<uint32_t>(T.table_rows);
-        if (!inside) dup[k] = V;
-        to = inside ? id : 0;
-      }
-      ig[k] = a.row * T.cols + start;
-      ip[k] = to * T.cols + start;
-      is[k] = to * per_row + a.at;
+  const float keep = 1.f - S.lr * T.decay;
+  for (int base = 0; base < count; base += at_once) {
+    const int i = base + mine;
+    const AdamPlace a = place_of(T.rows, per_row, first_row, first_at, i < count ? i : 0);
+    const int64_t c = a.at * kStateBlock + lane * V, start = c + V <= T.cols ? c : T.cols - V;
+    int dup = i >= count || c >= T.cols || lane >= vectors ? V : static_cast<int>(c - start);
+    int64_t to = a.row;
+    if (T.ids) {
+      const int32_t id = T.ids[a.row];
+      const bool inside = static_cast<uint32_t>(id) < static_cast<uint32_t>(T.table_rows);
+      if (!inside) dup = V;
+      to = inside ? id : 0;
     }
-    Elems<TG, V> eg[kTurns];
-    Elems<TP, V> ep[kTurns];
-    Elems<uint8_t, V> em[kTurns], ev[kTurns];
-    float sm[kTurns], sv[kTurns];
+    const int64_t ig = a.row * T.cols + start, ip = to * T.cols + start, is = to * per_row + a.at;
+    const Elems<TG, V> eg = load_once<TG, V>(static_cast<const TG*>(T.g) + ig);
+    const Elems<TP, V> ep = load_bytes<TP, V, ROWS>(static_cast<const TP*>(T.p) + ip);
+    Elems<uint8_t, V> em = load_bytes<uint8_t, V, ROWS>(static_cast<const uint8_t*>(T.m) + ip);
+    Elems<uint8_t, V> ev = load_bytes<uint8_t, V, ROWS>(static_cast<const uint8_t*>(T.v) + ip);
+    const float xm = T.m_scale[is] * (1.f / kStateM), xv = T.v_scale[is] * (1.f / kStateV);
+    float p[V], m[V], root[V], g[V];
+    adam_gradient(S, eg, g);
 #pragma unroll
-    for (int k = 0; k < kTurns; ++k) {
-      eg[k] = load_once<TG, V>(static_cast<const TG*>(T.g) + ig[k]);
-      ep[k] = load_bytes<TP, V, ROWS>(static_cast<const TP*>(T.p) + ip[k]);
-      em[k] = load_bytes<uint8_t, V, ROWS>(static_cast<const uint8_t*>(T.m) + ip[k]);
-      ev[k] = load_bytes<uint8_t, V, ROWS>(static_cast<const uint8_t*>(T.v) + ip[k]);
-      sm[k] = T.m_scale[is[k]];
-      sv[k] = T.v_scale[is[k]];
+    for (int j = 0; j < V; ++j) {
+      p[j] = as_float(ep.v[j]);
+      const float r = state_root(xv * S.root_b2, ev.v[j]);
+      m[j] = state_m(xm * S.b1, em.v[j]) + S.g1 * g[j];
+      root[j] = adam_update<true>(S, keep, p[j], m[j], r * r + (S.g2 * g[j]) * (S.g2 * g[j]));
     }
-#pragma unroll
-    for (int k = 0; k < kTurns; ++k) {
-      float p[V], m[V], root[V];
-      const float xm = sm[k] * (1.f / kStateM), xv = sv[k] * (1.f / kStateV);
-      uint32_t top_m = 0, top_v = 0;
+    store_params<TP, V>(T, ip, p, dup);
+    if (ragged) {  // columns of the block before
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        p[j] = as_float(ep[k].v[j]);
-        m[j] = state_m(xm, em[k].v[j]);
-        const float r = state_root(xv, ev[k].v[j]);
-        float v = r * r;
-        root[j] = adam_update<true>(S, decay, as_float(eg[k].v[j]), p[j], m[j], v);
-        if (j < dup[k]) continue;
-        top_m = max_u(top_m, magnitude(m[j]));
-        top_v = max_u(top_v, __float_as_uint(root[j]));
+        m[j] = j < dup ? 0.f : m[j];
+        root[j] = j < dup ? 0.f : root[j];
       }
-      store_params<TP, V>(T, ip[k], p, dup[k]);
-      const StateScale am = state_scale(lanes_max(top_m, lanes), kStateM), av = state_scale(lanes_max(top_v, lanes), kStateV);
+    }
+    float top_m = 0.f;
+    uint32_t top_v = 0;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float km = am.inverse == 0.f ? 0.f : __builtin_rintf(__builtin_amdgcn_sqrtf(fabsf(m[j]) * am.inverse));
-        const float kv = __builtin_rintf(__builtin_amdgcn_sqrtf(root[j] * av.inverse)), least = root[j] > 0.f ? 1.f : 0.f;
-        em[k].v[j] = static_cast<uint8_t>(static_cast<int>(copysignf(km, m[j])));
-        ev[k].v[j] = static_cast<uint8_t>(static_cast<int>(av.inverse == 0.f ? 0.f : fmaxf(kv, least)));
-      }
-      store_own(static_cast<uint8_t*>(T.m) + ip[k], em[k], dup[k]);
-      store_own(static_cast<uint8_t*>(T.v) + ip[k], ev[k], dup[k]);
-      if (lane == 0 && dup[k] < V) {
-        T.m_scale[is[k]] = am.kept;
-        T.v_scale[is[k]] = av.kept;
-      }
+    for (int j = 0; j < V; ++j) {
+      top_m = fmaxf(top_m, fabsf(m[j]));
+      top_v = max_u(top_v, __float_as_uint(root[j]));
+    }
+    // no maximum of floats lets a NaN through: it is in the root as well, but for one that a kept scale brought
+    if (!(fabsf(xm) < __builtin_inff())) top_v = 0x7fc00000u;
+    if (dup == V) {
+      top_m = 0.f;
+      top_v = 0;
+    }
+    top_v = lanes_max(top_v, lanes);
+    const StateScale av = state_scale(top_v, kStateV), am = state_scale(max_u(lanes_max(__float_as_uint(top_m), lanes), top_v < 0x7f800000u ? 0 : top_v), kStateM);
+    uint32_t wm[(V + 3) / 4], wv[(V + 3) / 4];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (j % 4 == 0) wm[j / 4] = wv[j / 4] = 0;
+      // The instruction rounds to nearest even, holds what is beyond to 0 or 255, and puts the byte in its place.  128 makes the signed ones positive.
+      const float km = copysignf(__builtin_amdgcn_sqrtf(fabsf(m[j]) * am.inverse), m[j]) + 128.f;
+      wm[j / 4] = __builtin_amdgcn_cvt_pk_u8_f32(km, j % 4, wm[j / 4]);
+      // at least 1 where the root, which is 2^-75 at least, is not 0
+      const float kv = __builtin_amdgcn_fmed3f(__builtin_amdgcn_sqrtf(root[j] * av.inverse), 1.f, root[j] * 0x1p100f);
+      wv[j / 4] = __builtin_amdgcn_cvt_pk_u8_f32(kv, j % 4, wv[j / 4]);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      em.v[j] = static_cast<uint8_t>((wm[j / 4] ^ 0x80808080u) >> 8 * (j % 4));
+      ev.v[j] = static_cast<uint8_t>(wv[j / 4] >> 8 * (j % 4));
+    }
+    store_own(static_cast<uint8_t*>(T.m) + ip, em, dup);
+    store_own(static_cast<uint8_t*>(T.v) + ip, ev, dup);
+    if (lane == 0 && dup < V) {
+      T.m_scale[is] = am.kept;
+      T.v_scale[is] = av.kept;
     }
   }
 }
@@ -322,7 +345,7 @@ __device__ __forceinline__ void adam_bytes(const AdamArgs& A, const AdamTensor& 
 template <typename TP, typename TG, bool BYTES>
 __device__ __forceinline__ void adam_any(const AdamArgs& A, const AdamTensor& T, const AdamStep& S, uint32_t q) {
   if constexpr (BYTES) {
-    constexpr int V = sizeof(TP) == 2 && sizeof(TG) == 2 ? 8 : 4;
+    constexpr int V = adam_bytes_vector(sizeof(TP), sizeof(TG));
     if (T.cols < V) adam_bytes<TP, TG, 1, true>(A, T, S, q);
     else if (T.rows > 1) adam_bytes<TP, TG, V, true>(A, T, S, q);
     else adam_bytes<TP, TG, V, false>(A, T, S, q);
