@@ -139,8 +139,12 @@ int smfg_adamw_values(const void* d_codes, const float* d_scales, int64_t numel,
   Launches go(hip_stream);
   const int64_t cols = row_elems > 0 ? row_elems : numel, blocks = ceil_div(numel, kValueSpan);
   if (blocks >= (int64_t(1) << 32)) return SMFG_ERR_INVALID_ARG;
-  const AdamValuesArgs A = {static_cast<const uint8_t*>(d_codes), d_scales, numel / cols, cols, second, d_out, 0};
-  with_type(out_dtype, [&](auto t) { go.all(k_adamw_values<decltype(t)>, blocks, kThreads, A); });
+  const AdamValuesArgs A = {static_cast<const uint8_t*>(d_codes), d_scales, numel / cols, cols, d_out, 0};
+  with_type(out_dtype, [&](auto t) {
+    using T = decltype(t);
+    if (A.rows > 1) second ? go.all(k_adamw_values<T, true, true>, blocks, kThreads, A) : go.all(k_adamw_values<T, true, false>, blocks, kThreads, A);
+    else second ? go.all(k_adamw_values<T, false, true>, blocks, kThreads, A) : go.all(k_adamw_values<T, false, false>, blocks, kThreads, A);
+  });
   return go.result();
 }
 

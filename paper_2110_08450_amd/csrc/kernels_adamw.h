@@ -167,19 +167,13 @@ __device__ __forceinline__ Elems<T, V> load_once(const T* src) {
     return __builtin_bit_cast(Elems<T , V>, x);
   }
 }
-// V values, of which the first `dup` are left alone.
+// The same for what is written; the first `dup` are left alone.
 template <typename T, int V>
-__device__ __forceinline__ void store_own(T* dst, const Elems<T, V>& e, int dup) {
-  if (dup == 0) {
-    if constexpr (V == 1) {
-      *reinterpret_cast<Elems<T, V>*>(dst) = e;
-    } else {
-      __builtin_nontemporal_store(__builtin_bit_cast(Raw<T , V>, e), reinterpret_cast<Raw<T, V>*>(dst));
-    }
-  } else if (dup < V) {
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (j >= dup) dst[j] = e.v[j];
+__device__ __forceinline__ void store_once(T* dst, const Elems<T, V>& e, int dup) {
+  if (V > 1 && dup == 0) {
+    if constexpr (V > 1) __builtin_nontemporal_store(__builtin_bit_cast(Raw<T, V>, e), reinterpret_cast<Raw<T, V>*>(dst));
+  } else {
+    store_own(dst, e, dup);
   }
 }
 template <typename TP, int V>
@@ -187,18 +181,18 @@ __device__ __forceinline__ void store_params(const AdamTensor& T, int64_t at, co
   Elems<TP, V> e;
 #pragma unroll
   for (int j = 0; j < V; ++j) e.v[j] = from_float<TP>(p[j]);
-  store_own(static_cast<TP*>(T.p) + at, e, dup);
+  store_once(static_cast<TP*>(T.p) + at, e, dup);
   if (!T.copy) return;
   if ((T.type >> 8 & 15) == SMFG_DTYPE_F16) {
     Elems<_Float16, V> o;
 #pragma unroll
     for (int j = 0; j < V; ++j) o.v[j] = from_float<_Float16>(p[j]);
-    store_own(static_cast<_Float16*>(T.copy) + at, o, dup);
+    store_once(static_cast<_Float16*>(T.copy) + at, o, dup);
   } else {
     Elems<__bf16, V> o;
 #pragma unroll
     for (int j = 0; j < V; ++j) o.v[j] = from_float<__bf16>(p[j]);
-    store_own(static_cast<__bf16*>(T.copy) + at, o, dup);
+    store_once(static_cast<__bf16*>(T.copy) + at, o, dup);
   }
 }
 
@@ -236,8 +230,8 @@ __device__ __forceinline__ void adam_floats(const AdamArgs& A, const AdamTensor&
       adam_update<false>(S, keep, p[j], em.v[j], ev.v[j]);
     }
     store_params<TP, V>(T, ip, p, dup);
-    store_own(static_cast<float*>(T.m) + ip, em, dup);
-    store_own(static_cast<float*>(T.v) + ip, ev, dup);
+    store_once(static_cast<float*>(T.m) + ip, em, dup);
+    store_once(static_cast<float*>(T.v) + ip, ev, dup);
   }
 }
 
@@ -332,8 +326,8 @@ __device__ __forceinline__ void adam_bytes(const AdamArgs& A, const AdamTensor& 
       em.v[j] = static_cast<uint8_t>((wm[j / 4] ^ 0x80808080u) >> 8 * (j % 4));
       ev.v[j] = static_cast<uint8_t>(wv[j / 4] >> 8 * (j % 4));
     }
-    store_own(static_cast<uint8_t*>(T.m) + ip, em, dup);
-    store_own(static_cast<uint8_t*>(T.v) + ip, ev, dup);
+    store_once(static_cast<uint8_t*>(T.m) + ip, em, dup);
+    store_once(static_cast<uint8_t*>(T.v) + ip, ev, dup);
     if (lane == 0 && dup < V) {
       T.m_scale[is] = am.kept;
       T.v_scale[is] = av.kept;
@@ -379,60 +373,59 @@ struct AdamValuesArgs {
   const uint8_t* codes;
   const float* scales;
   int64_t rows, cols;
-  int32_t second;
   void* out;
   uint32_t first_block;
 };
 // All values as one sequence, a vector of them a thread and turn; a block of kValueSpan begins anywhere in a row, the rest by 32-bit arithmetic.
 constexpr int kValueSpan = 8192;
-template <typename T>
+// A vector of a single row lies within one block, as it begins at a multiple of V.
+template <typename T, bool ROWS, bool SECOND>
 __global__ void __launch_bounds__(kThreads) k_adamw_values(AdamValuesArgs A) {
   constexpr int V = 8, kTurns = kValueSpan / kThreads / V;
   const int64_t block = static_cast<int64_t>(A.first_block) + blockIdx.x, first = block * kValueSpan, all = A.rows * A.cols;
   const int64_t row_units = (A.cols + kStateBlock - 1) / kStateBlock;
   const int64_t first_row = A.rows == 1 ? 0 : first / A.cols, first_col = first - first_row * A.cols;
-  const float most = A.second ? kStateV : kStateM;
+  constexpr float most = 1.f / (SECOND ? kStateV : kStateM);
   const auto value = [&](float scale, uint8_t k) {
+    if constexpr (!SECOND) return state_m(scale, k);
     const float root = state_root(scale, k);
-    return A.second ? root * root : state_m(scale, k);
+    return root * root;
   };
   Elems<uint8_t, V> e[kTurns];
-  float scale[kTurns];
-  int64_t row[kTurns], col[kTurns];
+  float scale[kTurns][2];  // of the vector's first elements, and of those from `cut` on
+  int cut[kTurns];         // V: there are none; negative: element by element
+  if (all >= V) {          // loads without conditions, all on their way before one is used
 #pragma unroll
-  for (int t = 0; t < kTurns; ++t) {
-    const int64_t i = first + (t * kThreads + static_cast<int>(threadIdx.x)) * V;
-    row[t] = first_row;
-    col[t] = i - first + first_col;
-    if (A.rows > 1) {  // first_col < cols <= 2^23
-      const uint32_t r = static_cast<uint32_t>(col[t]) / static_cast<uint32_t>(A.cols);
-      row[t] += r;
-      col[t] -= r * A.cols;
+    for (int t = 0; t < kTurns; ++t) {
+      const int here = (t * kThreads + static_cast<int>(threadIdx.x)) * V, i = first + here + V <= all ? here : 0;
+      const AdamPlace at = ROWS ? place_of(A.rows, A.cols, first_row, first_col, i) : AdamPlace{0, first + i};
+      const int64_t unit = at.row * row_units + at.at / kStateBlock;
+      e[t] = *reinterpret_cast<const Elems<uint8_t, V>*>(A.codes + (first + V <= all ? first + i : 0));
+      scale[t][0] = A.scales[unit];
+      cut[t] = i == here && first + here + V <= all ? V : -1;
+      if constexpr (ROWS) {
+        const int64_t left = A.cols - at.at, room = kStateBlock - at.at % kStateBlock, end = left < room ? left : room;  // of the block
+        const int64_t next = left > room ? left - room : A.cols;
+        if (cut[t] == V && end < V) cut[t] = next < V - end ? -1 : static_cast<int>(end);  // not across a third block
+        scale[t][1] = A.scales[cut[t] > 0 && cut[t] < V ? unit + 1 : unit];  // the next one of the row, or the first of the next row
+      }
     }
-    if (i + V > all) continue;
-    e[t] = *reinterpret_cast<const Elems<uint8_t, V>*>(A.codes + i);
-    scale[t] = A.scales[row[t] * row_units + col[t] / kStateBlock];
   }
 #pragma unroll
   for (int t = 0; t < kTurns; ++t) {
-    const int64_t i = first + (t * kThreads + static_cast<int>(threadIdx.x)) * V;
-    T* out = static_cast<T*>(A.out) + i;
-    const int64_t left = A.cols - col[t], here = kStateBlock - col[t] % kStateBlock;
-    if (i + V <= all && left >= V && here >= V) {
-      const float s = scale[t] / most;
+    const int here = (t * kThreads + static_cast<int>(threadIdx.x)) * V;
+    T* out = static_cast<T*>(A.out) + first + here;
+    if (all >= V && cut[t] >= 0) {
       Elems<T, V> o;
 #pragma unroll
-      for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(value(s, e[t].v[j]));
+      for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(value((ROWS && j >= cut[t] ? scale[t][1] : scale[t][0]) * most, e[t].v[j]));
       *reinterpret_cast<Elems<T, V>*>(out) = o;
-    } else {  // across rows or blocks, or at the end
-      int64_t r = row[t], c = col[t];
-      for (int j = 0; j < V && i + j < all; ++j) {
-        out[j] = from_float<T>(value(A.scales[r * row_units + c / kStateBlock] / most, A.codes[i + j]));
-        if (++c == A.cols) {
-          c = 0;
-          ++r;
-        }
+    } else {
+      for (int j = 0; j < V && first + here + j < all; ++j) {
+        const AdamPlace at = place_of(A.rows, A.cols, first_row, first_col, here + j);
+        out[j] = from_float<T>(value(A.scales[at.row * row_units + at.at / kStateBlock] * most, A.codes[first + here + j]));
       }
+      asm volatile("" ::: "memory");  // as in store_own
     }
   }
 }

@@ -198,13 +198,8 @@ __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs 
       Elems<T, V> o;
 #pragma unroll
       for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(v[k][j]);
-      if (!ragged || col.dup == 0) {
-        *reinterpret_cast<Elems<T, V>*>(dx + col.start) = o;
-      } else {  // columns that two vectors share have other roundings in each, as the lanes' maxima differ: the first writes them
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (j >= col.dup) dx[col.start + j] = o.v[j];
-      }
+      // columns that two vectors share have other roundings in each, as the lanes' maxima differ: the first writes them
+      store_own(dx + col.start, o, ragged ? col.dup : 0);
     }
   }
   leave_part<kBlock>(A, sum, rows);
@@ -264,11 +259,13 @@ __global__ void __launch_bounds__(kLongLossThreads) k_cross_entropy_long(LossArg
     for (int i = threadIdx.x; i < vectors; i += kLongLossThreads) {
       const Columns<V> col(i, A.classes);
       const Elems<T, V> e = *reinterpret_cast<const Elems<T, V>*>(x + col.start);
+      Elems<T, V> o;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float p = live ? exp_of(as_float(e.v[j]) - base) * f : 0.f;
-        if (j >= col.dup) dx[col.start + j] = from_float<T>(p - (col.start + j == y ? c : 0.f));
+        o.v[j] = from_float<T>(p - (col.start + j == y ? c : 0.f));
       }
+      store_own(dx + col.start, o, col.dup);
     }
   }
   leave_part<kLongLossThreads>(A, sum, rows);

@@ -108,14 +108,7 @@ template <int V>
 __device__ __forceinline__ void store_bytes(const RmsArgs& A, int64_t row, const Columns<V>& c, int index, const float (&y)[V], ByteScale s, int group_lanes) {
   if (c.dup == V) return;
   const Elems<uint8_t, V> o = to_bytes<V>(y, s.inverse, A.e4m3 != 0);
-  uint8_t* to = static_cast<uint8_t*>(A.y) + row * A.y_stride + c.start;
-  if (c.dup == 0) {
-    *reinterpret_cast<Elems<uint8_t, V>*>(to) = o;
-  } else {
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (j >= c.dup) to[j] = o.v[j];
-  }
+  store_own(static_cast<uint8_t*>(A.y) + row * A.y_stride + c.start, o, c.dup);
   if (index % group_lanes == 0) A.scales[row * A.scales_stride + index / group_lanes] = s.scale;
 }
 
@@ -248,12 +241,13 @@ __global__ void __launch_bounds__(kThreads) k_rms_norm_long(RmsArgs A) {
     const Columns<V> c(i, A.dim);
     float v[V];
     values(c, false, v);
+    Elems<T, V> o;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      if (j < c.dup) continue;
-      s += static_cast<double>(v[j]) * v[j];
-      if (total) total[c.start + j] = from_float<T>(v[j]);
+      s += j >= c.dup ? static_cast<double>(v[j]) * v[j] : 0.0;
+      o.v[j] = from_float<T>(v[j]);
     }
+    if (total) store_own(total + c.start, o, c.dup);
   }
   const float r = 1.f / sqrtf(static_cast<float>(group_sum<kThreads>(s, lds) / A.dim) + A.eps);
   if (threadIdx.x == 0 && A.rstd) A.rstd[row] = r;
@@ -291,9 +285,10 @@ __global__ void __launch_bounds__(kThreads) k_rms_norm_long(RmsArgs A) {
       store_bytes<V>(A, row, c, i, v, scale, A.group == 0 ? 1 << 30 : A.group / V);
     } else {
       T* y = static_cast<T*>(A.y) + row * A.y_stride;
+      Elems<T, V> o;
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (j >= c.dup) y[c.start + j] = from_float<T>(v[j]);
+      for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(v[j]);
+      store_own(y + c.start, o, c.dup);
     }
   }
 }
@@ -461,9 +456,10 @@ __global__ void __launch_bounds__(kThreads) k_rms_norm_grad_long(RmsGradArgs A) 
     if (dt) ed = *reinterpret_cast<const Elems<T, V>*>(dt + c.start);
     float w[V];
     load_params<T, V>(A.w, A.float_params != 0, c.start, 1.f, w);
+    Elems<T, V> o;
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (j >= c.dup) dx[c.start + j] = from_float<T>(r * (as_float(ey.v[j]) * w[j] - as_float(et.v[j]) * r * c2) + (dt ? as_float(ed.v[j]) : 0.f));
+    for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(r * (as_float(ey.v[j]) * w[j] - as_float(et.v[j]) * r * c2) + (dt ? as_float(ed.v[j]) : 0.f));
+    store_own(dx + c.start, o, c.dup);
   }
 }
 
