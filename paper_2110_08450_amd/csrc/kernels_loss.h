@@ -30,11 +30,12 @@ struct LossArgs {
   float* loss;
   LossPart* part;
   int32_t parts;
-  int64_t* counts;  // rows with a label among each kCountRows of them
+  int64_t* counts;  // rows with a label among each count_rows of them
   int32_t num_counts;  // 0: every block counts them itself
+  int64_t count_rows;
 };
 
-constexpr int kCountRows = 8192;
+constexpr int kCountAll = 8192;  // up to so many rows every block counts all labels itself
 constexpr float kLog2E = 1.44269504088896340736f;
 
 __device__ __forceinline__ int64_t label_of(const LossArgs& A, int64_t row) {
@@ -46,13 +47,14 @@ __device__ __forceinline__ bool is_class(int64_t label, int32_t classes) { retur
 template <int THREADS>
 __device__ __forceinline__ int64_t count_labels(const LossArgs& A, int64_t from, int64_t to, int64_t* lds) {
   int s = 0;
+#pragma unroll 4
   for (int64_t i = from + threadIdx.x; i < to; i += THREADS) s += is_class(label_of(A, i), A.classes);
   return group_sum<THREADS>(static_cast<int64_t>(s), lds);
 }
-static __global__ void __launch_bounds__(1024) k_loss_count(LossArgs A) {
-  __shared__ int64_t lds[16];
-  const int64_t n = count_of(A.num, A.max_rows), from = static_cast<int64_t>(blockIdx.x) * kCountRows, to = from + kCountRows;
-  const int64_t s = count_labels<1024>(A, from, to < n ? to : n, lds);
+static __global__ void __launch_bounds__(kThreads) k_loss_count(LossArgs A) {
+  __shared__ int64_t lds[kThreads / 64];
+  const int64_t n = count_of(A.num, A.max_rows), from = static_cast<int64_t>(blockIdx.x) * A.count_rows, to = from + A.count_rows;
+  const int64_t s = count_labels<kThreads>(A, from, to < n ? to : n, lds);
   if (threadIdx.x == 0) A.counts[blockIdx.x] = s;
 }
 
@@ -82,13 +84,8 @@ struct SoftSum {
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
 template <int LANES>
 __device__ __forceinline__ SoftSum wave_soft_sum(SoftSum a) {
-  float m = a.m;
-#pragma unroll
-  for (int o = 1; o < LANES; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  float s = a.s * exp_of(a.m - base_of(m));
-#pragma unroll
-  for (int o = 1; o < LANES; o <<= 1) s += __shfl_xor(s, o, 64);
-  return {m, s};
+  const float m = lanes_all<LANES>(a.m, max_f);
+  return {m, lanes_all<LANES>(a.s * exp_of(a.m - base_of(m)), sum_f)};
 }
 template <int LANES>
 __device__ __forceinline__ SoftSum group_soft_sum(SoftSum a, SoftSum* lds) {
@@ -115,8 +112,9 @@ __device__ __forceinline__ void leave_part(const LossArgs& A, double sum, int ro
 
 constexpr int loss_threads(int lanes) { return lanes > kThreads ? lanes : kThreads; }
 
-// A group of LANES lanes has a row in its registers, NV vectors of V columns a lane: read once, its exponentials kept until their sum is known, and asks for
-// its next row while it works on it.  The lane that has the label's column works out the loss.
+// A group of LANES lanes has a row in its registers, NV vectors of V columns a lane: it reads it once, keeps the exponentials until their sum is known, and has its
+// next row on its way meanwhile.  The lane that has the label's column works out the loss.
+// The gradient goes past the caches, and so do logits of long rows.
 template <typename T, int V, int NV, int LANES>
 __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs A) {
   constexpr int kBlock = loss_threads(LANES), kGroups = kBlock / LANES;
@@ -124,19 +122,24 @@ __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs 
   __shared__ int64_t count_lds[kBlock / 64];
   const int lane = threadIdx.x % LANES;
   const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
-  int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES;
+  // rows of a wave or more are the same for its lanes: addresses of scalars then
+  const int group = static_cast<int>(threadIdx.x) / LANES;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + (LANES >= 64 ? __builtin_amdgcn_readfirstlane(group) : group);
   const bool ragged = A.classes % V != 0;
   const T* const x = static_cast<const T*>(A.x);
-  Elems<T, V> e[NV];
+  Words<T, V> e[NV];
   int64_t label = 0;
+  const auto columns = [&](int k) { return columns_of<V, NV, LANES>(k, lane, A.classes); };
   const auto load = [&](int64_t i) {
     label = label_of(A, i);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) e[k] = *reinterpret_cast<const Elems<T, V>*>(x + i * A.x_stride + Columns<V>(k * LANES + lane, A.classes).start);
+    for (int k = 0; k < NV; ++k) e[k] = load_words<T, V, LANES == 1024>(x + i * A.x_stride + static_cast<unsigned>(columns(k).start));
   };
   load(row < A.max_rows ? row : A.max_rows - 1);
   const int64_t n = count_of(A.num, A.max_rows);
   const float c = gradient_scale<kBlock>(A, n, count_lds);
+  // Up to a wave the row's maximum is known to all lanes before the first exponential; beyond it each lane takes its own, so that one barrier does.
+  constexpr bool kCommon = LANES <= 64;
   double sum = 0.0;
   int rows = 0;
   for (int turn = 0; row < n; row += step, turn ^= 1) {
@@ -144,37 +147,42 @@ __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs 
     SoftSum a = {-__builtin_inff(), 0.f};
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[k][j] = as_float(e[k].v[j]);
       // columns that two vectors share do no harm to the maximum
 #pragma unroll
-      for (int j = 0; j < V; ++j) a.m = fmaxf(a.m, v[k][j]);
+      for (int j = 0; j < V; ++j) {
+        v[k][j] = e[k][j];
+        a.m = fmaxf(a.m, v[k][j]);
+      }
     }
     const bool live = is_class(label, A.classes);
     const int y = live ? static_cast<int>(label) : -1;
     if (row + step < n) load(row + step);
+    if constexpr (kCommon) a.m = lanes_all<LANES>(a.m, max_f);
     const float base = base_of(a.m);
     float xy = 0.f;
     bool owner = false;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const Columns<V> col(k * LANES + lane, A.classes);
+      float(&u)[V] = v[k];
+      const Columns<V> col = columns(k);
       const int at = y - col.start;
       if (static_cast<unsigned>(at) < static_cast<unsigned>(V) && at >= col.dup) {
         owner = true;
 #pragma unroll
-        for (int j = 0; j < V; ++j) xy = at == j ? v[k][j] : xy;
+        for (int j = 0; j < V; ++j) xy = at == j ? u[j] : xy;
       }
       float part = 0.f;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        v[k][j] = exp_of(v[k][j] - base);
+        u[j] = exp_of(u[j] - base);
         if (ragged && j < col.dup) continue;
-        part += v[k][j];
+        part += u[j];
       }
       a.s += col.dup < V ? part : 0.f;
     }
-    const SoftSum all = group_soft_sum<LANES>(a, lds[turn]);
+    SoftSum all = {a.m, 0.f};
+    if constexpr (kCommon) all.s = lanes_all<LANES>(a.s, sum_f);
+    else all = group_soft_sum<LANES>(a, lds[turn]);
     if (owner || (!live && lane == 0)) {
       const float loss = live ? logf(all.s) - (xy - base_of(all.m)) : 0.f;
       if (A.row_loss) A.row_loss[row] = loss;
@@ -182,34 +190,35 @@ __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs 
       rows += live;
     }
     if (!A.dx) continue;
-    const float f = exp_of(base - base_of(all.m)) * (c / all.s);
+    const float f = (kCommon ? 1.f : exp_of(base - base_of(all.m))) * (c / all.s);
     T* dx = static_cast<T*>(A.dx) + row * A.dx_stride;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const Columns<V> col(k * LANES + lane, A.classes);
-      if (col.dup == V) continue;
+      float(&u)[V] = v[k];
+      const Columns<V> col = columns(k);
       const int at = y - col.start;
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[k][j] = live ? v[k][j] * f : 0.f;
+      for (int j = 0; j < V; ++j) u[j] = live ? u[j] * f : 0.f;
       if (static_cast<unsigned>(at) < static_cast<unsigned>(V)) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[k][j] -= at == j ? c : 0.f;
+        for (int j = 0; j < V; ++j) u[j] -= at == j ? c : 0.f;
       }
       Elems<T, V> o;
 #pragma unroll
-      for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(v[k][j]);
-      // columns that two vectors share have other roundings in each, as the lanes' maxima differ: the first writes them
-      store_own(dx + col.start, o, ragged ? col.dup : 0);
+      for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(u[j]);
+      // columns that two vectors share have the same bits in both but where the lanes' maxima differ: there the first writes them
+      store_once(dx + static_cast<unsigned>(col.start), o, kCommon && col.dup < V ? 0 : col.dup);
     }
   }
   leave_part<kBlock>(A, sum, rows);
 }
 
-// Rows that outgrow the registers of a block: one to a block at a time, read twice.  A thread has the same columns both times and writes no others, so
-// that the gradient may take the place of the logits.
+// Rows that outgrow the registers of a block: one to a block at a time, read twice, four vectors of a thread at once.  A thread has the same columns both times and
+// writes no others, so that the gradient may take the place of the logits.
 constexpr int kLongLossThreads = 1024;
 template <typename T, int V>
 __global__ void __launch_bounds__(kLongLossThreads) k_cross_entropy_long(LossArgs A) {
+  constexpr int kTurns = 4;
   __shared__ SoftSum lds[2][kLongLossThreads / 64];
   __shared__ int64_t count_lds[kLongLossThreads / 64];
   const int64_t n = count_of(A.num, A.max_rows);
@@ -225,23 +234,30 @@ __global__ void __launch_bounds__(kLongLossThreads) k_cross_entropy_long(LossArg
     SoftSum a = {-__builtin_inff(), 0.f};
     float xy = 0.f;
     bool owner = false;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < vectors; i += kLongLossThreads) {
-      const Columns<V> col(i, A.classes);
-      const Elems<T, V> e = *reinterpret_cast<const Elems<T, V>*>(x + col.start);
+    for (int first = threadIdx.x; first < vectors; first += kTurns * kLongLossThreads) {
+      Words<T, V> e[kTurns];
+#pragma unroll
+      for (int k = 0; k < kTurns; ++k) e[k] = load_words<T, V, false>(x + static_cast<unsigned>(Columns<V>(first + k * kLongLossThreads, A.classes).start));
       float m = a.m;
 #pragma unroll
-      for (int j = 0; j < V; ++j) m = j >= col.dup ? fmaxf(m, as_float(e.v[j])) : m;
+      for (int k = 0; k < kTurns; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) m = fmaxf(m, e[k][j]);  // of columns of other threads as well, which does no harm
       const float base = base_of(m);
       a.s *= exp_of(a.m - base);
       a.m = m;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        if (j < col.dup) continue;
-        a.s += exp_of(as_float(e.v[j]) - base);
-        if (col.start + j == y) {
+      for (int k = 0; k < kTurns; ++k) {
+        const Columns<V> col(first + k * kLongLossThreads, A.classes);
+        float part = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) part += j >= col.dup ? exp_of(e[k][j] - base) : 0.f;
+        a.s += part;
+        const int at = y - col.start;
+        if (static_cast<unsigned>(at) < static_cast<unsigned>(V) && at >= col.dup) {
           owner = true;
-          xy = as_float(e.v[j]);
+#pragma unroll
+          for (int j = 0; j < V; ++j) xy = at == j ? e[k][j] : xy;
         }
       }
     }
@@ -255,34 +271,45 @@ __global__ void __launch_bounds__(kLongLossThreads) k_cross_entropy_long(LossArg
     if (!A.dx) continue;
     const float base = base_of(all.m), f = c / all.s;
     T* dx = static_cast<T*>(A.dx) + row * A.dx_stride;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < vectors; i += kLongLossThreads) {
-      const Columns<V> col(i, A.classes);
-      const Elems<T, V> e = *reinterpret_cast<const Elems<T, V>*>(x + col.start);
-      Elems<T, V> o;
+    for (int first = threadIdx.x; first < vectors; first += kTurns * kLongLossThreads) {
+      Words<T, V> e[kTurns];
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float p = live ? exp_of(as_float(e.v[j]) - base) * f : 0.f;
-        o.v[j] = from_float<T>(p - (col.start + j == y ? c : 0.f));
+      for (int k = 0; k < kTurns; ++k) e[k] = load_words<T, V, true>(x + static_cast<unsigned>(Columns<V>(first + k * kLongLossThreads, A.classes).start));
+#pragma unroll
+      for (int k = 0; k < kTurns; ++k) {
+        const Columns<V> col(first + k * kLongLossThreads, A.classes);
+        const int at = y - col.start;
+        float u[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) u[j] = live ? exp_of(e[k][j] - base) * f : 0.f;
+        if (static_cast<unsigned>(at) < static_cast<unsigned>(V)) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) u[j] -= at == j ? c : 0.f;
+        }
+        Elems<T, V> o;
+#pragma unroll
+        for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(u[j]);
+        store_once(dx + static_cast<unsigned>(col.start), o, col.dup);
       }
-      store_own(dx + col.start, o, col.dup);
     }
   }
   leave_part<kLongLossThreads>(A, sum, rows);
 }
 
 // The loss from the blocks' sums; of no rows with a label 0.
-static __global__ void __launch_bounds__(kThreads) k_loss_join(LossArgs A) {
-  __shared__ double sums[kThreads / 64];
-  __shared__ int64_t counts[kThreads / 64];
+constexpr int kLossJoinThreads = 1024;
+static __global__ void __launch_bounds__(kLossJoinThreads) k_loss_join(LossArgs A) {
+  __shared__ double sums[kLossJoinThreads / 64];
+  __shared__ int64_t counts[kLossJoinThreads / 64];
   double s = 0.0;
   int64_t rows = 0;
-  for (int i = threadIdx.x; i < A.parts; i += kThreads) {
+#pragma unroll 2
+  for (int i = threadIdx.x; i < A.parts; i += kLossJoinThreads) {
     s += A.part[i].sum;
     rows += A.part[i].rows;
   }
-  s = group_sum<kThreads>(s, sums);
-  rows = group_sum<kThreads>(rows, counts);
+  s = group_sum<kLossJoinThreads>(s, sums);
+  rows = group_sum<kLossJoinThreads>(rows, counts);
   if (threadIdx.x == 0) *A.loss = static_cast<float>(A.mean && rows > 0 ? s / static_cast<double>(rows) : s);
 }
 

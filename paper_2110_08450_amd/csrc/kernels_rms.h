@@ -36,25 +36,21 @@ struct RmsArgs {
 
 // Bits of a magnitude: as whole numbers they are in the order of the magnitudes, infinity and then NaN the largest, so that a maximum lets a NaN through.
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-__device__ __forceinline__ uint32_t max_u(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// Largest of groups of `lanes` lanes (1 to 32, a power of two), within the 16 of a row by register moves between lanes.
-template <int CONTROL>
-__device__ __forceinline__ uint32_t max_with(uint32_t x) {
-  return max_u(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), CONTROL, 15, 15, true)));
-}
+// Largest of groups of `lanes` lanes (1 to 32, a power of two).
 __device__ __forceinline__ uint32_t lanes_max(uint32_t x, int lanes) {
-  if (lanes > 1) x = max_with<0xb1>(x);   // the neighbour
-  if (lanes > 2) x = max_with<0x4e>(x);   // the other pair of four
-  if (lanes > 4) x = max_with<0x141>(x);  // the other four of eight, mirrored
-  if (lanes > 8) x = max_with<0x140>(x);  // the other eight of sixteen, mirrored
-  if (lanes > 16) x = max_u(x, static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), 16, 64)));
-  return x;
+  switch (lanes) {  // the same for all lanes
+    case 1: return x;
+    case 2: return lanes_all<2>(x, max_u);
+    case 4: return lanes_all<4>(x, max_u);
+    case 8: return lanes_all<8>(x, max_u);
+    case 16: return lanes_all<16>(x, max_u);
+    default: return lanes_all<32>(x, max_u);
+  }
 }
 template <int LANES>
 __device__ __forceinline__ uint32_t group_max(uint32_t x, uint32_t* lds) {
-  x = lanes_max(x, LANES < 32 ? LANES : 32);
-  if constexpr (LANES >= 64) x = max_u(x, static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), 32, 64)));
+  x = lanes_all<(LANES < 64 ? LANES : 64)>(x, max_u);
   if constexpr (LANES > 64) {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
@@ -128,22 +124,22 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_rms_norm(RmsArgs A) {
   float w[NV][V];
   const auto load = [&](int64_t i) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) e[k] = *reinterpret_cast<const Elems<T, V>*>(x + i * A.x_stride + Columns<V>(k * LANES + lane, A.dim).start);
+    for (int k = 0; k < NV; ++k) e[k] = *reinterpret_cast<const Elems<T, V>*>(x + i * A.x_stride + columns_of<V, NV, LANES>(k, lane, A.dim).start);
     if (res) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k) q[k] = *reinterpret_cast<const Elems<T, V>*>(res + i * A.residual_stride + Columns<V>(k * LANES + lane, A.dim).start);
+      for (int k = 0; k < NV; ++k) q[k] = *reinterpret_cast<const Elems<T, V>*>(res + i * A.residual_stride + columns_of<V, NV, LANES>(k, lane, A.dim).start);
     }
   };
   load(row < A.max_rows ? row : A.max_rows - 1);
 #pragma unroll
-  for (int k = 0; k < NV; ++k) load_params<T, V>(A.w, A.float_params != 0, Columns<V>(k * LANES + lane, A.dim).start, 1.f, w[k]);
+  for (int k = 0; k < NV; ++k) load_params<T, V>(A.w, A.float_params != 0, columns_of<V, NV, LANES>(k, lane, A.dim).start, 1.f, w[k]);
   const int64_t n = count_of(A.num, A.max_rows);
   for (int turn = 0; row < n; row += step, turn ^= 1) {
     float v[NV][V];
     float s = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const Columns<V> c(k * LANES + lane, A.dim);
+      const Columns<V> c = columns_of<V, NV, LANES>(k, lane, A.dim);
       float part = 0.f;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
@@ -154,14 +150,14 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_rms_norm(RmsArgs A) {
       s += c.dup < V ? part : 0.f;
     }
     if (row + step < n) load(row + step);
-    const float r = 1.f / sqrtf(group_sum<LANES>(s, lds[turn]) / static_cast<float>(A.dim) + A.eps);
+    const float r = 1.f / sqrtf(row_sum<LANES>(s, lds[turn]) / static_cast<float>(A.dim) + A.eps);
     if (lane == 0 && A.rstd) A.rstd[row] = r;
     // the sum: behind the barrier, as it may take the place of x or of the residual, which other lanes read as well
     if (A.total) {
       T* t = static_cast<T*>(A.total) + row * A.total_stride;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        const Columns<V> c(k * LANES + lane, A.dim);
+        const Columns<V> c = columns_of<V, NV, LANES>(k, lane, A.dim);
         if (c.dup == V) continue;
         Elems<T, V> o;
 #pragma unroll
@@ -177,7 +173,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_rms_norm(RmsArgs A) {
       uint32_t top[NV];
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        const Columns<V> c(k * LANES + lane, A.dim);
+        const Columns<V> c = columns_of<V, NV, LANES>(k, lane, A.dim);
         top[k] = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) top[k] = j >= c.dup ? max_u(top[k], magnitude(v[k][j])) : top[k];
@@ -196,12 +192,12 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_rms_norm(RmsArgs A) {
       }
 #pragma unroll
       for (int k = 0; k < NV; ++k)
-        store_bytes<V>(A, row, Columns<V>(k * LANES + lane, A.dim), k * LANES + lane, v[k], byte_scale(top[k], A.e4m3 != 0), lanes);
+        store_bytes<V>(A, row, columns_of<V, NV, LANES>(k, lane, A.dim), k * LANES + lane, v[k], byte_scale(top[k], A.e4m3 != 0), lanes);
     } else {
       T* y = static_cast<T*>(A.y) + row * A.y_stride;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        const Columns<V> c(k * LANES + lane, A.dim);
+        const Columns<V> c = columns_of<V, NV, LANES>(k, lane, A.dim);
         if (c.dup == V) continue;
         Elems<T, V> o;
 #pragma unroll
@@ -324,7 +320,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_rms_norm_grad(RmsGradAr
   float w[NV][V], dw[NV][V];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    load_params<T, V>(A.w, A.float_params != 0, Columns<V>(k * LANES + lane, A.dim).start, 1.f, w[k]);
+    load_params<T, V>(A.w, A.float_params != 0, columns_of<V, NV, LANES>(k, lane, A.dim).start, 1.f, w[k]);
 #pragma unroll
     for (int j = 0; j < V; ++j) dw[k][j] = 0.f;
   }
@@ -337,13 +333,13 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_rms_norm_grad(RmsGradAr
     r = A.rstd[row];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const Columns<V> c(k * LANES + lane, A.dim);
+      const Columns<V> c = columns_of<V, NV, LANES>(k, lane, A.dim);
       et[k] = *reinterpret_cast<const Elems<T, V>*>(t + row * A.t_stride + c.start);
       ey[k] = *reinterpret_cast<const Elems<T, V>*>(dy + row * A.dy_stride + c.start);
     }
     if (dt) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k) ed[k] = *reinterpret_cast<const Elems<T, V>*>(dt + row * A.dt_stride + Columns<V>(k * LANES + lane, A.dim).start);
+      for (int k = 0; k < NV; ++k) ed[k] = *reinterpret_cast<const Elems<T, V>*>(dt + row * A.dt_stride + columns_of<V, NV, LANES>(k, lane, A.dim).start);
     }
   };
   int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES;
@@ -353,7 +349,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_rms_norm_grad(RmsGradAr
     float s = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const Columns<V> c(k * LANES + lane, A.dim);
+      const Columns<V> c = columns_of<V, NV, LANES>(k, lane, A.dim);
       float part = 0.f;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
@@ -372,11 +368,11 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_rms_norm_grad(RmsGradAr
     const float scale = r;
     if (row + step < n) load(row + step);
     if (!A.dx) continue;
-    const float c2 = group_sum<LANES>(s, lds[turn]) * inv;
+    const float c2 = row_sum<LANES>(s, lds[turn]) * inv;
     T* dx = static_cast<T*>(A.dx) + row * A.dx_stride;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const Columns<V> c(k * LANES + lane, A.dim);
+      const Columns<V> c = columns_of<V, NV, LANES>(k, lane, A.dim);
       if (c.dup == V) continue;
       Elems<T, V> e;
 #pragma unroll
@@ -399,7 +395,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) k_rms_norm_grad(RmsGradAr
   if constexpr (LANES > 64) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const Columns<V> c(k * LANES + lane, A.dim);
+      const Columns<V> c = columns_of<V, NV, LANES>(k, lane, A.dim);
 #pragma unroll
       for (int j = 0; j < V; ++j)
         if (j >= c.dup) out[c.start + j] = dw[k][j];

@@ -13,16 +13,19 @@ namespace {
 
 using namespace smfg_dev;
 
-constexpr unsigned kLossBlocks = 2048, kLongLossBlocks = 512;
+constexpr unsigned kLossBlocks = 2048, kWideLossBlocks = 512, kLongLossBlocks = 256;  // at most
+constexpr int64_t kCounts = 512;
 
 // The blocks' sums, then the counts of labels.
 struct LossScratch {
-  int64_t counts, bytes;
+  int64_t counts, count_rows, bytes;
 };
 LossScratch loss_scratch(int64_t max_rows) {
   LossScratch S;
   S.counts = up256(kLossBlocks * static_cast<int64_t>(sizeof(LossPart)));
-  S.bytes = S.counts + up256(8 * ceil_div(max_rows, kCountRows));
+  S.count_rows = up256(ceil_div(max_rows, kCounts));
+  if (S.count_rows < 1024) S.count_rows = 1024;
+  S.bytes = S.counts + up256(8 * kCounts);
   return S;
 }
 
@@ -33,18 +36,36 @@ struct LaunchLoss {
   template <int V, int NV, int LANES>
   void operator()() const {
     constexpr int threads = loss_threads(LANES);
-    A.parts = static_cast<int32_t>(blocks_for(A.max_rows, threads / LANES, LANES == 1024 ? kLongLossBlocks : kLossBlocks));
+    A.parts = static_cast<int32_t>(blocks_for(A.max_rows, threads / LANES, LANES == 1024 ? kWideLossBlocks : kLossBlocks));
     go(k_cross_entropy<T, V, NV, LANES>, static_cast<unsigned>(A.parts), threads, A);
   }
 };
 
-// As with_row_shape; beyond 1536 vectors a row is that of 1024 lanes.
-template <typename T, typename F>
-bool with_loss_shape(int32_t classes, F f) {
+// How rows of `vectors` vectors are dealt.  Where a row is a wave's or less, up to four vectors a lane, as what a row takes besides its elements is shared by the rows
+// of a wave then, and no barrier is met (100 K rows of 512 halfs 41 us, with a vector a lane 51; 50 K of 700 floats 55, in blocks of 256 lanes 73); up to 16 vectors one a lane, whose
+// loads are next to each other (190 K rows of 47 floats 20.6, four lanes 41).
+template <typename T>
+bool launch_loss(LossArgs& A, Launches& go) {
   constexpr int V = kVec<T>;
-  if (with_row_shape<T, 1536>(classes, f)) return true;
-  const int64_t vectors = ceil_div(classes, V);
-  if (vectors <= 2048) f.template operator()<V, 2, 1024>();
+  const LaunchLoss<T> f{A, go};
+  const int64_t vectors = ceil_div(A.classes, V);
+  if (A.classes < V) f.template operator()<1, 1, V>();
+  else if (vectors <= 2) f.template operator()<V, 1, 2>();
+  else if (vectors <= 4) f.template operator()<V, 1, 4>();
+  else if (vectors <= 8) f.template operator()<V, 1, 8>();
+  else if (vectors <= 16) f.template operator()<V, 1, 16>();
+  else if (vectors <= 32) f.template operator()<V, 1, 32>();
+  else if (vectors <= 48) f.template operator()<V, 3, 16>();
+  else if (vectors <= 64) f.template operator()<V, 4, 16>();
+  else if (vectors <= 96) f.template operator()<V, 3, 32>();
+  else if (vectors <= 128) f.template operator()<V, 4, 32>();
+  else if (vectors <= 192) f.template operator()<V, 3, 64>();
+  else if (vectors <= 256) f.template operator()<V, 4, 64>();
+  else if (vectors <= 512) f.template operator()<V, 2, 256>();
+  else if (vectors <= 768) f.template operator()<V, 3, 256>();
+  else if (vectors <= 1024) f.template operator()<V, 2, 512>();
+  else if (vectors <= 1536) f.template operator()<V, 3, 512>();
+  else if (vectors <= 2048) f.template operator()<V, 2, 1024>();
   else if (vectors <= 3072) f.template operator()<V, 3, 1024>();
   else if (vectors <= 4096) f.template operator()<V, 4, 1024>();
   else if (vectors <= 5120) f.template operator()<V, 5, 1024>();
@@ -78,20 +99,20 @@ int smfg_cross_entropy(const void* d_logits, int64_t logits_stride, int32_t dtyp
   Launches go(hip_stream);
   uint8_t* scratch = static_cast<uint8_t*>(d_scratch);
   LossArgs A = {d_logits, logits_stride, d_labels, label_bytes, classes, d_num_rows, max_rows, reduction == SMFG_LOSS_MEAN, scale, d_dlogits, dlogits_stride,
-                d_row_loss, d_loss, reinterpret_cast<LossPart*>(scratch), 0, reinterpret_cast<int64_t*>(scratch + S.counts), 0};
+                d_row_loss, d_loss, reinterpret_cast<LossPart*>(scratch), 0, reinterpret_cast<int64_t*>(scratch + S.counts), 0, S.count_rows};
   if (max_rows > 0) {
-    if (A.mean && d_dlogits && max_rows > kCountRows) {
-      A.num_counts = static_cast<int32_t>(ceil_div(max_rows, kCountRows));
-      go(k_loss_count, static_cast<unsigned>(A.num_counts), 1024, A);
+    if (A.mean && d_dlogits && max_rows > kCountAll) {
+      A.num_counts = static_cast<int32_t>(ceil_div(max_rows, S.count_rows));
+      go(k_loss_count, static_cast<unsigned>(A.num_counts), kThreads, A);
     }
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
-      if (with_loss_shape<T>(classes, LaunchLoss<T>{A, go})) return;
+      if (launch_loss<T>(A, go)) return;
       A.parts = static_cast<int32_t>(blocks_for(max_rows, 1, kLongLossBlocks));
       go(k_cross_entropy_long<T, kVec<T>>, static_cast<unsigned>(A.parts), kLongLossThreads, A);
     });
   }
-  go(k_loss_join, 1, kThreads, A);
+  go(k_loss_join, 1, kLossJoinThreads, A);
   return go.result();
 }
 
