@@ -6,12 +6,14 @@ The nodes have no features; a table of floats, a row per node, is learned instea
   embedding            x = scale * table[node ids]
   layer_norm           z = norm(x)
   mean_aggregate       m = mean of z over each seed's neighbours
-                       logits = relu([z of the seeds | m] W1 + b1) W2 + b2, cross entropy        (torch)
+                       logits = relu([z of the seeds | m] W1 + b1) W2 + b2                       (torch)
+  cross_entropy        the loss and the logits' gradient
   embedding_grad       gradient of z: that of the seeds' own rows, and to it the share of every edge's source (accumulate)
   layer_norm_grad      gradients of x, weight and bias
   embedding_grad_rows  the touched rows of the table's gradient
   clip_grad_norm       all gradients together, the touched rows among them
-                       plain gradient descent
+                       plain gradient descent; or, with --adamw, the norm alone, and
+  adamw                all parameters, clipping on the way: of the table the touched rows, with states of 8 bits
 
 No size that depends on the batch leaves the GPU, so a step does not wait for it.
 
@@ -35,7 +37,7 @@ from paper_2110_08450_amd import synth  # noqa: E402
 
 class NodeEmbeddings:
     def __init__(self, g: smfg.Graph, batch_size: int, fanout: int, dim: int, hidden: int, classes: int, lr: float = 0.5,
-                 max_norm: float = 1.0, seed: int = 0):
+                 max_norm: float = 1.0, seed: int = 0, optimizer: str = "sgd"):
         dev = g.indptr.device
         gen = torch.Generator(device=dev).manual_seed(seed)
 
@@ -65,6 +67,19 @@ class NodeEmbeddings:
         self.ws_edges = smfg.embedding_grad_workspace(e, n, dim)
         self.ws_rows = smfg.embedding_grad_workspace(n, g.num_nodes, dim)
         self.all_grads = smfg.grad_list([self.rows] + self.grads, rows=[self.num_rows] + [None] * len(self.grads))
+        self.loss = torch.zeros(1, device=dev)
+        self.dlogits = torch.empty((batch_size, classes), device=dev)
+        self.ws_loss = smfg.cross_entropy_workspace(batch_size, classes)
+        assert optimizer in ("sgd", "adamw")
+        self.adamw, self.steps = None, 0
+        if optimizer == "adamw":
+            blocks = -(-dim // smfg.STATE_BLOCK)
+            m = [torch.zeros((g.num_nodes, dim), dtype=torch.int8, device=dev)] + [torch.zeros_like(p) for p in self.dense()]
+            v = [torch.zeros((g.num_nodes, dim), dtype=torch.uint8, device=dev)] + [torch.zeros_like(p) for p in self.dense()]
+            scales = [[torch.zeros((g.num_nodes, blocks), device=dev)] + [None] * len(self.grads) for _ in range(2)]
+            none = [None] * len(self.grads)
+            self.adamw = smfg.adamw_list([self.table] + self.dense(), [self.rows] + self.grads, m, v, *scales, rows=[self.num_rows] + none,
+                                         row_ids=[self.row_ids] + none, weight_decay=[0.0, 0.0, 0.0, 0.01, 0.0, 0.01, 0.0])
 
     def dense(self):
         return [self.weight, self.bias, self.w1, self.b1, self.w2, self.b2]
@@ -81,12 +96,8 @@ class NodeEmbeddings:
         smfg.mean_aggregate(indptr, indices, self.out.counts[0:1], s, self.z, self.m)
         h = torch.cat([self.z[:s], self.m[:s]], 1)
         a = torch.relu(h @ self.w1 + self.b1)
-        logp = torch.log_softmax(a @ self.w2 + self.b2, 1)
-        loss = -logp.gather(1, labels[:, None]).mean()
-
-        dlogits = logp.exp()
-        dlogits[torch.arange(s, device=seeds.device), labels] -= 1
-        dlogits /= s
+        logits, dlogits = a @ self.w2 + self.b2, self.dlogits[:s]
+        smfg.cross_entropy(logits, labels, self.out.counts[0:1], s, self.loss, self.ws_loss, grad_logits=dlogits)
         da = (dlogits @ self.w2.t()) * (a > 0)
         dh = da @ self.w1.t()
         gw, gb, gw1, gb1, gw2, gb2 = self.grads
@@ -103,10 +114,15 @@ class NodeEmbeddings:
         smfg.embedding_grad(indices, edges, self.e, share, self.dz, self.ws_edges, accumulate=True)
         smfg.layer_norm_grad(self.dz, self.x, nodes, self.n, self.weight, self.mean, self.rstd, self.dz, gw, gb, self.ws_norm)
         smfg.embedding_grad_rows(ids, nodes, self.n, self.dz, self.g.num_nodes, self.row_ids, self.num_rows, self.rows, self.ws_rows, scale=self.scale)
-        return loss
+        return self.loss[0].clone()
 
     def step(self, seeds: torch.Tensor, labels: torch.Tensor, rng_key: int) -> torch.Tensor:
         loss = self.gradients(seeds, labels, rng_key)
+        if self.adamw:
+            self.steps += 1
+            smfg.clip_grad_norm(self.all_grads, float("inf"), self.norm)
+            smfg.adamw(self.adamw, self.steps, self.lr, max_norm=self.max_norm, norm=self.norm)
+            return loss
         smfg.clip_grad_norm(self.all_grads, self.max_norm, self.norm)
         for p, g in zip(self.dense(), self.grads):
             p.sub_(g, alpha=self.lr)
@@ -115,7 +131,7 @@ class NodeEmbeddings:
         return loss
 
 
-def train(steps: int, dim: int = 64, hidden: int = 128, classes: int = 16, fanout: int = 10, report=None):
+def train(steps: int, dim: int = 64, hidden: int = 128, classes: int = 16, fanout: int = 10, report=None, optimizer: str = "sgd", lr: float = 0.5):
     """Trains on the seed batches of the smallest workload with random labels, which only a row per node can learn; the losses."""
     dev = "cuda:0"
     w = synth.WORKLOADS["tiny"]
@@ -123,7 +139,7 @@ def train(steps: int, dim: int = 64, hidden: int = 128, classes: int = 16, fanou
     g = smfg.graph_create(graph.indptr, graph.indices)
     batches = synth.make_seed_batches(w, device=dev)
     labels = torch.randint(0, classes, (w.num_nodes,), device=dev, generator=torch.Generator(device=dev).manual_seed(1))
-    model = NodeEmbeddings(g, w.batch_size, fanout, dim, hidden, classes)
+    model = NodeEmbeddings(g, w.batch_size, fanout, dim, hidden, classes, lr=lr, optimizer=optimizer)
     losses = []
     for i in range(steps):
         seeds = batches[i % len(batches)]
@@ -137,6 +153,7 @@ if __name__ == "__main__":
     p = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     p.add_argument("--steps", type=int, default=200)
     p.add_argument("--dim", type=int, default=64)
+    p.add_argument("--adamw", action="store_true")
     a = p.parse_args()
-    losses = train(a.steps, dim=a.dim, report=lambda s: print(s, flush=True))[1]
+    losses = train(a.steps, dim=a.dim, optimizer="adamw" if a.adamw else "sgd", lr=0.01 if a.adamw else 0.5, report=lambda s: print(s, flush=True))[1]
     print(f"loss {losses[0]:.4f} -> {losses[-1]:.4f}")

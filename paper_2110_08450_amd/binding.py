@@ -503,6 +503,16 @@ def _matrix(t: torch.Tensor, rows: int, name: str):
     return t.data_ptr(), stride if n > 1 else max(stride, dim), DTYPES[t.dtype]
 
 
+def _like(t: Optional[torch.Tensor], rows: int, dim: int, dtype, name: str):
+    """(address, row stride in elements) of a matrix with at least `rows` rows of `dim` columns, of a type; (None, 0) for none."""
+    if t is None:
+        return None, 0
+    n, d = t.shape
+    stride, step = t.stride()
+    assert t.dtype == dtype and d == dim and t.is_cuda and n >= rows and (step == 1 or d == 1), name
+    return t.data_ptr(), stride if n > 1 else max(stride, d)
+
+
 def _vector(t: Optional[torch.Tensor], n: int, dtype, name: str):
     if t is None:
         return None
@@ -651,28 +661,22 @@ def rms_norm(x: torch.Tensor, num_rows: torch.Tensor, max_rows: int, weight: Opt
     int64).  y of x's type, or int8 or float8_e4m3fn: then y stands for y * scales, scales (float32 [max_rows x groups]) one for each `group` columns
     (32, 64, 128; 0: a row).  weight float32 or of x's type, or None.  total may be None, x or residual; y may be x or residual.  rstd (float32
     [max_rows]) is what rms_norm_grad needs."""
-    assert x.dim() == 2 and y.dim() == 2 and x.shape[1] == y.shape[1]
-    dim = int(x.shape[1])
-    a, as_, at = _matrix(x, max_rows, "x")
-    r = t = s = None
-    rs = ts = ss = 0
-    if residual is not None:
-        assert residual.dim() == 2 and residual.shape[1] == dim and residual.dtype == x.dtype
-        r, rs, _ = _matrix(residual, max_rows, "residual")
-    if total is not None:
-        assert total.dim() == 2 and total.shape[1] == dim and total.dtype == x.dtype
-        t, ts, _ = _matrix(total, max_rows, "total")
-    if y.dtype in BYTE_DTYPES:
-        assert y.is_cuda and y.shape[0] >= max_rows and (y.stride(1) == 1 or dim == 1)
-        o, os_, ot = y.data_ptr(), y.stride(0) if y.shape[0] > 1 else max(y.stride(0), dim), BYTE_DTYPES[y.dtype]
-        assert scales is not None and scales.dim() == 2 and scales.dtype == torch.float32 and scales.shape[1] == (-(-dim // group) if group > 0 else 1)
-        s, ss, _ = _matrix(scales, max_rows, "scales")
+    dtype, dim = x.dtype, x.shape[1]
+    a, as_ = _like(x, max_rows, dim, dtype, "x")
+    r, rs = _like(residual, max_rows, dim, dtype, "residual")
+    t, ts = _like(total, max_rows, dim, dtype, "total")
+    if y.dtype == dtype:
+        assert scales is None, "scales"
+        o, os_ = _like(y, max_rows, dim, dtype, "y")
+        ot, s, ss = DTYPES[dtype], None, 0
     else:
-        assert y.dtype == x.dtype and scales is None
-        o, os_, ot = _matrix(y, max_rows, "y")
+        o, os_ = _like(y, max_rows, dim, y.dtype, "y")
+        ot = BYTE_DTYPES[y.dtype]
+        assert scales is not None, "scales"
+        s, ss = _like(scales, max_rows, -(-dim // group) if group > 0 else 1, torch.float32, "scales")
     pd = weight.dtype if weight is not None else torch.float32
     assert pd in DTYPES
-    rc = lib().smfg_rms_norm(a, as_, at, r, rs, t, ts, _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, dim, _vector(weight, dim, pd, "weight"),
+    rc = lib().smfg_rms_norm(a, as_, DTYPES[dtype], r, rs, t, ts, _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, dim, _vector(weight, dim, pd, "weight"),
                              DTYPES[pd], eps, o, os_, ot, s, ss, group, _vector(rstd, max_rows, torch.float32, "rstd"), _raw_stream(stream))
     _check(rc, "smfg_rms_norm")
 
@@ -688,21 +692,14 @@ def rms_norm_grad(grad_y: torch.Tensor, total: torch.Tensor, num_rows: torch.Ten
     """Gradients of rms_norm's input (and of its residual, which is the same) and weight; None where one is not wanted (without the latter, ws may be
     None).  total is the sum that was normed, or x; grad_total the gradient that reaches the sum from elsewhere, which is added.  grad_x is of x's type
     and may be grad_y, total or grad_total; grad_weight is of weight's type."""
-    assert total.dim() == 2 and grad_y.dim() == 2 and grad_y.shape[1] == total.shape[1] and grad_y.dtype == total.dtype
-    dim = int(total.shape[1])
-    d, ds, _ = _matrix(grad_y, max_rows, "grad_y")
-    a, as_, at = _matrix(total, max_rows, "total")
-    gx = gt = None
-    gs = gts = 0
-    if grad_x is not None:
-        assert grad_x.dim() == 2 and grad_x.shape[1] == dim and grad_x.dtype == total.dtype
-        gx, gs, _ = _matrix(grad_x, max_rows, "grad_x")
-    if grad_total is not None:
-        assert grad_total.dim() == 2 and grad_total.shape[1] == dim and grad_total.dtype == total.dtype
-        gt, gts, _ = _matrix(grad_total, max_rows, "grad_total")
+    dtype, dim = total.dtype, total.shape[1]
+    d, ds = _like(grad_y, max_rows, dim, dtype, "grad_y")
+    a, as_ = _like(total, max_rows, dim, dtype, "total")
+    gx, gs = _like(grad_x, max_rows, dim, dtype, "grad_x")
+    gt, gts = _like(grad_total, max_rows, dim, dtype, "grad_total")
     pd = next((t.dtype for t in (weight, grad_weight) if t is not None), torch.float32)
     assert pd in DTYPES
-    rc = lib().smfg_rms_norm_grad(d, ds, a, as_, at, gt, gts, _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, dim,
+    rc = lib().smfg_rms_norm_grad(d, ds, a, as_, DTYPES[dtype], gt, gts, _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, dim,
                                   _vector(weight, dim, pd, "weight"), DTYPES[pd], _vector(rstd, max_rows, torch.float32, "rstd"), gx, gs,
                                   _vector(grad_weight, dim, pd, "grad_weight"), ws.on(stream) if ws is not None else None,
                                   ws.nbytes if ws is not None else 0, _raw_stream(stream))
@@ -723,14 +720,12 @@ def cross_entropy(logits: torch.Tensor, labels: torch.Tensor, num_rows: torch.Te
     """loss (float32, one element) = mean or sum over rows i < num_rows (device int64) of log(sum(exp(logits[i]))) - logits[i, labels[i]]; grad_logits
     (of logits' type; may be logits) = its gradient times scale; row_loss (float32 [max_rows]) the rows' own.  A row whose label (int32 or int64) is
     no class does not count: loss 0, gradient zeros."""
-    assert logits.dim() == 2 and labels.dtype in (torch.int32, torch.int64)
-    x, xs, xt = _matrix(logits, max_rows, "logits")
-    g, gs = None, 0
-    if grad_logits is not None:
-        assert grad_logits.dim() == 2 and grad_logits.shape[1] == logits.shape[1] and grad_logits.dtype == logits.dtype
-        g, gs, _ = _matrix(grad_logits, max_rows, "grad_logits")
-    rc = lib().smfg_cross_entropy(x, xs, xt, _vector(labels, max_rows, labels.dtype, "labels"), labels.element_size(),
-                                  _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, logits.shape[1], REDUCTIONS[reduction], scale,
+    assert labels.dtype in (torch.int32, torch.int64)
+    dtype, classes = logits.dtype, logits.shape[1]
+    x, xs = _like(logits, max_rows, classes, dtype, "logits")
+    g, gs = _like(grad_logits, max_rows, classes, dtype, "grad_logits")
+    rc = lib().smfg_cross_entropy(x, xs, DTYPES[dtype], _vector(labels, max_rows, labels.dtype, "labels"), labels.element_size(),
+                                  _vector(num_rows, 1, torch.int64, "num_rows"), max_rows, classes, REDUCTIONS[reduction], scale,
                                   _vector(loss, 1, torch.float32, "loss"), _vector(row_loss, max_rows, torch.float32, "row_loss"), g, gs,
                                   ws.on(stream), ws.nbytes, _raw_stream(stream))
     _check(rc, "smfg_cross_entropy")
