@@ -441,9 +441,10 @@ int smfg_clip_grad_norm(const smfg_grad_t *grads /* host */, int32_t num_grads, 
 /*
  * One step of AdamW over any number of tensors, in place:
  *   g' = f g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
- *   p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),  f = scale min(1, max_norm / (norm + 1e-6))
- * With d_norm (the norm of smfg_clip_grad_norm, called with an infinite max_norm and no outputs) gradients are clipped here, and not written; where
- * *d_norm is not finite the step is not taken: nothing is written.  Without it f = scale.
+ *   p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),  
+ *   f = scale min(1, max_norm / (|scale| norm + 1e-6))
+ * With d_norm, the norm of the gradients as they are (smfg_clip_grad_norm with scale 1, an infinite max_norm and no outputs finds it and writes nothing else),
+ * they are clipped here, and not written; where *d_norm is not finite the step is not taken: nothing is written.  Without it f = scale.
  * No two of the buffers written to share memory.
  * A tensor is of rows of row_elems elements (0: a single row of numel).  With d_row_ids the gradient's row i is that of row d_row_ids[i] of a table of
  * num_rows rows (param, m, v and copy), whose other rows are left as they are: the touched rows that smfg_embedding_grad_rows tells.  These ids are
@@ -451,7 +452,7 @@ int smfg_clip_grad_norm(const smfg_grad_t *grads /* host */, int32_t num_grads, 
  * m and v are of float (state_bits 32), or of 8 bits: every SMFG_STATE_BLOCK consecutive elements of a row (the last of a row may be fewer) share two floats,
  * A in m_scale and B in v_scale, of ceil(row_elems / SMFG_STATE_BLOCK) a row, and
  *   m = A (k / 127) |k / 127| with k int8,  v = (B (k / 255)^2)^2 with k uint8
- * are what is next to the value in k, A and B being the largest |m| and sqrt(v) of the elements; v > 0 is kept as k >= 1.  A below 2^-100 counts as 0.
+ * are what is next to the value in k, A and B being the largest |m| and sqrt(v) of the elements; v > 0 is kept as k >= 1.  A below 2^-100 counts as 0, and v below 2^-126.
  * An infinity or a NaN in m or v makes the kept state of its block NaN.  Zeroed memory is the state of zeros, of either kind.  The step itself uses m
  * and v before they are rounded.
  */
@@ -471,7 +472,7 @@ typedef struct {
   int64_t num_rows;      /* of the table, with d_row_ids */
 } smfg_param_t;
 typedef struct {
-  double lr, beta1, beta2, eps; /* beta1, beta2 in [0, 1), eps >= 0 */
+  double lr, beta1, beta2, eps; /* beta1, beta2 in [0, 1), eps >= 2^-126 */
   double scale, max_norm;       /* max_norm > 0 */
   int64_t step;                 /* t = step + *d_step, 1 in the first step */
   const int64_t *d_step;        /* device, or NULL (0): for graphs, in which step is what it was when they were captured */

@@ -13,6 +13,7 @@ namespace {
 
 using namespace smfg_dev;
 static_assert(kStateBlock == SMFG_STATE_BLOCK, "blocks of the states");
+constexpr double kLeastNormal = 0x1p-126;  // of floats
 
 bool bad_param(const smfg_param_t& p) {
   if (p.numel < 0 || p.numel >= (int64_t(1) << 48) || type_bytes(p.param_dtype) == 0 || type_bytes(p.grad_dtype) == 0) return true;
@@ -75,7 +76,7 @@ int smfg_adamw(const smfg_param_t* params, int32_t num_params, const smfg_adamw_
   if ((num_params > 0 && !params) || !hyper) return SMFG_ERR_NULL_PTR;
   const smfg_adamw_t& h = *hyper;
   if (num_params < 0 || bad_params(params, num_params) || !std::isfinite(h.lr) || !(h.beta1 >= 0.0 && h.beta1 < 1.0) || !(h.beta2 >= 0.0 && h.beta2 < 1.0) ||
-      !(h.eps >= 0.0) || !std::isfinite(h.eps) || !std::isfinite(h.scale) || !(h.max_norm > 0.0) || h.step < (h.d_step ? 0 : 1) || h.step >= (int64_t(1) << 48) ||
+      !(h.eps >= kLeastNormal) || !std::isfinite(static_cast<float>(h.eps)) || !std::isfinite(h.scale) || !(h.max_norm > 0.0) || h.step < (h.d_step ? 0 : 1) || h.step >= (int64_t(1) << 48) ||
       misaligned(h.d_step, 8) || misaligned(h.d_lr, 4) || misaligned(h.d_norm, 4))
     return SMFG_ERR_INVALID_ARG;
   for (int i = 0; i < num_params; ++i)

@@ -1,7 +1,7 @@
 // libsmfg AdamW over many tensors, or over the touched rows of tables, with states of floats or of 8 bits.
 //
 //   g' = f g,  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,
-//   p = p - lr decay p - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps),   f = scale min(1, max_norm / (norm + 1e-6))
+//   p = p - lr decay p - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps),   f = scale min(1, max_norm / (|scale| norm + 1e-6))
 //
 // States of 8 bits: blocks of kStateBlock consecutive elements share two floats, A = max |m| and B = max sqrt(v), and an element has
 //   m = A sgn(k) (k / 127)^2, k = rint(127 sqrt(|m| / A)) with m's sign;   sqrt(v) = B (k / 255)^2, k = rint(255 sqrt(sqrt(v) / B)), at least 1 if v > 0.
@@ -83,7 +83,7 @@ __device__ __forceinline__ AdamStep adam_step(const AdamArgs& A) {
   S.root_b2 = A.root_b2;
   double f = A.scale;
   if (A.norm) {
-    const double c = A.max_norm / (static_cast<double>(*A.norm) + 1e-6);
+    const double c = A.max_norm / (fabs(A.scale) * static_cast<double>(*A.norm) + 1e-6);
     if (c < 1.0) f *= c;
   }
   S.power = 0;

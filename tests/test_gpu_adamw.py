@@ -178,7 +178,7 @@ def test_clipping_by_a_norm_at_hand(norm, max_norm, scale):
         before = (t.p.clone(), t.state(), t.g.clone())
         n = torch.tensor([norm], device=DEV)
         run([t], step=5, norm=n, max_norm=max_norm, scale=scale)
-        check_step(t, before, 5, scale * min(1.0, max_norm / (float(n) + 1e-6)), WD)
+        check_step(t, before, 5, scale * min(1.0, max_norm / (scale * float(n) + 1e-6)), WD)
 
 
 def test_factors_below_a_floats_range():
@@ -219,6 +219,25 @@ def test_infinite_and_nan_gradients(bytes_):
         smfg.adamw_values(t.v, t.vs, v)
         for x in (m, v):
             assert x[128:256].isnan().all() and x[640:768].isnan().all() and bool(x[:128].isfinite().all()) and bool(x[768:].isfinite().all())
+
+
+def test_nothing_to_step():
+    smfg.adamw(smfg.adamw_list([], [], [], []), 1, LR)
+    e = [torch.zeros(0, device=DEV) for _ in range(4)]
+    smfg.adamw(smfg.adamw_list([e[0]], [e[1]], [e[2]], [e[3]]), 1, LR)
+
+
+def test_a_loss_scale_is_undone_with_the_norm_of_the_scaled_gradients():
+    """Gradients 1024 times as large, their norm, and a scale of 1 / 1024: the step of the gradients themselves, bit for bit, as powers of two are exact."""
+    a, b = Tensor((3000,), F32, F32, None, False, 2), Tensor((3000,), F32, F32, None, False, 2)
+    b.g.mul_(1024)
+    norm = torch.zeros(1, device=DEV)
+    for t, scale in ((a, 1.0), (b, 1 / 1024)):
+        before = t.g.clone()
+        smfg.clip_grad_norm(smfg.grad_list([t.g]), float("inf"), norm)
+        assert torch.equal(t.g, before)
+        run([t], step=2, norm=norm, max_norm=0.5, scale=scale)
+    assert torch.equal(a.p, b.p) and torch.equal(a.m, b.m) and torch.equal(a.v, b.v)
 
 
 def test_zeros():

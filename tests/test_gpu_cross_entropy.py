@@ -186,6 +186,14 @@ def test_counts_are_held_to_the_launch(n, max_rows):
         check(loss, want.mean()[None], ((tol_row + 3 * U * want.abs()).mean())[None])
 
 
+def test_no_rows_at_all():
+    x, y = torch.zeros((0, 7), device=DEV), torch.zeros(0, dtype=torch.int64, device=DEV)
+    for reduction in ("mean", "sum"):
+        loss = torch.full((1,), 9.0, device=DEV)
+        smfg.cross_entropy(x, y, count(0), 0, loss, smfg.cross_entropy_workspace(0, 7), grad_logits=x, reduction=reduction)
+        assert loss == 0
+
+
 def test_rows_2_31_elements_apart():
     n, classes, apart = 3, 72, 2 ** 31 + 8
     buf = torch.empty((n - 1) * apart + classes, dtype=F16, device=DEV)

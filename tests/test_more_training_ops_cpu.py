@@ -104,7 +104,7 @@ def test_adamw_refusals():
     assert L.smfg_adamw(None, 1, hyper(), None) == NULL and L.smfg_adamw(param(), 1, None, None) == NULL
     assert L.smfg_adamw(param(), -1, hyper(), None) == ARG
     inf, nan = float("inf"), float("nan")
-    for bad in (dict(lr=nan), dict(lr=inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta1=nan), dict(beta2=1.0), dict(beta2=-1e-9), dict(eps=-1e-9), dict(eps=inf),
+    for bad in (dict(lr=nan), dict(lr=inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta1=nan), dict(beta2=1.0), dict(beta2=-1e-9), dict(eps=-1e-9), dict(eps=0.0), dict(eps=1e-39), dict(eps=1e39), dict(eps=inf),
                 dict(eps=nan), dict(scale=inf), dict(scale=nan), dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=nan), dict(step=0), dict(step=-1),
                 dict(step=1 << 48), dict(step=-1, d_step=P), dict(d_step=P + 4), dict(d_lr=P + 2), dict(d_norm=P + 1)):
         assert adamw(hyper(**bad)) == ARG, bad
