@@ -99,7 +99,11 @@ __device__ __forceinline__ SoftSum group_soft_sum(SoftSum a, SoftSum* lds) {
   return a;
 }
 
-// The block's sums of its threads' losses.
+// The loss from the sum of the rows'; of no rows with a label 0.
+__device__ __forceinline__ float loss_of(const LossArgs& A, double sum, int64_t rows) {
+  return static_cast<float>(A.mean && rows > 0 ? sum / static_cast<double>(rows) : sum);
+}
+// The block's sums of its threads' losses, or the loss if there is no other block.
 template <int THREADS>
 __device__ __forceinline__ void leave_part(const LossArgs& A, double sum, int rows) {
   __shared__ double sums[THREADS / 64];
@@ -107,7 +111,9 @@ __device__ __forceinline__ void leave_part(const LossArgs& A, double sum, int ro
   __syncthreads();
   sum = group_sum<THREADS>(sum, sums);
   const int64_t all = group_sum<THREADS>(static_cast<int64_t>(rows), counts);
-  if (threadIdx.x == 0) A.part[blockIdx.x] = {sum, all};
+  if (threadIdx.x != 0) return;
+  if (gridDim.x == 1) *A.loss = loss_of(A, sum, all);
+  else A.part[blockIdx.x] = {sum, all};
 }
 
 constexpr int loss_threads(int lanes) { return lanes > kThreads ? lanes : kThreads; }
@@ -296,7 +302,7 @@ __global__ void __launch_bounds__(kLongLossThreads) k_cross_entropy_long(LossArg
   leave_part<kLongLossThreads>(A, sum, rows);
 }
 
-// The loss from the blocks' sums; of no rows with a label 0.
+// The loss from the blocks' sums.
 constexpr int kLossJoinThreads = 1024;
 static __global__ void __launch_bounds__(kLossJoinThreads) k_loss_join(LossArgs A) {
   __shared__ double sums[kLossJoinThreads / 64];
@@ -310,7 +316,7 @@ static __global__ void __launch_bounds__(kLossJoinThreads) k_loss_join(LossArgs 
   }
   s = group_sum<kLossJoinThreads>(s, sums);
   rows = group_sum<kLossJoinThreads>(rows, counts);
-  if (threadIdx.x == 0) *A.loss = static_cast<float>(A.mean && rows > 0 ? s / static_cast<double>(rows) : s);
+  if (threadIdx.x == 0) *A.loss = loss_of(A, s, rows);
 }
 
 }  // namespace smfg_dev
