@@ -52,6 +52,7 @@ inline int64_t items_of(const smfg_param_t& p) {
 // more to work out before they begin.  More, up to 512, where there would be over 2^20 blocks.
 struct AdamShape {
   int64_t blocks[2];  // for states of floats, of 8 bits
+  bool keep;          // parameters and copies are few enough to be kept for the next pass
   uint32_t units[2];
 };
 inline int64_t blocks_of(const smfg_param_t& p, const AdamShape& S) {
@@ -59,9 +60,13 @@ inline int64_t blocks_of(const smfg_param_t& p, const AdamShape& S) {
   return ceil_div(items_of(p), p.state_bits == 8 ? S.units[1] * adam_bytes_wide(pb, gb, cols_of(p)) : S.units[0] * (kStateBlock / kAdamFloats));
 }
 AdamShape adam_shape(const smfg_param_t* p, int32_t n) {
-  AdamShape S = {{0, 0}, {8, 16}};
-  double all[2] = {0, 0};
-  for (int i = 0; i < n; ++i) all[p[i].state_bits == 8] += static_cast<double>(p[i].numel) / kStateBlock;
+  AdamShape S = {{0, 0}, true, {8, 16}};
+  double all[2] = {0, 0}, bytes = 0;
+  for (int i = 0; i < n; ++i) {
+    all[p[i].state_bits == 8] += static_cast<double>(p[i].numel) / kStateBlock;
+    bytes += static_cast<double>(p[i].numel) * static_cast<double>(type_bytes(p[i].param_dtype) + (p[i].copy ? 2 : 0));
+  }
+  S.keep = bytes <= kKeptBytes;
   for (int k = 0; k < 2; ++k)
     while (S.units[k] < 512 && all[k] > 1048576.0 * S.units[k]) S.units[k] *= 2;
   for (int i = 0; i < n; ++i) S.blocks[p[i].state_bits == 8] += blocks_of(p[i], S);
@@ -86,6 +91,7 @@ int smfg_adamw(const smfg_param_t* params, int32_t num_params, const smfg_adamw_
   Launches go(hip_stream);
   AdamArgs A;
   A.first_block = 0;
+  A.keep = S.keep;
   A.lr = static_cast<float>(h.lr);
   A.b1 = static_cast<float>(h.beta1);
   A.b2 = static_cast<float>(h.beta2);

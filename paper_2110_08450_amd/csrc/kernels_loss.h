@@ -33,6 +33,7 @@ struct LossArgs {
   int64_t* counts;  // rows with a label among each count_rows of them
   int32_t num_counts;  // 0: every block counts them itself
   int64_t count_rows;
+  int32_t keep;  // the gradient stays in the caches
 };
 
 constexpr int kCountAll = 8192;  // up to so many rows every block counts all labels itself
@@ -120,7 +121,7 @@ constexpr int loss_threads(int lanes) { return lanes > kThreads ? lanes : kThrea
 
 // A group of LANES lanes has a row in its registers, NV vectors of V columns a lane: it reads it once, keeps the exponentials until their sum is known, and has its
 // next row on its way meanwhile.  The lane that has the label's column works out the loss.
-// The gradient goes past the caches, and so do logits of long rows.
+// Logits of long rows are read past the caches (8192 rows of 32 000 bfloat16 194 -> 184 us).
 template <typename T, int V, int NV, int LANES>
 __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs A) {
   constexpr int kBlock = loss_threads(LANES), kGroups = kBlock / LANES;
@@ -213,7 +214,9 @@ __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs 
 #pragma unroll
       for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(u[j]);
       // columns that two vectors share have the same bits in both but where the lanes' maxima differ: there the first writes them
-      store_once(dx + static_cast<unsigned>(col.start), o, kCommon && col.dup < V ? 0 : col.dup);
+      const int shared = kCommon && col.dup < V ? 0 : col.dup;
+      if (A.keep) store_own(dx + static_cast<unsigned>(col.start), o, shared);
+      else store_once(dx + static_cast<unsigned>(col.start), o, shared);
     }
   }
   leave_part<kBlock>(A, sum, rows);
@@ -295,7 +298,8 @@ __global__ void __launch_bounds__(kLongLossThreads) k_cross_entropy_long(LossArg
         Elems<T, V> o;
 #pragma unroll
         for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(u[j]);
-        store_once(dx + static_cast<unsigned>(col.start), o, col.dup);
+        if (A.keep) store_own(dx + static_cast<unsigned>(col.start), o, col.dup);
+        else store_once(dx + static_cast<unsigned>(col.start), o, col.dup);
       }
     }
   }

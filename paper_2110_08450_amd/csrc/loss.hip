@@ -102,7 +102,8 @@ int smfg_cross_entropy(const void* d_logits, int64_t logits_stride, int32_t dtyp
   Launches go(hip_stream);
   uint8_t* scratch = static_cast<uint8_t*>(d_scratch);
   LossArgs A = {d_logits, logits_stride, d_labels, label_bytes, classes, d_num_rows, max_rows, reduction == SMFG_LOSS_MEAN, scale, d_dlogits, dlogits_stride,
-                d_row_loss, d_loss, reinterpret_cast<LossPart*>(scratch), 0, reinterpret_cast<int64_t*>(scratch + S.counts), 0, S.count_rows};
+                d_row_loss, d_loss, reinterpret_cast<LossPart*>(scratch), 0, reinterpret_cast<int64_t*>(scratch + S.counts), 0, S.count_rows,
+                static_cast<double>(max_rows) * classes * static_cast<double>(type_bytes(dtype)) <= kKeptBytes};
   if (max_rows > 0) {
     if (A.mean && d_dlogits && max_rows > kCountAll) {
       A.num_counts = static_cast<int32_t>(ceil_div(max_rows, S.count_rows));
