@@ -5,6 +5,8 @@
 #ifndef SMFG_KERNELS_LOSS_H_
 #define SMFG_KERNELS_LOSS_H_
 
+#include <type_traits>
+
 #include "elements.h"
 
 namespace smfg_dev {
@@ -199,25 +201,29 @@ __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs 
     if (!A.dx) continue;
     const float f = (kCommon ? 1.f : exp_of(base - base_of(all.m))) * (c / all.s);
     T* dx = static_cast<T*>(A.dx) + row * A.dx_stride;
+    const auto leave = [&](auto keep) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      float(&u)[V] = v[k];
-      const Columns<V> col = columns(k);
-      const int at = y - col.start;
+      for (int k = 0; k < NV; ++k) {
+        float(&u)[V] = v[k];
+        const Columns<V> col = columns(k);
+        const int at = y - col.start;
 #pragma unroll
-      for (int j = 0; j < V; ++j) u[j] = live ? u[j] * f : 0.f;
-      if (static_cast<unsigned>(at) < static_cast<unsigned>(V)) {
+        for (int j = 0; j < V; ++j) u[j] = live ? u[j] * f : 0.f;
+        if (static_cast<unsigned>(at) < static_cast<unsigned>(V)) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) u[j] -= at == j ? c : 0.f;
+          for (int j = 0; j < V; ++j) u[j] -= at == j ? c : 0.f;
+        }
+        Elems<T, V> o;
+#pragma unroll
+        for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(u[j]);
+        // columns that two vectors share have the same bits in both but where the lanes' maxima differ: there the first writes them
+        const int shared = kCommon && col.dup < V ? 0 : col.dup;
+        if constexpr (decltype(keep)::value) store_own(dx + static_cast<unsigned>(col.start), o, shared);
+        else store_once(dx + static_cast<unsigned>(col.start), o, shared);
       }
-      Elems<T, V> o;
-#pragma unroll
-      for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(u[j]);
-      // columns that two vectors share have the same bits in both but where the lanes' maxima differ: there the first writes them
-      const int shared = kCommon && col.dup < V ? 0 : col.dup;
-      if (A.keep) store_own(dx + static_cast<unsigned>(col.start), o, shared);
-      else store_once(dx + static_cast<unsigned>(col.start), o, shared);
-    }
+    };
+    if (A.keep) leave(std::true_type{});
+    else leave(std::false_type{});
   }
   leave_part<kBlock>(A, sum, rows);
 }
