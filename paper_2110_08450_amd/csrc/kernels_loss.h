@@ -123,7 +123,9 @@ constexpr int loss_threads(int lanes) { return lanes > kThreads ? lanes : kThrea
 
 // A group of LANES lanes has a row in its registers, NV vectors of V columns a lane: it reads it once, keeps the exponentials until their sum is known, and has its
 // next row on its way meanwhile.  The lane that has the label's column works out the loss.
-// Logits of long rows are read past the caches (8192 rows of 32 000 bfloat16 194 -> 184 us).
+// Logits of long rows are read past the caches (8192 rows of 32 000 bfloat16 194 -> 184 us).  Memory bounds it: 8192 rows of 50 K bfloat16 322 us, 5.1 TB/s;
+// 33 K rows of 1013 floats 52 us, 5.2 TB/s.  All vectors but a lane's last are known to be whole: with places of their own they took the registers that the next
+// row lies in (572 us for the first).
 template <typename T, int V, int NV, int LANES>
 __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs A) {
   constexpr int kBlock = loss_threads(LANES), kGroups = kBlock / LANES;
@@ -228,7 +230,8 @@ __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs 
   leave_part<kBlock>(A, sum, rows);
 }
 
-// Rows that outgrow the registers of a block: one to a block at a time, read twice, four vectors of a thread at once.  A thread has the same columns both times and
+// Rows that outgrow the registers of a block: one to a block at a time, read twice, four vectors of a thread at once (3000 rows of 128 K bfloat16 330 us, one at
+// a time 475; the second time they come from the memory side's cache).  A thread has the same columns both times and
 // writes no others, so that the gradient may take the place of the logits.
 constexpr int kLongLossThreads = 1024;
 template <typename T, int V>
