@@ -219,8 +219,8 @@ __host__ __device__ constexpr int adam_bytes_vector(size_t param, size_t grad) {
 __host__ __device__ constexpr uint32_t adam_bytes_wide(size_t param, size_t grad, int64_t cols) {
   return adam_bytes_vector(param, grad) == 8 && cols >= 8 ? 2 : 1;
 }
-// States of 8 bits: an item is a block of kStateBlock columns, whose largest values its lanes tell each other.  400 M bfloat16, 10 bytes each, 710 us (5.7 TB/s) of some
-// 55 vector instructions an element, which keep the chip's units as busy as its memory.
+// States of 8 bits: an item is a block of kStateBlock columns, whose largest values its lanes tell each other.  400 M bfloat16, 10 bytes each, 718 us (5.6 TB/s) with some
+// 55 vector instructions an element (counted).
 // Rows are read through the caches: those of few bytes share their lines with their neighbours (200 K rows of 100 halfs 404 us instead of 431).
 template <typename T, int V, bool ROWS>
 __device__ __forceinline__ Elems<T, V> load_bytes(const T* src) {

@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs 
 }
 
 // Rows that outgrow the registers of a block: one to a block at a time, read twice, four vectors of a thread at once (3000 rows of 128 K bfloat16 330 us, one at
-// a time 475; the second time they come from the memory side's cache).  A thread has the same columns both times and
+// a time 475).  A thread has the same columns both times and
 // writes no others, so that the gradient may take the place of the logits.
 constexpr int kLongLossThreads = 1024;
 template <typename T, int V>
