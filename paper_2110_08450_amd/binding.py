@@ -753,8 +753,8 @@ def adamw_list(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     lists = [params, grads, m, v] + [t if t is not None else [None] * n for t in (m_scales, v_scales, copies, rows, row_ids)]
     decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
     assert all(len(t) == n for t in lists) and len(decay) == n
-    own = [t.data_ptr() for t in (*params, *m, *v) if t.numel() > 0]
-    assert len(set(own)) == len(own), "a tensor twice"  # two steps of one tensor at once
+    own = [t.data_ptr() for t in (*params, *m, *v, *lists[4], *lists[5], *lists[6]) if t is not None and t.numel() > 0]
+    assert len(set(own)) == len(own), "a tensor twice"  # all that a step writes has one place each
     c = (_Param * max(1, n))()
     for e, p, g, a, b, sa, sb, copy, count, ids, wd in zip(c, *lists, decay):
         assert p.dtype in DTYPES and g.dtype in DTYPES and all(t.is_contiguous() and t.is_cuda for t in (p, g, a, b))

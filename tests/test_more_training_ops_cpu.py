@@ -184,3 +184,22 @@ def test_lists_of_tensors_are_checked():
         smfg.adamw_list([table], [tensor(3, 100)], [tensor(4, 200)], [tensor(4, 200)], row_ids=[tensor(3, dtype=torch.int32)])
     with pytest.raises(AssertionError):
         smfg.adamw_list([table], [tensor(3, 200)], [tensor(4, 200)], [tensor(4, 200)], row_ids=[tensor(2, dtype=torch.int32)])
+
+
+@pytest.mark.parametrize("shared", ["one tensor's scales", "two tensors' m_scales", "two tensors' v_scales", "two tensors' copies"])
+def test_lists_refuse_an_output_given_twice(shared):
+    """All that a step writes has one place each: of two writers either may be the last."""
+    p, g = [tensor(300), tensor(300)], [tensor(300), tensor(300)]
+    if shared == "two tensors' copies":
+        m, v, copies = [tensor(300), tensor(300)], [tensor(300), tensor(300)], [tensor(300, dtype=torch.float16)] * 2
+        lists = dict(copies=copies)
+        apart = dict(copies=[copies[0], tensor(300, dtype=torch.float16)])
+    else:
+        m, v = [tensor(300, dtype=torch.int8) for _ in range(2)], [tensor(300, dtype=torch.uint8) for _ in range(2)]
+        a = [tensor(3) for _ in range(4)]
+        apart = dict(m_scales=a[:2], v_scales=a[2:])
+        lists = {"one tensor's scales": dict(m_scales=a[:2], v_scales=[a[0], a[3]]), "two tensors' m_scales": dict(m_scales=[a[0], a[0]], v_scales=a[2:]),
+                 "two tensors' v_scales": dict(m_scales=a[:2], v_scales=[a[2], a[2]])}[shared]
+    assert smfg.adamw_list(p, g, m, v, **apart).n == 2
+    with pytest.raises(AssertionError, match="twice"):
+        smfg.adamw_list(p, g, m, v, **lists)
