@@ -68,13 +68,17 @@ bool launch_loss(LossArgs& A, Launches& go) {
   else if (vectors <= 768) f.template operator()<V, 3, 256>();
   else if (vectors <= 1024) f.template operator()<V, 2, 512>();
   else if (vectors <= 1536) f.template operator()<V, 3, 512>();
-  else if (vectors <= 2048) f.template operator()<V, 2, 1024>();
-  else if (vectors <= 3072) f.template operator()<V, 3, 1024>();
-  else if (vectors <= 4096) f.template operator()<V, 4, 1024>();
-  else if (vectors <= 5120) f.template operator()<V, 5, 1024>();
-  else if (vectors <= 6144) f.template operator()<V, 6, 1024>();
-  else if (vectors <= 7168) f.template operator()<V, 7, 1024>();
-  else return false;
+  else {
+    switch (ceil_div(vectors, 1024)) {  // a block of the largest size: as few vectors a lane as hold the row
+      case 2: f.template operator()<V, 2, 1024>(); break;
+      case 3: f.template operator()<V, 3, 1024>(); break;
+      case 4: f.template operator()<V, 4, 1024>(); break;
+      case 5: f.template operator()<V, 5, 1024>(); break;
+      case 6: f.template operator()<V, 6, 1024>(); break;
+      case 7: f.template operator()<V, 7, 1024>(); break;
+      default: return false;
+    }
+  }
   return true;
 }
 
