@@ -201,7 +201,8 @@ __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs 
       rows += live;
     }
     if (!A.dx) continue;
-    const float f = (kCommon ? 1.f : exp_of(base - base_of(all.m))) * (c / all.s);
+    // A lane whose columns are all -infinity has a factor of 0 beside its zeros: from its base of 0 the factor would be infinite where the row's largest logit is below -88.
+    const float f = (kCommon ? 1.f : exp_of(a.m - base_of(all.m))) * (c / all.s);
     T* dx = static_cast<T*>(A.dx) + row * A.dx_stride;
     const auto leave = [&](auto keep) {
 #pragma unroll

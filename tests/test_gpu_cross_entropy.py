@@ -239,3 +239,27 @@ def test_streams_and_again():
             outs.append((loss, row, dx))
         for o in outs[1:]:
             assert all(torch.equal(a, b) for a, b in zip(outs[0], o))
+
+
+@pytest.mark.parametrize("classes", [1500, 3000, 5000, 20_000, 28_672, 50_000, 57_344, 70_000])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("level", [-80.0, -100.0, -1000.0, -60_000.0])
+def test_masked_columns_beside_low_logits(classes, dtype, level):
+    """What is left of a row after masking may be far below zero: lanes that hold masked columns alone have no exponential, whatever the row's largest logit is."""
+    for masked in (NINF, torch.finfo(dtype).min):
+        x = torch.full((5, classes), masked, device=DEV)
+        x[0, :40] = torch.randn(40, device=DEV, generator=gen(1)) + level  # the head of a vocabulary
+        x[1, -9:] = torch.randn(9, device=DEV, generator=gen(2)) + level  # its end
+        x[2, classes // 2] = level  # one class
+        x[3, ::2] = torch.randn(len(range(0, classes, 2)), device=DEV, generator=gen(3)) + level
+        x[4, :40] = level
+        x = x.to(dtype)
+        y = torch.tensor([3, classes - 2, classes // 2, 0, -100], device=DEV)
+        loss, row, dx, ws = torch.zeros(1, device=DEV), torch.zeros(5, device=DEV), torch.empty_like(x), smfg.cross_entropy_workspace(5, classes)
+        smfg.cross_entropy(x, y, count(5), 5, loss, ws, grad_logits=dx, row_loss=row, scale=0.5)
+        want, grad, _, tol_row, tol = loss_of(x, y, 0.5 / 4)
+        check(row, want, rounded(tol_row, want, F32))
+        check(dx, grad, rounded(tol, grad, dtype))
+        z = x.clone()
+        smfg.cross_entropy(z, y, count(5), 5, loss, ws, grad_logits=z, scale=0.5)
+        assert torch.equal(z, dx)
