@@ -375,7 +375,7 @@ int smfg_layer_norm_grad(const void *d_dy, int64_t dy_stride, const void *d_x, i
  *               SMFG_DTYPE_I8    y = s q, q a whole number in [-127, 127], s = (largest |y|) / 127
  *               SMFG_DTYPE_E4M3  y = s q, q a float of 8 bits (4 of exponent, 3 of mantissa, no infinities), s = (largest |y|) / 448
  *             for every `group` consecutive columns of a row (32, 64 or 128; 0: the whole row), q rounded to nearest even.  A largest value below
- *             2^-120 counts as 0: s = 0, q = 0.  With an infinity or a NaN among the values s is NaN and q = 0.
+ *             2^-120 (e4m3: 2^-119) counts as 0: s = 0, q = 0.  With an infinity or a NaN among the values s is NaN and q = 0.
  *   d_scales  float, s of group k of row i at i * scales_stride + k; NULL if y is of dtype
  *   d_rstd    float [max_rows], r for the gradient, or NULL
  * Squares are added in float (in double in rows of over 16384 halfs or 8192 floats).

@@ -68,14 +68,15 @@ __device__ __forceinline__ Elems<T, V> load_row(const T* src) {
   else return *reinterpret_cast<const Elems<T, V>*>(src);
 }
 
-// The scale of values up to a largest magnitude, and what they are multiplied by.  The largest becomes 127, or 448, the largest e4m3.  Below 2^-120 its
-// inverse would leave a float's range: all are zeros then, and the scale as well.  With an infinity or a NaN among them the scale is NaN.
+// The scale of values up to a largest magnitude, and what they are multiplied by.  The largest becomes 127, or 448, the largest e4m3.  Below 2^-120 (e4m3: 2^-119) the
+// factor would leave a float's range, of which 127 * 2^120 and 448 * 2^119 are the last: all are zeros then, and the scale as well.  With an infinity or a NaN
+// among them the scale is NaN.
 struct ByteScale {
   float scale, inverse;
 };
 __device__ __forceinline__ ByteScale byte_scale(uint32_t top, bool e4m3) {
   const float most = e4m3 ? 448.f : 127.f;
-  if (top < 0x03800000u) return {0.f, 0.f};
+  if (top < (e4m3 ? 0x04000000u : 0x03800000u)) return {0.f, 0.f};
   if (top >= 0x7f800000u) return {__uint_as_float(0x7fc00000u), 0.f};
   return {__uint_as_float(top) / most, most / __uint_as_float(top)};
 }

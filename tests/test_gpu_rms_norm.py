@@ -290,3 +290,25 @@ def test_many_rows_and_streams():
         assert torch.equal(a, b)
     want, rs, tol, _ = norm_of(outs[0][1], torch.ones(dim, device=DEV), 1e-5)
     check(outs[0][0], want, rounded(tol, want, F16))
+
+
+@pytest.mark.parametrize("out,least", [(I8, 2.0 ** -120), (E4M3, 2.0 ** -119)])
+@pytest.mark.parametrize("group", [0, 32])
+@pytest.mark.parametrize("dim", [7, 64, 1000, 9000])
+def test_bytes_of_groups_of_tiny_values(dim, group, out, least):
+    """Down to the largest value that counts as 0 the factor, 127 or 448 divided by the group's largest, is a float.  Rows of ones have the weight as their norm;
+    the shares of the largest value lie apart from what two neighbours of 8 bits have in their middle."""
+    share = torch.tensor([0.7, -1.0, 0.0, -0.3], device=DEV).repeat(-(-dim // 4))[:dim]
+    groups, width = -(-dim // group) if group else 1, group or dim
+    q = (share * TOP[out]).round() if out == I8 else (share * TOP[out]).to(E4M3).float()
+    for top in (2.0 ** -124, 2.0 ** -121, 2.0 ** -120, 1.5 * 2.0 ** -120, 1.74 * 2.0 ** -120, 1.76 * 2.0 ** -120, 2.0 ** -119, 2.0 ** -100):
+        y, s = torch.full((2, dim), 85, dtype=torch.uint8, device=DEV).view(out), torch.full((2, groups), 9.0, device=DEV)
+        smfg.rms_norm(torch.ones((2, dim), device=DEV), count(2), 2, share * top, 0.0, y, scales=s, group=group)
+        if top < least:
+            assert not s.any() and not y.float().any()
+            continue
+        tops = torch.nn.functional.pad(share.abs(), (0, groups * width - dim)).view(groups, width).amax(1) * top
+        assert bool((tops == top).all())
+        # one rounding; a scale below a float's normal range has the steps of its least numbers
+        check(s, (tops.double() / TOP[out])[None].expand(2, -1), U * s.double() + 2.0 ** -150)
+        assert torch.equal(y.float(), q[None].expand(2, -1))
