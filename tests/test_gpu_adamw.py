@@ -394,3 +394,28 @@ def test_streams_and_again():
             outs.append([x for t in tensors for x in (t.p, t.m, t.v, t.copy)])
         for o in outs[1:]:
             assert all(torch.equal(a, b) for a, b in zip(outs[0], o))
+
+
+@pytest.mark.parametrize("bytes_", [False, True])
+@pytest.mark.parametrize("by_row", [False, True])
+@pytest.mark.parametrize("k", [3, 16, 1000])
+def test_a_small_decay_is_as_large_as_it_should_be(k, by_row, bytes_):
+    """lr weight_decay = d = (k + 1/2) 2^-24: exact as a product, and in the middle between two values of 1 - d.  The change d p of parameters in [1, 2) is rounded to
+    steps of 2^-23, to either side: what d p / 2^-23, which runs over L = k / 2 + 1 / 4 steps, is off by evens out over whole steps, and leaves an eighth of a step times
+    1 / L in the mean at most.  2^20 values of p stand for all of them: their mean is off by 2 L 2^-20 < 2^-10 steps at most (a sawtooth of L teeth).  The product rounds by U."""
+    n, d = 1 << 20, (k + 0.5) * 2.0 ** -24
+    p = (1 + torch.arange(n, device=DEV) * 2.0 ** -20).reshape(-1, 512 if by_row else n)
+    p = p if by_row else p.reshape(-1)
+    before = p.clone()
+    g, m, v = torch.zeros_like(p), torch.zeros_like(p), torch.zeros_like(p)
+    scales = {}
+    if bytes_:
+        m, v = m.to(torch.int8), v.to(torch.uint8)
+        shape = (p.shape[0], 4) if by_row else (n // B,)
+        scales = dict(m_scales=[torch.zeros(shape, device=DEV)], v_scales=[torch.zeros(shape, device=DEV)])
+    smfg.adamw(smfg.adamw_list([p], [g], [m], [v], weight_decay=(k + 0.5) * 2.0 ** -14, **scales), 1, 2.0 ** -10)
+    moved = float((before.double() - p.double()).mean())
+    want = d * float(before.double().mean())
+    assert abs(moved - want) <= 2.0 ** -23 * (1 / 8 / (k / 2 + 0.25) + 2.0 ** -10) + 2 * U * want
+    # and each by its own
+    assert float(((before.double() - p.double()) - d * before.double()).abs().max()) <= 2.0 ** -24 * 1.001 + 2 * U * d * 2
