@@ -746,8 +746,8 @@ def adamw_list(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
                copies: Optional[Sequence[Optional[torch.Tensor]]] = None, rows: Optional[Sequence[Optional[torch.Tensor]]] = None,
                row_ids: Optional[Sequence[Optional[torch.Tensor]]] = None, weight_decay=0.0) -> AdamWList:
     """The buffers of adamw: contiguous parameters, their gradients and states.  m[i], v[i] float32, or int8 and uint8 with m_scales[i], v_scales[i]
-    (float32, one for each STATE_BLOCK elements: of the whole tensor if they have one dimension, of each row if they have two).  copies[i] (float16 or bfloat16):
-    where float32 parameters are written to as well, rounded.  row_ids[i] (int32): the rows of params[i] that grads[i] has rows of, rows[i] (device int64) how many
+    (float32, one for each STATE_BLOCK elements: of the whole tensor if they have one dimension, of each row if they have two, as they have to where rows or row_ids
+    are given).  copies[i] (float16 or bfloat16): where float32 parameters are written to as well, rounded.  row_ids[i] (int32): the rows of params[i] that grads[i] has rows of, rows[i] (device int64) how many
     of them count (None: all), as embedding_grad_rows tells both.  weight_decay: one for all, or one each.  What the buffers hold is read by each step anew."""
     n = len(params)
     lists = [params, grads, m, v] + [t if t is not None else [None] * n for t in (m_scales, v_scales, copies, rows, row_ids)]
@@ -767,7 +767,9 @@ def adamw_list(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
             e.state_bits = 32
         else:
             assert a.dtype == torch.int8 and b.dtype == torch.uint8 and sa is not None and sb is not None and sa.shape == sb.shape
-            by_row = by_row or sa.dim() == 2
+            # their shape tells adamw_values how they lie
+            by_row = by_row or sa.dim() != 1
+            assert not by_row or sa.dim() == 2 and sa.shape[0] == p.shape[0], "scales"
             want = (p.shape[0] if by_row else 1) * -(-(p.numel() // max(1, p.shape[0]) if by_row else p.numel()) // STATE_BLOCK)
             assert all(t.dtype == torch.float32 and t.is_contiguous() and t.is_cuda and t.numel() == want for t in (sa, sb))
             e.state_bits, e.m_scale, e.v_scale = 8, sa.data_ptr(), sb.data_ptr()
@@ -804,7 +806,7 @@ def adamw_values(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, s
     assert all(t.is_contiguous() and t.is_cuda for t in (codes, scales, out)) and scales.dtype == torch.float32
     rows = codes.shape[0] if scales.dim() == 2 else 1
     cols = codes.numel() // max(1, rows)
-    assert scales.numel() == rows * -(-cols // STATE_BLOCK)
+    assert scales.numel() == rows * -(-cols // STATE_BLOCK) and (scales.dim() == 1 or scales.dim() == 2 and scales.shape[0] == rows), "scales"
     rc = lib().smfg_adamw_values(codes.data_ptr(), scales.data_ptr(), codes.numel(), cols if scales.dim() == 2 else 0, int(codes.dtype == torch.uint8),
                                  out.data_ptr(), DTYPES[out.dtype], _raw_stream(stream))
     _check(rc, "smfg_adamw_values")

@@ -203,3 +203,29 @@ def test_lists_refuse_an_output_given_twice(shared):
     assert smfg.adamw_list(p, g, m, v, **apart).n == 2
     with pytest.raises(AssertionError, match="twice"):
         smfg.adamw_list(p, g, m, v, **lists)
+
+
+@pytest.mark.parametrize("by", ["rows", "row_ids"])
+def test_scales_of_tensors_that_are_stepped_by_row_have_two_dimensions(by):
+    """5 rows of 120 have as many blocks by row as in one piece: 5.  A step by row uses a scale for each row, while one dimension tells adamw_values that the second
+    begins at element 128."""
+    p, g, m, v = tensor(5, 120), tensor(5, 120), tensor(5, 120, dtype=torch.int8), tensor(5, 120, dtype=torch.uint8)
+    more = dict(rows=[tensor(1, dtype=torch.int64)]) if by == "rows" else dict(row_ids=[tensor(5, dtype=torch.int32)])
+
+    def made(*shape, **more):
+        return smfg.adamw_list([p], [g], [m], [v], m_scales=[tensor(*shape)], v_scales=[tensor(*shape)], **more)
+
+    assert made(5, 1, **more).c[0].row_elems == 120 == made(5, 1).c[0].row_elems and made(5).c[0].row_elems == 0
+    for shape in ((5,), (1, 5), (1, 5, 1), (5, 1, 1), (6, 1)):
+        with pytest.raises(AssertionError):
+            made(*shape, **more)
+    for shape in ((1, 5), (1, 5, 1), (4,), (4, 1)):
+        with pytest.raises(AssertionError):
+            made(*shape)
+
+
+@pytest.mark.parametrize("codes,scales", [((5, 120), (1, 5)), ((5, 120), (5, 1, 1)), ((5, 120), (4,)), ((5, 120), (6,)), ((5, 120), (5, 2)), ((600,), (1, 5)), ((600,), (5, 1)),
+                                          ((5, 120), ())])
+def test_values_refuse_scales_that_are_not_their_rows(codes, scales):
+    with pytest.raises(AssertionError):
+        smfg.adamw_values(tensor(*codes, dtype=torch.int8), tensor(*scales), tensor(*codes))
