@@ -444,7 +444,7 @@ int smfg_clip_grad_norm(const smfg_grad_t *grads /* host */, int32_t num_grads, 
  *   p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),  
  *   f = scale min(1, max_norm / (|scale| norm + 1e-6))
  * With d_norm, the norm of the gradients as they are (smfg_clip_grad_norm with scale 1, an infinite max_norm and no outputs finds it and writes nothing else),
- * they are clipped here, and not written; where *d_norm is not finite the step is not taken: nothing is written.  Without it f = scale.
+ * they are clipped here, and not written; where *d_norm is not finite the step is not taken: nothing is written.  Without it f = scale, whatever max_norm is.
  * No two of the buffers written to share memory.
  * A tensor is of rows of row_elems elements (0: a single row of numel).  With d_row_ids the gradient's row i is that of row d_row_ids[i] of a table of
  * num_rows rows (param, m, v and copy), whose other rows are left as they are: the touched rows that smfg_embedding_grad_rows tells.  These ids are

@@ -793,7 +793,8 @@ def adamw(params: AdamWList, step: int, lr: float, betas=(0.9, 0.999), eps: floa
           stream: Optional[torch.cuda.Stream] = None) -> None:
     """One step of AdamW, step + device_step (device int64) the first being 1, with lr * device_lr (device float32).  Gradients are multiplied by
     scale, and by min(1, max_norm / (|scale| norm + 1e-6)) where norm (device float32), that of the gradients as they are, is given; if that is not finite the step
-    is not taken."""
+    is not taken.  A max_norm without a norm is refused, as nothing would be clipped."""
+    assert norm is not None or max_norm == float("inf"), "max_norm without norm"
     h = _AdamW(lr, betas[0], betas[1], eps, scale, max_norm, step, _vector(device_step, 1, torch.int64, "device_step"),
                _vector(device_lr, 1, torch.float32, "device_lr"), _vector(norm, 1, torch.float32, "norm"))
     rc = lib().smfg_adamw(params.c, params.n, h, _raw_stream(stream))

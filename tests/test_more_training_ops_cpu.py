@@ -229,3 +229,11 @@ def test_scales_of_tensors_that_are_stepped_by_row_have_two_dimensions(by):
 def test_values_refuse_scales_that_are_not_their_rows(codes, scales):
     with pytest.raises(AssertionError):
         smfg.adamw_values(tensor(*codes, dtype=torch.int8), tensor(*scales), tensor(*codes))
+
+
+def test_a_limit_without_a_norm_is_refused():
+    """The norm is found by clip_grad_norm; without one a step would be of the gradients as they are, whatever the limit."""
+    empty = smfg.adamw_list([], [], [], [])
+    for max_norm in (1.0, 1e30, float("nan")):
+        with pytest.raises(AssertionError, match="norm"):
+            smfg.adamw(empty, 1, 1e-3, max_norm=max_norm)
