@@ -455,6 +455,14 @@ int smfg_clip_grad_norm(const smfg_grad_t *grads /* host */, int32_t num_grads, 
  * are what is next to the value in k, A and B being the largest |m| and sqrt(v) of the elements; v > 0 is kept as k >= 1.  A below 2^-100 counts as 0, and v below 2^-126.
  * An infinity or a NaN in m or v makes the kept state of its block NaN.  Zeroed memory is the state of zeros, of either kind.  The step itself uses m
  * and v before they are rounded.
+ * States of 8 bits are rounded to the nearest in each step, so that slow changes are lost: k moves only where a step changes it by a half or more, for m if about
+ * (1 - beta1) |g' / m - 1| k > 1, for v if (1 - beta2) |g'^2 / v - 1| k > 2.  An element that does not move keeps its share of its block's largest, whatever its gradients do meanwhile.
+ * With beta2 = 0.999 gradients that get smaller never lower a k of v, and it rises only where g'^2 > (1 + 2000 / k) v, so that steps are too small behind the former, and behind gradients that
+ * get larger up to sqrt(1 + 2000 / k) times too large; with 0.99 the first holds for k up to 200, with 0.95 up to 40.  By a simulation with normal gradients of one size (256 blocks) sqrt(v) is
+ * off by 5 % (rms) after 1000 steps and 15 % after 3000 with beta2 = 0.999, by 1.6 % with 0.99, by 0.8 % with 0.95; where half of a block's gradients become a quarter, theirs is 1.6 times too large
+ * 1000 steps later and 4.3 times 6000 steps later with 0.999, 1 % with 0.99.  Where that matters: states of floats, or beta2 <= 0.99.
+ * Parameters of half or bfloat16 that are not copies of float ones lose what a step changes by less than half their last digit: 2^-12 to 2^-11
+ * of the value, or 2^-9 to 2^-8.
  */
 #define SMFG_STATE_BLOCK 128
 typedef struct {

@@ -748,7 +748,9 @@ def adamw_list(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m:
     """The buffers of adamw: contiguous parameters, their gradients and states.  m[i], v[i] float32, or int8 and uint8 with m_scales[i], v_scales[i]
     (float32, one for each STATE_BLOCK elements: of the whole tensor if they have one dimension, of each row if they have two, as they have to where rows or row_ids
     are given).  copies[i] (float16 or bfloat16): where float32 parameters are written to as well, rounded.  row_ids[i] (int32): the rows of params[i] that grads[i] has rows of, rows[i] (device int64) how many
-    of them count (None: all), as embedding_grad_rows tells both.  weight_decay: one for all, or one each.  What the buffers hold is read by each step anew."""
+    of them count (None: all), as embedding_grad_rows tells both.  weight_decay: one for all, or one each.  What the buffers hold is read by each step anew.
+    States of 8 bits lose slow changes: with betas[1] = 0.999 the second moment follows its block's largest more than its own gradients (smfg.h has the rule and figures); 0.99 or less, or float
+    states, do not.  Parameters of 16 bits lose updates below half their last digit: keep float32 ones, with copies, where that matters."""
     n = len(params)
     lists = [params, grads, m, v] + [t if t is not None else [None] * n for t in (m_scales, v_scales, copies, rows, row_ids)]
     decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n

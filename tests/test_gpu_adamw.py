@@ -419,3 +419,47 @@ def test_a_small_decay_is_as_large_as_it_should_be(k, by_row, bytes_):
     assert abs(moved - want) <= 2.0 ** -23 * (1 / 8 / (k / 2 + 0.25) + 2.0 ** -10) + 2 * U * want
     # and each by its own
     assert float(((before.double() - p.double()) - d * before.double()).abs().max()) <= 2.0 ** -24 * 1.001 + 2 * U * d * 2
+
+
+@pytest.mark.parametrize("beta2,factor,most", [(0.999, 0.0, 250), (0.999, 2.0, 250), (0.999, 10.0, 60), (0.99, 0.0, 230), (0.95, 0.0, 250), (0.95, 2.0, 128)])
+def test_second_moments_of_8_bits_over_many_steps(beta2, factor, most):
+    """One element of a block keeps its gradient, all others' have become `factor` times their root of v.  The states are the ones that the definition with its rounding gives,
+    step by step in 64 bits, for all whose number is never within 2^-10 of the middle between two (v is off by 23 U, its root's root by a quarter, and by 6 U for itself: below
+    2^-12 of up to 255).  A number stays for good where a step changes it by less than a half, and the moment then has its share of the block's largest: the
+    deviation from the moments without rounding is what it is by that."""
+    steps = 200
+    k = torch.ceil(torch.arange(1, B + 1, dtype=torch.float64) * most / B)
+    k[0] = 255
+    first, g = k.clone(), (factor * (k / 255) ** 2).float()
+    g[0] = 1.0
+    p, m, v = torch.zeros(B, device=DEV), torch.zeros(B, dtype=torch.int8, device=DEV), k.to(torch.uint8).to(DEV)
+    ms, vs = torch.zeros(1, device=DEV), torch.ones(1, device=DEV)
+    lst = smfg.adamw_list([p], [g.to(DEV)], [m], [v], [ms], [vs])
+    gg, top, exact, apart = g.double(), 1.0, (k / 255) ** 4, torch.ones(B, dtype=torch.float64)
+    for i in range(1, steps + 1):
+        smfg.adamw(lst, i, LR, betas=(B1, beta2), eps=EPS)
+        root = torch.sqrt(beta2 * (top * (k / 255) ** 2) ** 2 + (1 - beta2) * gg * gg)
+        exact = beta2 * exact + (1 - beta2) * gg * gg
+        top = float(root.max())
+        x = 255 * torch.sqrt(root / top)
+        apart = torch.minimum(apart, (x % 1 - 0.5).abs())
+        k = torch.round(x).clamp(min=1)
+    sure = apart > 2.0 ** -10
+    assert int(sure.sum()) >= 96
+    assert torch.equal(v.cpu()[sure].double(), k[sure])
+    # the root of v is off by 15 U a step relative to the block's largest, which has nothing to be rounded to
+    assert abs(float(vs) - top) <= 20 * steps * U * top
+    still = (first * (1 + (1 - beta2) * (factor ** 2 - 1)) ** 0.25 - first).abs() < 0.499
+    still[0] = True
+    assert torch.equal(k[still], first[still]) and bool((k != first)[~still].all())
+    out = torch.empty(B, device=DEV)
+    smfg.adamw_values(v, vs, out)
+    share = (top * (k / 255) ** 2) ** 2
+    assert bool(((out.cpu().double() - share).abs() <= (2 * 20 * steps + 11) * U * share)[sure].all())
+    off = (share / exact)[1:]
+    if factor == 0.0:  # what stays is too large by what the moment should have lost
+        want = beta2 ** -steps
+        assert bool((((off - want).abs() <= 1e-9 * want) == still[1:]).all()) and bool((off <= want * (1 + 1e-9)).all())
+    else:  # what stays is too small by what it should have gained
+        want = 1 / (beta2 ** steps + (1 - beta2 ** steps) * factor ** 2)
+        assert bool((((off - want).abs() <= 1e-6 * want) == still[1:]).all()) and bool((off >= want * (1 - 1e-6)).all())
