@@ -47,9 +47,10 @@ inline int64_t items_of(const smfg_param_t& p) {
   if (cols == 0) return 0;
   return p.numel / cols * (p.state_bits == 8 ? ceil_div(cols, kStateBlock) : cols >= kAdamFloats ? ceil_div(cols, kAdamFloats) : cols);
 }
-// Blocks of threads, and how many times kStateBlock elements each has.  States of floats: a vector a thread (400 M of them 2040 us; two 2100, 16 2150, 64 2250),
-// as short-lived blocks keep the memory busiest.  Of 8 bits: what leaves 2048 blocks, but 16 at least and 64 at most (1204; 16 1700, 32 1229), as they have
-// more to work out before they begin.  More, up to 512, where there would be over 2^20 blocks.
+// Blocks of threads, and how many times kStateBlock elements each has.  States of floats: 8, a vector a thread, as short-lived blocks keep the memory busiest (400 M with half
+// gradients and copies 1840 us; 16 1875, 64 2140, 128 2220).  Of 8 bits, which have more to work out before they begin: 16, and with adam_bytes_wide 32 (400 M bfloat16 704 to 720 us;
+// half as many 755, twice 789, four times 855; 300 M floats by half gradients 722, 786, 778 and 822).  Small calls and touched rows lean to either side: 20 M bfloat16 91 us,
+// with half as many 79; 200 K rows of 100 floats 91, with half 103, with twice 87.  More, up to 512, where there would be over 2^20 blocks.
 struct AdamShape {
   int64_t blocks[2];  // for states of floats, of 8 bits
   bool keep;          // parameters and copies are few enough to be kept for the next pass

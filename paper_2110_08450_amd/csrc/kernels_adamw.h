@@ -176,7 +176,7 @@ __device__ __forceinline__ void store_params(const AdamTensor& T, int64_t at, co
 }
 
 // States of floats: an item is a vector of V columns.  Memory bounds it: 400 M floats with half gradients and copies 1845 us, 6.1 TB/s; 240 K rows of 100 floats of a
-// table 198 us for 673 MB, as rows that begin within 64 bytes cost the lines at both ends (of 96 floats the same bytes take 131).
+// table 190 to 199 us for 673 MB, as rows that begin within 64 bytes cost the lines at both ends (of 96 floats the same bytes take 131).
 constexpr int kAdamFloats = 4;  // columns of a vector
 template <typename TP, typename TG, int V>
 __device__ __forceinline__ void adam_floats(const AdamArgs& A, const AdamTensor& T, const AdamStep& S, uint32_t q) {
@@ -222,7 +222,8 @@ __host__ __device__ constexpr uint32_t adam_bytes_wide(size_t param, size_t grad
 }
 // States of 8 bits: an item is a block of kStateBlock columns, whose largest values its lanes tell each other.  400 M bfloat16, 10 bytes each, 718 us (5.6 TB/s) with some
 // 55 vector instructions an element (counted).
-// Rows are read through the caches: those of few bytes share their lines with their neighbours (200 K rows of 100 halfs 404 us instead of 431).
+// Rows are read through the caches: those of few bytes share their lines with their neighbours, and a row has four bytes of a line of each scale.  200 K rows of 100 floats
+// of a table of 2 M by half gradients 91 us (110 past the caches) for 284 MB; of 96 81 (80), of 128 80 (76).
 template <typename T, int V, bool ROWS>
 __device__ __forceinline__ Elems<T, V> load_bytes(const T* src) {
   if constexpr (ROWS) return *reinterpret_cast<const Elems<T, V>*>(src);

@@ -76,7 +76,8 @@ __device__ __forceinline__ float gradient_scale(const LossArgs& A, int64_t n, in
   return rows > 0 ? A.scale / static_cast<float>(rows) : 0.f;
 }
 
-// exp(x) by the hardware's power of two: a result below 2^-126 is zero.
+// exp(x), x <= 0, by the hardware's power of two: a result below 2^-126 is zero.  The exponent is a product of two rounded numbers, rounded: with the rounding of x
+// itself a result is off by up to 3 * 2^-24 |x| of itself.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
 
 // Maximum, and sum of exponentials relative to it, of several lanes: each lane brings its own maximum (-inf: none) and its sum relative to that.
@@ -123,8 +124,10 @@ constexpr int loss_threads(int lanes) { return lanes > kThreads ? lanes : kThrea
 
 // A group of LANES lanes has a row in its registers, NV vectors of V columns a lane: it reads it once, keeps the exponentials until their sum is known, and has its
 // next row on its way meanwhile.  The lane that has the label's column works out the loss.
-// Logits of long rows are read past the caches (8192 rows of 32 000 bfloat16 194 -> 184 us).  Memory bounds it: 8192 rows of 50 K bfloat16 322 us, 5.1 TB/s;
-// 33 K rows of 1013 floats 52 us, 5.2 TB/s.  All vectors but a lane's last are known to be whole: with places of their own they took the registers that the next
+// Logits of rows of 1024 lanes are read past the caches: of 1000 rows of 50 K bfloat16, 100 MB, 50.6 us instead of 57.0 (with a pass over the gradient behind 80 and 88); of
+// 8192, where nothing stays in them, 321 and 314 (587 and 582), of 32 000 columns 200 either way.  Fewer lanes read through them: 10 K rows of 8192 70 us (past them 67.5), 8192 of
+// 12 000 83.5 (84), 16 K of 4096 60 (54.7), 80 K of 1000 70.6 (68), 150 K of 172 halfs 37.2 (39.8), 50 K of 700 floats 61.5 (52.9).  Memory bounds it: 8192 rows of 50 K bfloat16
+// 322 us, 5.1 TB/s; 33 K rows of 1013 floats 52 us, 5.2 TB/s.  All vectors but a lane's last are known to be whole: with places of their own they took the registers that the next
 // row lies in (572 us for the first).
 template <typename T, int V, int NV, int LANES>
 __global__ void __launch_bounds__(loss_threads(LANES)) k_cross_entropy(LossArgs A) {

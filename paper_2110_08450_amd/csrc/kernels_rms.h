@@ -61,7 +61,10 @@ __device__ __forceinline__ uint32_t group_max(uint32_t x, uint32_t* lds) {
 }
 
 // Rows of 128 vectors and more are read past the caches, and the sum, which the next layer reads much later, is written past them; what the next operator reads is
-// not (16 K rows of 4096 halfs with the sum 100 -> 80 us, with a product of y behind it 145 -> 118; y past the caches as well 80, and 152).
+// not (16 K rows of 4096 halfs with the sum 100 -> 80 us, with a product of y behind it 145 -> 118; y past the caches as well 80, and 152).  Both ways of reading, halfs
+// with the sum, alone / with a pass over y behind: 16 K x 4096 through 102 / 149 us, past 83 / 140; 50 K x 2048 156 / 227 and 157 / 216; 100 K x 1024 (128 vectors) 153 / 224
+// and 157 / 215; 20 K x 1024 26 / 41 and 28 / 39.  Below the limit, where they are read through, 200 K x 512 158 / 228 and 160 / 218; 154 K x 256 60 / 88 and 52 / 75: narrower
+// rows would gain as well, down to 16 vectors (400 K x 128 78 / 114 and 65 / 102).  The gradient likewise: 94 / 142 past for 104 / 153 at 4096, 65 / 94 through for 57 / 81 at 256.
 template <typename T, int V, int VECTORS>
 __device__ __forceinline__ Elems<T, V> load_row(const T* src) {
   if constexpr (VECTORS >= 128) return load_once<T, V>(src);

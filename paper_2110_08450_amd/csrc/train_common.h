@@ -73,7 +73,8 @@ constexpr int kVec = 16 / static_cast<int>(sizeof(T));  // columns of a 16-byte 
 
 // What the next operator reads stays in the caches if it is no more than this, twice the 256 MB that the memory side's has; more of it goes past them.  Measured with a product of
 // it behind the operator: gradients of 30 K rows of 4096 logits, 246 MB, 186 us kept and 194 past the caches; 40 K rows 246 and 256; 8192 rows of 50 K, 819 MB,
-// 615 and 590.  Parameters: 50 M floats and their half copies, 300 MB, 255 us kept and 271 past; 400 M with copies, the step alone, 1985 and 1832.
+// 615 and 590.  Parameters: 50 M floats and their half copies, 300 MB, 255 us kept and 271 past; 400 M with copies, the step alone, 1985 and 1832.  It goes by the
+// size of the arrays, as how many of their rows are in use is not known on the host.  The norm's outputs always stay.
 constexpr double kKeptBytes = 512.0 * (1 << 20);
 
 // ---- rows in registers --------------------------------------------------------------------------
