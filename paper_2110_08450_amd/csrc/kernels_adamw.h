@@ -106,11 +106,13 @@ __device__ __forceinline__ void adam_gradient(const AdamStep& S, const Elems<TG,
 }
 // The parameter from the moments, and the root of the second.  States of 8 bits keep the hardware busy with roots: theirs are its own, off by one in the last digit
 // (a v below 2^-126 counts as 0), and the quotient is a product with its reciprocal; floats, which the memory bounds, have the exact ones.
-// What is taken from the parameter is added up before: 1 - lr decay as a float has steps of 2^-24, which a decay of 1e-7 misses by 19 %, of 2e-8 altogether.
+// What is taken from the parameter is added up before: 1 - lr decay as a float has steps of 2^-24, which a decay of 1e-7 misses by 19 %, of 2e-8 altogether.  An infinite
+// parameter, such as a mask's, has the largest float's decay, so that it stays what it is.
 template <bool FAST>
 __device__ __forceinline__ float adam_update(const AdamStep& S, float decay, float& p, float m, float v) {
   const float root = FAST ? __builtin_amdgcn_sqrtf(v) : sqrtf(v), den = root * S.root + S.eps;
-  p -= decay * p + (FAST ? S.step * m * __builtin_amdgcn_rcpf(den) : S.step * m / den);
+  constexpr float kMost = 0x1.fffffep127f;
+  p -= decay * __builtin_amdgcn_fmed3f(p, -kMost, kMost) + (FAST ? S.step * m * __builtin_amdgcn_rcpf(den) : S.step * m / den);
   return root;
 }
 
@@ -221,7 +223,7 @@ __host__ __device__ constexpr uint32_t adam_bytes_wide(size_t param, size_t grad
   return adam_bytes_vector(param, grad) == 8 && cols >= 8 ? 2 : 1;
 }
 // States of 8 bits: an item is a block of kStateBlock columns, whose largest values its lanes tell each other.  400 M bfloat16, 10 bytes each, 718 us (5.6 TB/s) with some
-// 55 vector instructions an element (counted).
+// 57 vector instructions an element (counted).
 // Rows are read through the caches: those of few bytes share their lines with their neighbours, and a row has four bytes of a line of each scale.  200 K rows of 100 floats
 // of a table of 2 M by half gradients 91 us (110 past the caches) for 284 MB; of 96 81 (80), of 128 80 (76).
 template <typename T, int V, bool ROWS>

@@ -463,3 +463,19 @@ def test_second_moments_of_8_bits_over_many_steps(beta2, factor, most):
     else:  # what stays is too small by what it should have gained
         want = 1 / (beta2 ** steps + (1 - beta2 ** steps) * factor ** 2)
         assert bool((((off - want).abs() <= 1e-6 * want) == still[1:]).all()) and bool((off >= want * (1 - 1e-6)).all())
+
+
+@pytest.mark.parametrize("bytes_", [False, True])
+@pytest.mark.parametrize("ptype", [F32, F16, BF16])
+@pytest.mark.parametrize("decay", [0.0, WD])
+def test_infinite_parameters_stay_infinite(decay, ptype, bytes_):
+    """A parameter of -infinity masks what it is added to; a step with a finite gradient leaves it there, a NaN is one behind the step too, and the others take theirs."""
+    t = Tensor((1000,), ptype, ptype, None, bytes_, 11, decay=decay)
+    t.p[7::100], t.p[8::100], t.p[9::100] = float("-inf"), float("inf"), float("nan")
+    t.g[7:500:100] = 0.0
+    before = (t.p.clone(), t.state(), t.g.clone())
+    run([t], step=3)
+    fine = before[0].isfinite()
+    assert int(fine.sum()) == 970 and torch.equal(t.p.isnan(), before[0].isnan()) and bool((t.p[7::100] == float("-inf")).all()) and bool((t.p[8::100] == float("inf")).all())
+    want, _, _, tp, _, _ = step_of(*before[:1], *before[1][:2], before[2], *before[1][2:], 3, 1.0, decay)
+    check(t.p[fine], want[fine], rounded(tp, want, ptype)[fine])
